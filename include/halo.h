@@ -341,6 +341,79 @@ halo_status halo_peft_bwd(const halo_linear_desc* desc, int32_t rank, const void
                           const int8_t* Wq, const float* s_w, const void* U, const void* V, void* EX, float* GU, float* GV,
                           void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Dropout from a counter-based generator.   out = residual + drop(in), with a mask that is never stored:
+ *
+ *   drop(in)[i, j] = in[i, j] * 65536 / (65536 - q)  where the element is kept, 0 elsewhere (whatever in[i, j] is);  q = rint(65536 p).
+ *   The element is kept where its 16 random bits, as a number, are at least q: half j % 2 (the low one first) of word (j % 8) / 2 of
+ *   Philox4x32-10 with the counter words (j / 8, i, offset mod 2^32, offset / 2^32) and the key (seed mod 2^32, seed / 2^32).
+ *
+ * The mask depends on (seed, offset, i, j) alone, neither on ld nor on the machine, so the gradient of the branch is the same call
+ * on the output's gradient, without the residual.  A caller takes another offset for every tensor and step.
+ *
+ *   in, residual, out   [rows x cols] of type dt (bf16 or fp32), each with its own leading dimension; residual may be NULL (0).  out
+ *                       may be in or residual themselves (same leading dimension), and overlap neither otherwise.
+ *   p                   probability of zero, in [0, 1] (HALO_EINVAL otherwise).
+ * The sum is formed in fp32 and rounded once.  rows == 0 or cols == 0 is a no-op.
+ */
+halo_status halo_dropout(const void* in, halo_dtype dt, int64_t rows, int64_t cols, int64_t ld_in, const void* residual,
+                         int64_t ld_res, double p, uint64_t seed, uint64_t offset, void* out, int64_t ld_out, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a projection that they share.   (Section 3.3 "Parameter Efficient Fine Tuning": the
+ * low-rank branch of the LoRA-style module, for a batch whose tokens have different adapters.)  halo_peft_* has one adapter for all
+ * tokens; here token t has adapter a = adapter_of[t], and the shared projection's own output comes as `base`:
+ *
+ *   forward    T   = drop(X) U_a^T                     Y   = base + scale_a * T V_a^T
+ *   backward   S   = scale_a * E V_a                   E_X = base + drop'(S U_a)
+ *              G_U[a] = sum S_t^T drop(X)_t            G_V[a] = scale_a * sum E_t^T T_t         over the tokens t of adapter a
+ *
+ * drop() is halo_dropout's, with the token as the row; drop' applies the same mask to the product S U_a.  dropout_p = 0: none.
+ *
+ *   b, m, n        tokens, in-features, out-features; m and n multiples of 8.
+ *   slots          adapters in the pool, 1 .. 65535.
+ *   max_rank       what the pool allots to an adapter: a multiple of 8, at most 128.
+ *   U, V           bf16, dense: U [slots x max_rank x m], V [slots x n x max_rank].
+ *   ranks          int32 [slots] or NULL (all max_rank).  Of adapter a the first ranks[a] rows of U and columns of V are used (any number,
+ *                  taken as 0 or max_rank if it lies outside); what lies beyond is not used and may hold anything.
+ *   scale          fp32 [slots] or NULL (all 1).
+ *   adapter_of     int32 [b]; a value outside [0, slots) stands for no adapter: that token's Y (E_X) is base, its T is 0, and
+ *                  no gradient has it.  Tokens may come in any order; fastest is one in which neighbours have the same adapter.
+ *   X, E           bf16 [b x m] and [b x n], leading dimensions ld_x, ld_e.
+ *   base           [b x n] (forward) or [b x m] (backward), of type out_dt, leading dimension ld_base; NULL = 0.  May be Y (E_X) itself,
+ *                  with the same leading dimension.
+ *   Y, EX          of type out_dt.  The sum is formed in fp32 and rounded once.
+ *   T              fp32 [b x max_rank], dense: written by the forward pass, read by the backward pass (for G_V).  Columns beyond the
+ *                  adapter's rank are 0.
+ *   GU, GV         fp32, dense, laid out like U and V; 0 beyond an adapter's rank and for adapters without tokens (b == 0 included).
+ *   EX, GU, GV     any may be NULL to skip it (not all three).  X is read for G_U only, T for G_V only, U for E_X, V for E_X and G_U.
+ *   workspace      halo_adapters_fwd_workspace_bytes(desc) resp. halo_adapters_bwd_workspace_bytes(desc) bytes, 16-byte aligned
+ *                  (may be NULL where that is 0); nothing in it is carried from call to call.
+ * ranks, scale and adapter_of need 4-byte alignment only.  Products of bf16 values accumulate in fp32, T and S are not rounded to
+ * fewer bits.  m == 0, n == 0 or (forward) b == 0 is a no-op.  Errors as elsewhere; HALO_EUNSUPPORTED: max_rank > 128, slots > 65535,
+ * b, m or n > 2^22.
+ */
+typedef struct halo_adapters_desc {
+    int64_t b, m, n;
+    int32_t slots, max_rank;
+    int32_t out_dt;         /* halo_dtype of base, Y and EX */
+    int32_t reserved;       /* 0 */
+    double dropout_p;
+    uint64_t seed, offset;
+} halo_adapters_desc;
+
+size_t halo_adapters_fwd_workspace_bytes(const halo_adapters_desc* desc);
+size_t halo_adapters_bwd_workspace_bytes(const halo_adapters_desc* desc);
+
+halo_status halo_adapters_fwd(const halo_adapters_desc* desc, const void* X, int64_t ld_x, const void* U, const void* V,
+                              const int32_t* ranks, const float* scale, const int32_t* adapter_of, const void* base, int64_t ld_base,
+                              void* Y, int64_t ld_y, float* T, void* workspace, size_t workspace_bytes, void* stream);
+
+halo_status halo_adapters_bwd(const halo_adapters_desc* desc, const void* E, int64_t ld_e, const void* X, int64_t ld_x, const float* T,
+                              const void* U, const void* V, const int32_t* ranks, const float* scale, const int32_t* adapter_of,
+                              const void* base, int64_t ld_base, void* EX, int64_t ld_ex, float* GU, float* GV, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,6 +36,8 @@ EXPORTED_SYMBOLS = (
     "halo_dequant_unrotate_workspace_bytes", "halo_dequant_unrotate",
     "halo_linear_workspace_bytes", "halo_linear_fwd", "halo_linear_bwd",
     "halo_peft_workspace_bytes", "halo_peft_fwd", "halo_peft_bwd",
+    "halo_dropout",
+    "halo_adapters_fwd_workspace_bytes", "halo_adapters_bwd_workspace_bytes", "halo_adapters_fwd", "halo_adapters_bwd",
 )
 
 
@@ -57,6 +59,12 @@ class LinearDesc(ctypes.Structure):
     _fields_ = [("b", ctypes.c_int64), ("m", ctypes.c_int64), ("n", ctypes.c_int64),
                 ("level", ctypes.c_int32), ("had_block_m", ctypes.c_int32),
                 ("had_block_b", ctypes.c_int32), ("out_dt", ctypes.c_int32), ("scale_mode", ctypes.c_int32)]
+
+
+class AdaptersDesc(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int64), ("m", ctypes.c_int64), ("n", ctypes.c_int64), ("slots", ctypes.c_int32),
+                ("max_rank", ctypes.c_int32), ("out_dt", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("dropout_p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -123,6 +131,16 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.halo_peft_fwd.argtypes = [c.POINTER(LinearDesc), i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.halo_peft_bwd.restype = c.c_int
     lib.halo_peft_bwd.argtypes = [c.POINTER(LinearDesc), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.halo_dropout.restype = c.c_int
+    lib.halo_dropout.argtypes = [vp, c.c_int, i64, i64, i64, vp, i64, c.c_double, c.c_uint64, c.c_uint64, vp, i64, vp]
+    for f in (lib.halo_adapters_fwd_workspace_bytes, lib.halo_adapters_bwd_workspace_bytes):
+        f.restype = sz
+        f.argtypes = [c.POINTER(AdaptersDesc)]
+    lib.halo_adapters_fwd.restype = c.c_int
+    lib.halo_adapters_fwd.argtypes = [c.POINTER(AdaptersDesc), vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+    lib.halo_adapters_bwd.restype = c.c_int
+    lib.halo_adapters_bwd.argtypes = [c.POINTER(AdaptersDesc), vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
+                                      sz, vp]
     if path == _build.LIB_PATH:
         _lib = lib
     return lib
@@ -404,3 +422,49 @@ def halo_peft_bwd(desc: LinearDesc, E: torch.Tensor, X: torch.Tensor, T: torch.T
     """Backward pass of the module; returns (E_X, G_U [rank x m] fp32, G_V [n x rank] fp32), None where not wanted."""
     r = _native().peft_bwd(desc, E, X, T, Wq, s_w, U, V, bool(want_ex), bool(want_gu), bool(want_gv), workspace, EX, GU, GV)
     return r if type(r) is tuple else _failed(r, "halo_peft_bwd")
+
+
+def halo_dropout(x: torch.Tensor, p: float, seed: int, offset: int, *, residual: Optional[torch.Tensor] = None,
+                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """residual + drop(x), x a bf16 or fp32 matrix.  The mask is a function of (seed, offset, row, column), both 64-bit integers: the
+    same call on the gradient, without the residual, is the backward pass."""
+    r = _native().dropout(x, p, seed, offset, residual, out)
+    return r if type(r) is not int else _failed(r, "halo_dropout")
+
+
+def adapters_desc(b: int, m: int, n: int, slots: int, max_rank: int, out_dtype: torch.dtype = torch.bfloat16,
+                  dropout_p: float = 0.0, seed: int = 0, offset: int = 0) -> AdaptersDesc:
+    return AdaptersDesc(b, m, n, slots, max_rank, _dt(out_dtype), 0, dropout_p, seed, offset)
+
+
+def halo_adapters_fwd_workspace_bytes(desc: AdaptersDesc) -> int:
+    return int(load_library().halo_adapters_fwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def halo_adapters_bwd_workspace_bytes(desc: AdaptersDesc) -> int:
+    return int(load_library().halo_adapters_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def halo_adapters_fwd(X: torch.Tensor, U: torch.Tensor, V: torch.Tensor, adapter_of: torch.Tensor, *,
+                      ranks: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                      base: Optional[torch.Tensor] = None, dropout_p: float = 0.0, seed: int = 0, offset: int = 0,
+                      out_dtype: torch.dtype = torch.bfloat16, Y: Optional[torch.Tensor] = None,
+                      T: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Low-rank adapters of many requests beside a shared projection: Y = base + scale_a (drop(X) U_a^T) V_a^T with the adapter
+    a = adapter_of[t] of each token t (none outside [0, slots)).  U [slots, max_rank, m], V [slots, n, max_rank]; returns (Y, T =
+    drop(X) U_a^T in fp32, which the backward pass takes).  base and Y have out_dtype and may be one tensor."""
+    r = _native().adapters_fwd(X, U, V, adapter_of, ranks, scale, base, _dt(out_dtype), dropout_p, seed, offset, Y, T, workspace)
+    return r if type(r) is tuple else _failed(r, "halo_adapters_fwd")
+
+
+def halo_adapters_bwd(E: torch.Tensor, X: Optional[torch.Tensor], T: Optional[torch.Tensor], U: torch.Tensor, V: torch.Tensor,
+                      adapter_of: torch.Tensor, *, ranks: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                      base: Optional[torch.Tensor] = None, dropout_p: float = 0.0, seed: int = 0, offset: int = 0,
+                      out_dtype: torch.dtype = torch.bfloat16, want_ex: bool = True, want_gu: bool = True, want_gv: bool = True,
+                      EX: Optional[torch.Tensor] = None, GU: Optional[torch.Tensor] = None, GV: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None):
+    """Gradients of halo_adapters_fwd, with its dropout arguments; returns (E_X = base + the adapters' part, G_U fp32 shaped like U,
+    G_V fp32 shaped like V), None where not wanted.  X is needed for G_U, T for G_V."""
+    r = _native().adapters_bwd(E, X, T, U, V, adapter_of, ranks, scale, base, _dt(out_dtype), dropout_p, seed, offset, bool(want_ex),
+                               bool(want_gu), bool(want_gv), EX, GU, GV, workspace)
+    return r if type(r) is tuple else _failed(r, "halo_adapters_bwd")

@@ -2,6 +2,7 @@
 #include <cmath>
 #include <cstdint>
 
+#include "adapters.h"
 #include "halo_internal.h"
 
 using namespace halo;
@@ -9,6 +10,7 @@ using namespace halo;
 namespace {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline size_t round256(size_t v) { return (v + 255) & ~size_t(255); }
 inline halo_status from_hip(hipError_t e) { return e == hipSuccess ? HALO_OK : HALO_EHIP; }
 
@@ -241,6 +243,22 @@ halo_status resolve_peft(const halo_linear_desc* d, int32_t rank, int32_t* hm, i
     if (d->m % 64 || d->n % 64) return HALO_ESHAPE;       // both are reduction lengths of a K-step GEMM
     if (!lr_row_fwht_shape_ok(d->m, *hm)) return HALO_EUNSUPPORTED;
     return HALO_OK;
+}
+
+halo_status check_adapters(const halo_adapters_desc* d) {
+    if (!d || d->b < 0 || d->m < 0 || d->n < 0 || d->reserved != 0) return HALO_EINVAL;
+    if (d->out_dt != HALO_BF16 && d->out_dt != HALO_F32) return HALO_EINVAL;
+    if (!(d->dropout_p >= 0.0 && d->dropout_p <= 1.0)) return HALO_EINVAL;
+    if (d->slots < 1 || d->max_rank < 8 || d->max_rank % 8 || d->m % 8 || d->n % 8) return HALO_ESHAPE;
+    if (d->max_rank > kMaxAdapterRank || d->slots > 65535) return HALO_EUNSUPPORTED;
+    if (d->b > kMaxDim || d->m > kMaxDim || d->n > kMaxDim) return HALO_EUNSUPPORTED;
+    return HALO_OK;
+}
+
+AdapterPool adapter_pool(const halo_adapters_desc* d, const void* U, const void* V, const int32_t* ranks, const float* scale,
+                         const int32_t* adapter_of) {
+    return AdapterPool{reinterpret_cast<const uint16_t*>(U), reinterpret_cast<const uint16_t*>(V), ranks, scale, adapter_of, d->b, d->m,
+                       d->n, d->slots, d->max_rank};
 }
 
 }  // namespace
@@ -946,6 +964,93 @@ halo_status halo_peft_bwd(const halo_linear_desc* desc, int32_t rank, const void
     r.in = c32; r.ld_in = m; r.rows = b; r.cols = m; r.out = EX; r.ld_out = m;
     set_right_block(r, hm);
     return from_hip(launch_row_transform(r, IN_F32, odt == HALO_BF16 ? OUT_BF16 : OUT_F32, hs));
+}
+
+// ------------------------------------------------------------------------------------------------
+halo_status halo_dropout(const void* in, halo_dtype dt, int64_t rows, int64_t cols, int64_t ld_in, const void* residual,
+                         int64_t ld_res, double p, uint64_t seed, uint64_t offset, void* out, int64_t ld_out, void* stream) {
+    if (rows < 0 || cols < 0 || (dt != HALO_BF16 && dt != HALO_F32)) return HALO_EINVAL;
+    if (!(p >= 0.0 && p <= 1.0)) return HALO_EINVAL;
+    if (rows == 0 || cols == 0) return HALO_OK;
+    if (!in || !out) return HALO_EINVAL;
+    if (rows > kMaxDim || cols > kMaxDim) return HALO_EUNSUPPORTED;
+    if (ld_in < cols || ld_out < cols || (residual && ld_res < cols)) return HALO_ESHAPE;
+    if ((out == in && ld_out != ld_in) || (residual && out == residual && ld_out != ld_res)) return HALO_ESHAPE;
+    const int64_t per16 = dt == HALO_BF16 ? 8 : 4;
+    if (!aligned16(in) || !aligned16(out) || (residual && !aligned16(residual)) || ld_in % per16 || ld_out % per16 ||
+        (residual && ld_res % per16))
+        return HALO_EALIGN;
+    DropoutArgs a{in, ld_in, residual, ld_res, out, ld_out, rows, cols, dt == HALO_F32 ? 1 : 0, make_dropout_mask(p, seed, offset)};
+    return from_hip(launch_dropout(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+size_t halo_adapters_fwd_workspace_bytes(const halo_adapters_desc* desc) {
+    return check_adapters(desc) == HALO_OK ? adapters_fwd_workspace(desc->b, desc->m, desc->n, desc->slots, desc->max_rank) : 0;
+}
+
+size_t halo_adapters_bwd_workspace_bytes(const halo_adapters_desc* desc) {
+    return check_adapters(desc) == HALO_OK ? adapters_bwd_workspace(desc->b, desc->m, desc->n, desc->slots, desc->max_rank) : 0;
+}
+
+halo_status halo_adapters_fwd(const halo_adapters_desc* desc, const void* X, int64_t ld_x, const void* U, const void* V,
+                              const int32_t* ranks, const float* scale, const int32_t* adapter_of, const void* base, int64_t ld_base,
+                              void* Y, int64_t ld_y, float* T, void* workspace, size_t workspace_bytes, void* stream) {
+    const halo_status st = check_adapters(desc);
+    if (st != HALO_OK) return st;
+    const int64_t b = desc->b, m = desc->m, n = desc->n;
+    if (b == 0 || m == 0 || n == 0) return HALO_OK;
+    if (!X || !U || !V || !adapter_of || !Y || !T) return HALO_EINVAL;
+    const int f32 = desc->out_dt == HALO_F32 ? 1 : 0;
+    if (ld_x < m || ld_y < n || (base && ld_base < n) || (base == Y && ld_base != ld_y)) return HALO_ESHAPE;
+    const int64_t per16 = f32 ? 4 : 8;
+    if (ld_x % 8 || ld_y % per16 || (base && ld_base % per16)) return HALO_EALIGN;
+    if (!aligned16(X) || !aligned16(U) || !aligned16(V) || !aligned16(Y) || !aligned16(T) || (base && !aligned16(base)) ||
+        !aligned4(ranks) || !aligned4(scale) || !aligned4(adapter_of))
+        return HALO_EALIGN;
+    const size_t need = adapters_fwd_workspace(b, m, n, desc->slots, desc->max_rank);
+    if (need && (!workspace || workspace_bytes < need)) return HALO_EWORKSPACE;
+    if (need && !aligned16(workspace)) return HALO_EALIGN;
+    AdaptersFwd a{};
+    a.pool = adapter_pool(desc, U, V, ranks, scale, adapter_of);
+    a.X = reinterpret_cast<const uint16_t*>(X); a.ld_x = ld_x;
+    a.base = base; a.ld_base = ld_base; a.Y = Y; a.ld_y = ld_y; a.out_f32 = f32; a.T = T;
+    a.drop = make_dropout_mask(desc->dropout_p, desc->seed, desc->offset);
+    a.workspace = workspace;
+    return from_hip(launch_adapters_fwd(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+halo_status halo_adapters_bwd(const halo_adapters_desc* desc, const void* E, int64_t ld_e, const void* X, int64_t ld_x, const float* T,
+                              const void* U, const void* V, const int32_t* ranks, const float* scale, const int32_t* adapter_of,
+                              const void* base, int64_t ld_base, void* EX, int64_t ld_ex, float* GU, float* GV, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+    const halo_status st = check_adapters(desc);
+    if (st != HALO_OK) return st;
+    if (!EX && !GU && !GV) return HALO_EINVAL;
+    const int64_t b = desc->b, m = desc->m, n = desc->n;
+    if (m == 0 || n == 0) return HALO_OK;
+    const int f32 = desc->out_dt == HALO_F32 ? 1 : 0;
+    if (b > 0) {
+        if (!E || !adapter_of) return HALO_EINVAL;
+        if ((EX && !U) || ((EX || GU) && !V) || (GU && !X) || (GV && !T)) return HALO_EINVAL;
+        if (ld_e < n || (GU && ld_x < m) || (EX && ld_ex < m) || (EX && base && ld_base < m) || (EX && base == EX && ld_base != ld_ex))
+            return HALO_ESHAPE;
+        const int64_t per16 = f32 ? 4 : 8;
+        if (ld_e % 8 || (GU && ld_x % 8) || (EX && ld_ex % per16) || (EX && base && ld_base % per16)) return HALO_EALIGN;
+    }
+    if (!aligned16(E) || !aligned16(X) || !aligned16(T) || !aligned16(U) || !aligned16(V) || !aligned16(base) || !aligned16(EX) ||
+        !aligned16(GU) || !aligned16(GV) || !aligned4(ranks) || !aligned4(scale) || !aligned4(adapter_of))
+        return HALO_EALIGN;
+    const size_t need = adapters_bwd_workspace(b, m, n, desc->slots, desc->max_rank);
+    if (need && (!workspace || workspace_bytes < need)) return HALO_EWORKSPACE;
+    if (need && !aligned16(workspace)) return HALO_EALIGN;
+    AdaptersBwd a{};
+    a.pool = adapter_pool(desc, U, V, ranks, scale, adapter_of);
+    a.E = reinterpret_cast<const uint16_t*>(E); a.ld_e = ld_e;
+    a.X = reinterpret_cast<const uint16_t*>(X); a.ld_x = ld_x;
+    a.T = T; a.base = base; a.ld_base = ld_base; a.EX = EX; a.ld_ex = ld_ex; a.out_f32 = f32; a.GU = GU; a.GV = GV;
+    a.drop = make_dropout_mask(desc->dropout_p, desc->seed, desc->offset);
+    a.workspace = workspace;
+    return from_hip(launch_adapters_bwd(a, reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

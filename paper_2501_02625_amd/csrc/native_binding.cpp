@@ -54,6 +54,19 @@ long integer(PyObject* o) {
     return v;
 }
 
+double real(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Failed();
+    return v;
+}
+
+// A Python integer from 0 to 2^64 - 1.
+uint64_t word64(PyObject* o) {
+    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    if (v == (unsigned long long)-1 && PyErr_Occurred()) throw Failed();
+    return v;
+}
+
 void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
 size_t bytes(const at::Tensor* t) { return t ? (size_t)t->numel() : 0; }      // workspaces are uint8
 
@@ -121,6 +134,14 @@ PyObject* wrap_or_none(bool want, const at::Tensor& t) {
     if (want) return THPVariable_Wrap(t);
     Py_RETURN_NONE;
 }
+
+// None, or [rows, cols] of the type with contiguous rows.
+bool matrix(const at::Tensor* t, int64_t rows, int64_t cols, at::ScalarType dtype) {
+    return !t || (t->dim() == 2 && t->size(0) == rows && t->size(1) == cols && t->scalar_type() == dtype &&
+                  (rows == 0 || cols <= 1 || t->stride(1) == 1));
+}
+// Elements from row to row; that of a matrix of one row does not matter.
+int64_t pitch(const at::Tensor* t) { return !t ? 0 : t->size(0) > 1 ? t->stride(0) : (t->size(1) + 7) / 8 * 8; }
 
 // The given output, or a new one.
 at::Tensor output(const at::Tensor* given, bool want, at::IntArrayRef size, at::ScalarType dtype, const at::Tensor& like,
@@ -337,6 +358,96 @@ PyObject* gemm_i8(PyObject* const* a) {
     return Py_BuildValue("(NN)", wrap_or_none(C.defined(), C), wrap_or_none(S.defined(), S));
 }
 
+// x, p, seed, offset, residual, out
+PyObject* dropout(PyObject* const* a) {
+    const at::Tensor *x = tensor(a[0]), *res = tensor(a[4]), *out = tensor(a[5]);
+    require(x && x->dim() == 2 && matrix(x, x->size(0), x->size(1), x->scalar_type()), "x is a matrix with contiguous rows");
+    const int64_t rows = x->size(0), cols = x->size(1);
+    require(matrix(res, rows, cols, x->scalar_type()) && matrix(out, rows, cols, x->scalar_type()),
+            "residual and out are matrices like x, with contiguous rows");
+    const double p = real(a[1]);
+    const uint64_t seed = word64(a[2]), offset = word64(a[3]);
+    const halo_dtype dt = dtype_code(*x);
+    const Context c;
+    const at::Tensor y = out ? *out : new_padded(rows, cols, x->scalar_type(), *x, c.device);
+    const halo_status st = without_gil(halo_dropout, data(x), dt, rows, cols, pitch(x), data(res), pitch(res), p, seed, offset, data(y),
+                                       pitch(&y), c.stream);
+    if (st != HALO_OK) return PyLong_FromLong(st);
+    return wrap(y);
+}
+
+// What both passes of the adapters take.
+struct Adapters {
+    const at::Tensor *U, *V, *of, *ranks, *scale;
+    halo_adapters_desc d{};
+    Adapters(PyObject* u, PyObject* v, PyObject* adapter_of, PyObject* rank, PyObject* s, const at::Tensor* rows, long out_code,
+             PyObject* p, PyObject* seed, PyObject* offset)
+        : U(tensor(u)), V(tensor(v)), of(tensor(adapter_of)), ranks(tensor(rank)), scale(tensor(s)) {
+        require(U && V && of && rows, "U, V, adapter_of and the tokens are needed");
+        require(bf16(U) && bf16(V) && U->is_contiguous() && V->is_contiguous() && U->dim() == 3 && V->dim() == 3 &&
+                    U->size(0) == V->size(0) && U->size(1) == V->size(2),
+                "U [slots, max_rank, m] and V [slots, n, max_rank] are contiguous bf16");
+        d.b = rows->size(0); d.m = U->size(2); d.n = V->size(1);
+        require(U->size(0) <= INT32_MAX && U->size(1) <= INT32_MAX, "the pool is too large");
+        d.slots = (int32_t)U->size(0); d.max_rank = (int32_t)U->size(1);
+        require(of->scalar_type() == at::kInt && of->is_contiguous() && of->dim() == 1 && of->size(0) == d.b, "adapter_of is int32 [b]");
+        require(!ranks || (ranks->scalar_type() == at::kInt && ranks->is_contiguous() && ranks->numel() == d.slots), "ranks is int32 [slots]");
+        require(!scale || (scale->scalar_type() == at::kFloat && scale->is_contiguous() && scale->numel() == d.slots), "scale is fp32 [slots]");
+        d.out_dt = (int32_t)out_code;
+        d.dropout_p = real(p); d.seed = word64(seed); d.offset = word64(offset);
+    }
+    at::ScalarType out_type() const { return out_dtype(d.out_dt); }
+    at::Tensor workspace(const at::Tensor* given, size_t need, const Context& c) const {
+        if (given) return *given;
+        return new_tensor({(int64_t)(need > 16 ? need : 16)}, at::kByte, *U, c.device);
+    }
+};
+
+// X, U, V, adapter_of, ranks, scale, base, dtype of Y, p, seed, offset, Y, T, workspace
+PyObject* adapters_fwd(PyObject* const* a) {
+    const at::Tensor *X = tensor(a[0]), *base = tensor(a[6]), *y = tensor(a[11]), *t = tensor(a[12]), *ws = tensor(a[13]);
+    require(X && X->dim() == 2, "X is a bf16 matrix with contiguous rows");
+    const Adapters f(a[1], a[2], a[3], a[4], a[5], X, integer(a[7]), a[8], a[9], a[10]);
+    const halo_adapters_desc& d = f.d;
+    require(matrix(X, d.b, d.m, at::kBFloat16), "X is a bf16 matrix with contiguous rows");
+    require(matrix(base, d.b, d.n, f.out_type()) && matrix(y, d.b, d.n, f.out_type()), "base and Y are [b, n] of the output's type");
+    require(!t || (matrix(t, d.b, d.max_rank, at::kFloat) && t->is_contiguous()), "T is fp32 [b, max_rank]");
+    const Context c;
+    const at::Tensor Y = output(y, true, {d.b, d.n}, f.out_type(), *X, c), T = output(t, true, {d.b, d.max_rank}, at::kFloat, *X, c),
+                     W = f.workspace(ws, halo_adapters_fwd_workspace_bytes(&d), c);
+    const halo_status st = without_gil(
+        halo_adapters_fwd, &d, data(X), pitch(X), data(f.U), data(f.V), (int32_t*)data(f.ranks), (float*)data(f.scale),
+        (int32_t*)data(f.of), data(base), pitch(base), data(Y), pitch(&Y), (float*)data(T), data(W), bytes(&W), c.stream);
+    if (st != HALO_OK) return PyLong_FromLong(st);
+    return Py_BuildValue("(NN)", wrap(Y), wrap(T));
+}
+
+// E, X, T, U, V, adapter_of, ranks, scale, base, dtype of EX, p, seed, offset, want_ex, want_gu, want_gv, EX, GU, GV, workspace
+PyObject* adapters_bwd(PyObject* const* a) {
+    const at::Tensor *E = tensor(a[0]), *X = tensor(a[1]), *T = tensor(a[2]), *base = tensor(a[8]), *ex = tensor(a[16]),
+                     *gu = tensor(a[17]), *gv = tensor(a[18]), *ws = tensor(a[19]);
+    const bool want_ex = a[13] == Py_True, want_gu = a[14] == Py_True, want_gv = a[15] == Py_True;
+    require(E && E->dim() == 2, "E is a bf16 matrix with contiguous rows");
+    const Adapters f(a[3], a[4], a[5], a[6], a[7], E, integer(a[9]), a[10], a[11], a[12]);
+    const halo_adapters_desc& d = f.d;
+    require(matrix(E, d.b, d.n, at::kBFloat16) && matrix(X, d.b, d.m, at::kBFloat16), "E and X are bf16 matrices with contiguous rows");
+    require(!T || (matrix(T, d.b, d.max_rank, at::kFloat) && T->is_contiguous()), "T is fp32 [b, max_rank]");
+    require(matrix(base, d.b, d.m, f.out_type()) && matrix(ex, d.b, d.m, f.out_type()), "base and EX are [b, m] of the output's type");
+    require(!gu || (gu->scalar_type() == at::kFloat && gu->is_contiguous() && gu->sizes() == f.U->sizes()), "GU is fp32, shaped like U");
+    require(!gv || (gv->scalar_type() == at::kFloat && gv->is_contiguous() && gv->sizes() == f.V->sizes()), "GV is fp32, shaped like V");
+    const Context c;
+    const at::Tensor EX = output(want_ex ? ex : nullptr, want_ex, {d.b, d.m}, f.out_type(), *E, c),
+                     GU = output(want_gu ? gu : nullptr, want_gu, f.U->sizes(), at::kFloat, *E, c),
+                     GV = output(want_gv ? gv : nullptr, want_gv, f.V->sizes(), at::kFloat, *E, c),
+                     W = f.workspace(ws, halo_adapters_bwd_workspace_bytes(&d), c);
+    const halo_status st = without_gil(
+        halo_adapters_bwd, &d, data(E), pitch(E), data(X), pitch(X), (float*)data(T), data(f.U), data(f.V), (int32_t*)data(f.ranks),
+        (float*)data(f.scale), (int32_t*)data(f.of), data(base), pitch(base), data(EX), want_ex ? pitch(&EX) : 0, (float*)data(GU),
+        (float*)data(GV), data(W), bytes(&W), c.stream);
+    if (st != HALO_OK) return PyLong_FromLong(st);
+    return Py_BuildValue("(NNN)", wrap_or_none(want_ex, EX), wrap_or_none(want_gu, GU), wrap_or_none(want_gv, GV));
+}
+
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t count) {
     if (count != N) {
@@ -359,7 +470,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t count) {
 #define HALO_ENTRY(F, N) {#F, (PyCFunction)(void (*)(void))entry<F, N>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HALO_ENTRY(linear_fwd, 10), HALO_ENTRY(linear_bwd, 11), HALO_ENTRY(peft_fwd, 9), HALO_ENTRY(peft_bwd, 15),
                          HALO_ENTRY(mx6_quant, 4),  HALO_ENTRY(gemm_mx6, 6),    HALO_ENTRY(hadamard_quant, 8),
-                         HALO_ENTRY(gemm_i8, 9),    {nullptr, nullptr, 0, nullptr}};
+                         HALO_ENTRY(gemm_i8, 9),    HALO_ENTRY(dropout, 6),     HALO_ENTRY(adapters_fwd, 14),
+                         HALO_ENTRY(adapters_bwd, 20), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_halo_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
