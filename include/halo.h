@@ -371,7 +371,7 @@ halo_status halo_dropout(const void* in, halo_dtype dt, int64_t rows, int64_t co
  * drop() is halo_dropout's, with the token as the row; drop' applies the same mask to the product S U_a.  dropout_p = 0: none.
  *
  *   b, m, n        tokens, in-features, out-features; m and n multiples of 8.
- *   slots          adapters in the pool, 1 .. 65535.
+ *   slots          adapters in the pool, 1 .. 32768.
  *   max_rank       what the pool allots to an adapter: a multiple of 8, at most 128.
  *   U, V           bf16, dense: U [slots x max_rank x m], V [slots x n x max_rank].
  *   ranks          int32 [slots] or NULL (all max_rank).  Of adapter a the first ranks[a] rows of U and columns of V are used (any number,
@@ -390,7 +390,7 @@ halo_status halo_dropout(const void* in, halo_dtype dt, int64_t rows, int64_t co
  *   workspace      halo_adapters_fwd_workspace_bytes(desc) resp. halo_adapters_bwd_workspace_bytes(desc) bytes, 16-byte aligned
  *                  (may be NULL where that is 0); nothing in it is carried from call to call.
  * ranks, scale and adapter_of need 4-byte alignment only.  Products of bf16 values accumulate in fp32, T and S are not rounded to
- * fewer bits.  m == 0, n == 0 or (forward) b == 0 is a no-op.  Errors as elsewhere; HALO_EUNSUPPORTED: max_rank > 128, slots > 65535,
+ * fewer bits.  m == 0, n == 0 or (forward) b == 0 is a no-op.  Errors as elsewhere; HALO_EUNSUPPORTED: max_rank > 128, slots > 32768,
  * b, m or n > 2^22.
  */
 typedef struct halo_adapters_desc {

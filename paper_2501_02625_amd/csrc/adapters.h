@@ -10,6 +10,7 @@
 namespace halo {
 
 constexpr int kMaxAdapterRank = 128;
+constexpr int kMaxAdapterSlots = 32768;       // with the most cuts of 2^22 tokens still a grid dimension (65535)
 
 // The pool: U bf16 [slots x max_rank x m], V bf16 [slots x n x max_rank], of which adapter a's first ranks[a] rows of U and columns of
 // V are used (ranks null: max_rank); scale fp32 [slots] or null (1).  adapter_of [b]: the adapter of each token, none where it is not

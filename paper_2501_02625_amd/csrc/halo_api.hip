@@ -250,7 +250,7 @@ halo_status check_adapters(const halo_adapters_desc* d) {
     if (d->out_dt != HALO_BF16 && d->out_dt != HALO_F32) return HALO_EINVAL;
     if (!(d->dropout_p >= 0.0 && d->dropout_p <= 1.0)) return HALO_EINVAL;
     if (d->slots < 1 || d->max_rank < 8 || d->max_rank % 8 || d->m % 8 || d->n % 8) return HALO_ESHAPE;
-    if (d->max_rank > kMaxAdapterRank || d->slots > 65535) return HALO_EUNSUPPORTED;
+    if (d->max_rank > kMaxAdapterRank || d->slots > kMaxAdapterSlots) return HALO_EUNSUPPORTED;
     if (d->b > kMaxDim || d->m > kMaxDim || d->n > kMaxDim) return HALO_EUNSUPPORTED;
     return HALO_OK;
 }
