@@ -11,6 +11,8 @@
 // that group_kernel writes down.  No two adapters meet in one accumulator: what one holds (infinities, NaN) reaches its own tokens only.
 #pragma clang fp contract(off)
 
+#include <type_traits>
+
 #include "adapters.h"
 
 namespace halo {
@@ -36,6 +38,25 @@ __device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uin
     const float h = __uint_as_float(hi), r = h == x ? 0.0f : x - h;
     mid = __float_as_uint(r) & 0xFFFF0000u;
     lo = __float_as_uint(r - __uint_as_float(mid));
+}
+
+// Loads at a 32-bit byte offset from an address that is the same for the wavefront: one register of address.
+template <typename V>
+__device__ __forceinline__ V load_at(const void* base, uint32_t offset) {
+    return *reinterpret_cast<const V*>(reinterpret_cast<const char*>(base) + offset);
+}
+
+// Eight rows of eight bf16 values become eight columns: x[v] is the v-th of each row, in row order.
+__device__ __forceinline__ void transpose8(v4u (&x)[8]) {
+    v4u y[8];
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+        const int d = v >> 1;
+        y[v] = (v & 1) ? v4u{pack_hi(x[0][d], x[1][d]), pack_hi(x[2][d], x[3][d]), pack_hi(x[4][d], x[5][d]), pack_hi(x[6][d], x[7][d])}
+                       : v4u{pack_lo(x[0][d], x[1][d]), pack_lo(x[2][d], x[3][d]), pack_lo(x[4][d], x[5][d]), pack_lo(x[6][d], x[7][d])};
+    }
+#pragma unroll
+    for (int v = 0; v < 8; ++v) x[v] = y[v];
 }
 
 __device__ __forceinline__ bool is_adapter(const AdapterPool& p, int a) { return (unsigned)a < (unsigned)p.slots; }
@@ -77,13 +98,94 @@ struct TileAdapters {
     }
 };
 
+// ------------------------------------------------------------------------------------------------ tokens by their adapters
+// The gradients take the tokens adapter by adapter.  order: places for tokens, b + 32 (slots + 1) of them; adapter a's tokens, by index, have the
+// places from range[a].x on, a multiple of 32, to range[a].y; a place without a token holds -1.  With `before` tokens of lower adapters the
+// range begins at before, rounded up to 32, plus 32 a: so each finds its own alone, and none overlap.
+// A cut is a multiple of `chunk` (of 32) of places; a segment is what one adapter has between cuts, so adapter a has 1 + (cuts strictly inside
+// its range) of them, at least one even without tokens.  Segment i of adapter a has the index a + range[a].x / chunk + i: at most slots + cuts
+// of them, in order, none shared; indices that no adapter takes hold no adapter.
+struct Segment {
+    int adapter;             // -1: none
+    int begin, end;          // places
+    int part;                // where its sum goes: -1: it is the adapter's only segment, straight to the result
+};
+
+struct GroupArgs {
+    int chunk, cuts;         // cuts: ceil(places / chunk)
+    int* order;
+    int2* range;             // [slots]
+    Segment* segments;       // [slots + cuts]
+};
+
+// One adapter's, by a workgroup.  A segment that is not alone begins or ends at a cut k: its sum goes to part k (it begins there) or cuts + k
+// (it is the first one, and ends there).
+template <int THREADS>
+__device__ __forceinline__ void group_tokens(const AdapterPool& p, const GroupArgs& g, int a) {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ int s_less[WAVES], s_same[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int b = (int)p.b, chunk = g.chunk;
+    int less = 0, same = 0;
+    for (int t = tid; t < b; t += THREADS) {
+        const int id = p.adapter_of[t];
+        less += id >= 0 && id < a;
+        same += id == a;
+    }
+    for (int h = 32; h > 0; h >>= 1) { less += __shfl_xor(less, h); same += __shfl_xor(same, h); }
+    if (lane == 0) { s_less[wave] = less; s_same[wave] = same; }
+    __syncthreads();
+    less = same = 0;
+    for (int w = 0; w < WAVES; ++w) { less += s_less[w]; same += s_same[w]; }
+    const int begin = (less + 31) / 32 * 32 + 32 * a, end = begin + same;
+    if (tid == 0) g.range[a] = make_int2(begin, end);
+    const int after = (less + same + 31) / 32 * 32 + 32 * (a + 1);     // where the next adapter begins
+    const int count = same ? (end + chunk - 1) / chunk - begin / chunk : 1;
+    const int index = a + begin / chunk, next = a == p.slots - 1 ? p.slots + g.cuts : a + 1 + after / chunk;
+    for (int i = tid; index + i < next; i += THREADS) {
+        Segment q{-1, 0, 0, -1};
+        if (i < count) {
+            const int cut = begin / chunk + i;           // the segment lies between this cut and the next
+            q.adapter = a;
+            q.begin = i == 0 ? begin : cut * chunk;
+            q.end = i == count - 1 ? end : (cut + 1) * chunk;
+            q.part = count == 1 ? -1 : i == 0 ? g.cuts + cut + 1 : cut;
+        }
+        g.segments[index + i] = q;
+    }
+    if (tid < after - end) g.order[end + tid] = -1;      // fewer than 64 places
+    if (a == 0 && tid < begin) g.order[tid] = -1;
+    int at = begin;
+    for (int t0 = 0; t0 < b && same > 0; t0 += THREADS) {
+        const int t = t0 + tid;
+        const bool hit = t < b && p.adapter_of[t] == a;
+        const uint64_t hits = __ballot(hit);
+        __syncthreads();
+        if (lane == 0) s_same[wave] = __builtin_popcountll(hits);
+        __syncthreads();
+        int before = 0, all = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            before += w < wave ? s_same[w] : 0;
+            all += s_same[w];
+        }
+        const int to = at + before + __builtin_popcountll(hits & ((1ull << lane) - 1));
+        if (hit && to < end) g.order[to] = t;
+        at += all;
+    }
+}
+
+__global__ void __launch_bounds__(512)
+group_kernel(AdapterPool p, GroupArgs g) { group_tokens<512>(p, g, blockIdx.x); }
+
 // ------------------------------------------------------------------------------------------------ T and S
 // part[split][t][c] = factor * sum over the split's k of in[t, k] * B_a[k, c]; B_a = U_a^T (K-contiguous) or, with KMAJOR, V_a (rows of
 // max_rank).  factor: that of dropout, or with KMAJOR scale_a.  A workgroup owns 16 MT tokens and, of the different adapters among
 // them, every gridDim.z-th; its wavefronts and the splits take 64-element chunks of K round robin (a chunk is one 128-byte line of every
-// row).  v_mfma_f32_16x16x32_bf16: lane l supplies row (column) l % 16, elements 8 (l / 16) .. + 8; result lane l holds column l % 16,
-// rows 4 (l / 16) .. + 4.  Rows of other adapters' tokens are replaced by one of the adapter's own: no line is fetched for them.
-// KMAJOR: the lane loads NT neighbouring columns of eight rows at once and packs them, so instruction t covers the columns l % 16 * NT + t.
+// row), each tile of tokens beginning at another of them: rows lie whole powers of two apart, and tiles in step would ask the same few
+// memory channels at a time.  v_mfma_f32_16x16x32_bf16: lane l supplies row (column) l % 16, elements 8 (l / 16) .. + 8; result lane l holds
+// column l % 16, rows 4 (l / 16) .. + 4.  Rows of other adapters' tokens are replaced by one of the adapter's own: no line is fetched
+// for them.  KMAJOR: the lane loads NT neighbouring columns of eight rows at once and packs them, so instruction t covers the columns
+// l % 16 * NT + t.
 constexpr int kThinWaves = 8;
 
 struct ThinArgs {
@@ -92,52 +194,66 @@ struct ThinArgs {
     int64_t ld;
     float* part;             // [splits][b][max_rank]
     DropoutMask drop;
+    int tiles;               // workgroups along x beyond those write down one adapter's tokens each (the backward pass)
+    GroupArgs group;
 };
 
 template <int NT, bool KMAJOR>
-__device__ __forceinline__ void load_b(v4u (&out)[NT], const uint16_t* const (&bp)[NT], int64_t k, int R) {
+__device__ __forceinline__ void load_b(v4u (&out)[NT], const void* b, const uint32_t (&at)[NT], uint32_t k, uint32_t R) {
     if constexpr (!KMAJOR) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) out[t] = *reinterpret_cast<const v4u*>(bp[t] + k);
+        for (int t = 0; t < NT; ++t) out[t] = load_at<v4u>(b, at[t] + 2 * k);
     } else {
-        const uint16_t* b = bp[0] + k * R;
-        if constexpr (NT == 1) {
-            uint32_t e[8];
+        typedef uint32_t row __attribute__((ext_vector_type(NT > 2 ? NT / 2 : 2)));
+        std::conditional_t<NT <= 2, uint32_t, row> e[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) e[u] = b[u * R];
-            out[0] = v4u{pack_lo(e[0], e[1]), pack_lo(e[2], e[3]), pack_lo(e[4], e[5]), pack_lo(e[6], e[7])};
-        } else {
-            uint32_t e[8][NT / 2];
+        for (int u = 0; u < 8; ++u) {
+            const uint32_t o = at[0] + 2 * R * (k + u);
+            if constexpr (NT == 1) e[u] = load_at<uint16_t>(b, o);
+            else e[u] = load_at<std::conditional_t<NT <= 2, uint32_t, row>>(b, o);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            uint32_t w[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const uint16_t* q = b + u * R;
-                if constexpr (NT == 2) {
-                    e[u][0] = *reinterpret_cast<const uint32_t*>(q);
-                } else if constexpr (NT == 4) {
-                    const uint2 w = *reinterpret_cast<const uint2*>(q);
-                    e[u][0] = w.x; e[u][1] = w.y;
-                } else {
-                    const uint4 w = *reinterpret_cast<const uint4*>(q);
-                    e[u][0] = w.x; e[u][1] = w.y; e[u][2] = w.z; e[u][3] = w.w;
-                }
+                if constexpr (NT <= 2) w[u] = e[u];
+                else w[u] = e[u][t / 2];
             }
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-                out[t] = (t & 1) ? v4u{pack_hi(e[0][t / 2], e[1][t / 2]), pack_hi(e[2][t / 2], e[3][t / 2]),
-                                       pack_hi(e[4][t / 2], e[5][t / 2]), pack_hi(e[6][t / 2], e[7][t / 2])}
-                                 : v4u{pack_lo(e[0][t / 2], e[1][t / 2]), pack_lo(e[2][t / 2], e[3][t / 2]),
-                                       pack_lo(e[4][t / 2], e[5][t / 2]), pack_lo(e[6][t / 2], e[7][t / 2])};
+            out[t] = (t & 1) ? v4u{pack_hi(w[0], w[1]), pack_hi(w[2], w[3]), pack_hi(w[4], w[5]), pack_hi(w[6], w[7])}
+                             : v4u{pack_lo(w[0], w[1]), pack_lo(w[2], w[3]), pack_lo(w[4], w[5]), pack_lo(w[6], w[7])};
         }
     }
 }
+
+// The operands of one chunk.
+template <int NT, int MT>
+struct Chunk {
+    v4u x[MT][2], b[2][NT];
+    template <bool KMAJOR>
+    __device__ __forceinline__ void load(const uint16_t* const (&ap)[MT], const void* bbase, const uint32_t (&bat)[NT], uint32_t k0,
+                                         uint32_t R) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) x[i][h] = *reinterpret_cast<const v4u*>(ap[i] + k0 + h * 32);
+            load_b<NT, KMAJOR>(b[h], bbase, bat, k0 + h * 32, R);
+        }
+    }
+};
 
 template <int NT, int MT, bool KMAJOR, bool DROP>
 __global__ void __launch_bounds__(64 * kThinWaves)
 thin_kernel(ThinArgs g) {
     constexpr int ROWS = 16 * MT;
+    constexpr bool AHEAD = 16 * (MT + NT) + 4 * MT * NT <= 128;      // registers for two chunks
     __shared__ float s_part[kThinWaves][NT][4][64];      // [wavefront][rank tile][register][lane]
     __shared__ int s_id[64];
     const AdapterPool& p = g.p;
+    if (KMAJOR && (int)blockIdx.x >= g.tiles) {
+        if (blockIdx.y == 0 && blockIdx.z == 0) group_tokens<64 * kThinWaves>(p, g.group, (int)blockIdx.x - g.tiles);
+        return;
+    }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lr = lane & 15, kg = lane >> 4;
     const int R = p.max_rank;
@@ -155,6 +271,8 @@ thin_kernel(ThinArgs g) {
             if (row0 + r < p.b && !is_adapter(p, s_id[r])) part[row0 * R + i] = 0.0f;
         }
     }
+    const int chunk0 = split * kThinWaves + wave, step = splits * kThinWaves, whole = (int)(K >> 6);
+    const int count = whole > chunk0 ? (whole - chunk0 + step - 1) / step : 0;      // whole chunks of this wavefront
     for (unsigned seen = 0; tile.todo; ++seen) {
         uint64_t mine;
         const int a = tile.next(mine);
@@ -170,54 +288,61 @@ thin_kernel(ThinArgs g) {
             ap[i] = g.in + (int64_t)token[i] * g.ld + kg * 8;
         }
         // columns beyond the pool's, or beyond the adapter's own, are replaced by the first one; their results are zero
-        const uint16_t* bp[NT];
+        const uint16_t* b = (KMAJOR ? p.V : p.U) + (int64_t)a * K * R;
+        uint32_t bat[NT];                                // bytes from there; an adapter has at most 2^30
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            if (KMAJOR) bp[t] = p.V + (int64_t)a * p.n * R + (int64_t)(kg * 8) * R + (lr * NT < R ? lr * NT : 0);
-            else bp[t] = p.U + ((int64_t)a * R + (t * 16 + lr < rank ? t * 16 + lr : 0)) * K + kg * 8;
+            if (KMAJOR) bat[t] = 2 * (kg * 8 * R + (lr * NT < R ? lr * NT : 0));
+            else bat[t] = 2 * ((uint32_t)(t * 16 + lr < rank ? t * 16 + lr : 0) * (uint32_t)K + kg * 8);
         }
         v4f acc[MT][NT];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int t = 0; t < NT; ++t) acc[i][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        const int64_t step = (int64_t)splits * kThinWaves * 64;
-        int64_t k0 = ((int64_t)split * kThinWaves + wave) * 64;
-        for (; k0 + 64 <= K; k0 += step) {
-            v4u x[MT][2], b[2][NT];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < MT; ++i) x[i][h] = *reinterpret_cast<const v4u*>(ap[i] + k0 + h * 32);
-                load_b<NT, KMAJOR>(b[h], bp, k0 + h * 32, R);
-            }
+        const auto multiply = [&](const Chunk<NT, MT>& q, uint32_t k0) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    if (DROP) x[i][h] = drop_eight(g.drop, x[i][h], token[i], (uint32_t)((k0 + h * 32) >> 3) + kg);
+                    v4u x = q.x[i][h];
+                    if (DROP) x = drop_eight(g.drop, x, token[i], ((k0 + h * 32) >> 3) + kg);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[i][t] = mfma(x[i][h], b[h][t], acc[i][t]);
+                    for (int t = 0; t < NT; ++t) acc[i][t] = mfma(x, q.b[h][t], acc[i][t]);
                 }
+        };
+        if (count > 0) {
+            int at = (int)(blockIdx.x % (unsigned)count);
+            const auto k_of = [&](int i) { return (uint32_t)(chunk0 + i * step) * 64; };
+            const auto after = [&](int i) { return i + 1 < count ? i + 1 : 0; };
+            Chunk<NT, MT> now, next;
+            now.template load<KMAJOR>(ap, b, bat, k_of(at), R);
+#pragma unroll 1
+            for (int j = 0; j < count; ++j) {
+                if (AHEAD && j + 1 < count) next.template load<KMAJOR>(ap, b, bat, k_of(after(at)), R);
+                multiply(now, k_of(at));
+                at = after(at);
+                if (AHEAD) now = next;
+                else if (j + 1 < count) now.template load<KMAJOR>(ap, b, bat, k_of(at), R);
+            }
         }
-        if (k0 < K) {                                    // the last chunk, if K is not a multiple of 64: eights beyond K are zero
+        if ((K & 63) && whole % step == chunk0) {        // the last chunk, if K is not a multiple of 64: eights beyond K are zero
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int64_t k = k0 + h * 32;
-                const bool ok = k + kg * 8 < K;
-                const int64_t kc = ok ? k : -(int64_t)kg * 8;
-                v4u b[NT];
-                load_b<NT, KMAJOR>(b, bp, kc, R);
+                const int64_t k = (int64_t)whole * 64 + h * 32;
+                const bool ok = k + kg * 8 < K;          // a lane without elements loads the row's first
+                v4u y[NT];
+                load_b<NT, KMAJOR>(y, b, bat, (uint32_t)(ok ? k : -(int64_t)kg * 8), R);
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
-                    if (!ok) b[t] = v4u{0, 0, 0, 0};
+                    if (!ok) y[t] = v4u{0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    v4u x = *reinterpret_cast<const v4u*>(ap[i] + kc);
+                    v4u x = *reinterpret_cast<const v4u*>(ap[i] + (ok ? k : -(int64_t)kg * 8));
                     if (DROP) x = drop_eight(g.drop, x, token[i], (uint32_t)(k >> 3) + kg);
                     if (!ok) x = v4u{0, 0, 0, 0};
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[i][t] = mfma(x, b[t], acc[i][t]);
+                    for (int t = 0; t < NT; ++t) acc[i][t] = mfma(x, y[t], acc[i][t]);
                 }
             }
         }
@@ -243,25 +368,76 @@ thin_kernel(ThinArgs g) {
     }
 }
 
-// out = sum of the splits' parts, in order.
-__global__ void __launch_bounds__(256)
-thin_join_kernel(const float* part, int splits, int64_t total, float* out) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;       // total is a multiple of 8
-    if (i >= total) return;
-    float4 sum = *reinterpret_cast<const float4*>(part + i);
-    for (int s = 1; s < splits; ++s) {
-        const float4 q = *reinterpret_cast<const float4*>(part + s * total + i);
-        sum.x += q.x; sum.y += q.y; sum.z += q.z; sum.w += q.w;
+// Eight neighbouring values of the parts' sum, the parts in order; four of them on their way at once.
+__device__ __forceinline__ void sum_parts(const float* part, int splits, int64_t size, int64_t at, v4f& lo, v4f& hi) {
+    lo = hi = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = 0; s0 < splits; s0 += 4) {
+        v4f l[4], h[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float* q = part + (s0 + u < splits ? s0 + u : s0) * size + at;
+            l[u] = *reinterpret_cast<const v4f*>(q);
+            h[u] = *reinterpret_cast<const v4f*>(q + 4);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (s0 + u < splits) { lo += l[u]; hi += h[u]; }
     }
-    *reinterpret_cast<float4*>(out + i) = sum;
 }
+
+// ------------------------------------------------------------------------------------------------ pieces of T and S for the gradients
+// What grad_kernel multiplies with: for every 32 places of the order, rank tile of 16 and piece the second operand of one matrix
+// instruction as the lanes hold it (lane l: column l % 16, places 8 (l / 16) .. + 8), 16 bytes a lane; 0 where a place has no token.  Split here
+// once, and not by each of the column tiles that read it.
+struct PieceArgs {
+    int64_t b, groups;       // groups: of 32 places
+    int R, tiles;            // tiles: ceil(R / 16)
+    const int* order;
+    const float* thin[2];    // T, and the parts of S; null: not wanted
+    int splits[2];
+    v4u* out[2];             // [places / 32][tiles][3][64]
+};
+
+__device__ __forceinline__ void write_pieces(const PieceArgs& g, int64_t group) {
+    if (group >= g.groups) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int* order = g.order + group * 32 + 8 * (lane >> 4);
+    int token[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) token[u] = order[u];
+    for (int i = wave; i < 2 * g.tiles; i += waves) {
+        const int job = i >= g.tiles ? 1 : 0, t = i - job * g.tiles, c = t * 16 + (lane & 15);
+        if (!g.thin[job]) continue;
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            x[u] = 0.0f;
+            if ((uint64_t)(int64_t)token[u] < (uint64_t)g.b && c < g.R) {
+                const float* q = g.thin[job] + (int64_t)token[u] * g.R + c;
+                for (int s = 0; s < g.splits[job]; ++s) x[u] += q[s * g.b * g.R];
+            }
+        }
+        uint32_t piece[3][8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) split3(x[u], piece[0][u], piece[1][u], piece[2][u]);
+        v4u* o = g.out[job] + ((group * g.tiles + t) * 3) * 64 + lane;
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            o[k * 64] = v4u{pack_hi(piece[k][0], piece[k][1]), pack_hi(piece[k][2], piece[k][3]), pack_hi(piece[k][4], piece[k][5]),
+                            pack_hi(piece[k][6], piece[k][7])};
+    }
+}
+
+__global__ void __launch_bounds__(256)
+pieces_kernel(PieceArgs g) { write_pieces(g, blockIdx.x); }
 
 // ------------------------------------------------------------------------------------------------ Y and E_X
 // out[t, f] = base[t, f] + sum over c of thin[t, c] * B_a[f, c]; B_a = scale_a V_a (c contiguous) or, with BWD, U_a^T with the mask of dropout
-// on the sum.  A wavefront owns 16 MT tokens, the columns of its matrix instructions (their thin values stay in registers, split in
-// pieces), and goes over blocks of features, the rows: 64 with 16-byte loads of V, or 128 columns of U, loaded eight neighbouring
-// columns of eight rank rows at a time and packed, so that instruction v covers the columns 8 i + v.  Either way a lane ends up with
-// runs of eight neighbouring features of one token: 16-byte loads of base and stores.
+// on the sum.  A workgroup owns 16 MT tokens, the columns of its matrix instructions, whose thin values it keeps in LDS as the operands'
+// lanes hold them, split in pieces.  Its wavefronts go over blocks of features, the rows: 64 with 16-byte loads of V, or 64 columns of U,
+// loaded four neighbouring columns of eight rank rows at a time and packed, so that instruction v covers the columns 4 i + v.  Either way a
+// lane ends up with runs of eight neighbouring features of one token: 16-byte loads of base and stores.  The next block's adapter values and
+// the next token tile's base are on their way while one is worked on.
 // RC: rank chunks of 32.  RC == 0 (rank up to 16): the halves of the instruction's 32 products hold the pieces (high, middle) and (low,
 // nothing), two instructions instead of three.
 constexpr int kWideWaves = 4;
@@ -270,305 +446,290 @@ struct WideArgs {
     AdapterPool p;
     const float* part;       // [splits][b][max_rank]
     int splits;
-    float* thin;             // the sum of the parts is written here if splits > 1
+    float* thin;             // the sum of the parts is written here (not if null)
     const void* base;
     int64_t ld_base;
     void* out;
     int64_t ld_out;
     DropoutMask drop;
+    int tiles;               // workgroups along x beyond those write 32 places' pieces each (the backward pass)
+    PieceArgs pieces;
 };
 
+// Eight neighbouring elements of base, as they are in memory.
 template <bool F32>
-__device__ __forceinline__ void add_base_and_store(const WideArgs& g, int64_t token, int64_t f, float (&y)[8]) {
-    if constexpr (F32) {
-        float* o = reinterpret_cast<float*>(g.out) + token * g.ld_out + f;
-        if (g.base) {
-            const float* q = reinterpret_cast<const float*>(g.base) + token * g.ld_base + f;
-            const v4f lo = *reinterpret_cast<const v4f*>(q), hi = *reinterpret_cast<const v4f*>(q + 4);
+struct BaseEight {
+    v4u q[F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const void* base, int64_t at) {
+        const v4u* s = reinterpret_cast<const v4u*>(reinterpret_cast<const char*>(base) + at * (F32 ? 4 : 2));
+        q[0] = s[0];
+        if constexpr (F32) q[1] = s[1];
+    }
+    __device__ __forceinline__ void add(float (&y)[8]) const {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { y[j] += lo[j]; y[4 + j] += hi[j]; }
-        }
-        *reinterpret_cast<v4f*>(o) = v4f{y[0], y[1], y[2], y[3]};
-        *reinterpret_cast<v4f*>(o + 4) = v4f{y[4], y[5], y[6], y[7]};
-    } else {
-        uint16_t* o = reinterpret_cast<uint16_t*>(g.out) + token * g.ld_out + f;
-        if (g.base) {
-            const v4u q = *reinterpret_cast<const v4u*>(reinterpret_cast<const uint16_t*>(g.base) + token * g.ld_base + f);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                y[2 * j] += __uint_as_float(q[j] << 16);
-                y[2 * j + 1] += __uint_as_float(q[j] & 0xFFFF0000u);
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (F32) {
+                y[j] += __uint_as_float(q[0][j]);
+                y[4 + j] += __uint_as_float(q[1][j]);
+            } else {
+                y[2 * j] += __uint_as_float(q[0][j] << 16);
+                y[2 * j + 1] += __uint_as_float(q[0][j] & 0xFFFF0000u);
             }
         }
+    }
+};
+template <bool F32>
+__device__ __forceinline__ void store_eight(void* out, int64_t at, const float (&y)[8]) {
+    v4u* o = reinterpret_cast<v4u*>(reinterpret_cast<char*>(out) + at * (F32 ? 4 : 2));
+    if constexpr (F32) {
+        o[0] = __builtin_bit_cast(v4u, v4f{y[0], y[1], y[2], y[3]});
+        o[1] = __builtin_bit_cast(v4u, v4f{y[4], y[5], y[6], y[7]});
+    } else {
         v4u w;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[2 * j]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[2 * j + 1]) << 16;
-        *reinterpret_cast<v4u*>(o) = w;
+        o[0] = w;
     }
 }
 
 template <int RC_, int MT, bool BWD, bool F32>
-__global__ void __launch_bounds__(64 * kWideWaves)
+__global__ void __launch_bounds__(64 * kWideWaves, BWD && RC_ == 4 ? 1 : 2)
 wide_kernel(WideArgs g) {
     constexpr bool STACK = RC_ == 0;
     constexpr int RC = STACK ? 1 : RC_, NP = STACK ? 2 : 3, ROWS = 16 * MT;
-    constexpr int FB = BWD ? 128 : 64;                   // features per trip
+    constexpr int FB = 64;                               // features per block
+    constexpr int NQ = 2;                                // runs of eight features of a lane and token tile
+    constexpr bool AHEAD = RC <= 2;                      // registers for two blocks of the adapter
+    __shared__ v4u s_thin[MT * RC * NP][64];
+    __shared__ int s_id[64];
+    if (BWD && (int)blockIdx.x >= g.tiles) {
+        if (blockIdx.z == 0) {
+            const int64_t group = ((int64_t)blockIdx.x - g.tiles) * gridDim.y + blockIdx.y;
+            write_pieces(g.pieces, group);
+        }
+        return;
+    }
     const AdapterPool& p = g.p;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int lr = lane & 15, kg = lane >> 4;
     const int R = p.max_rank;
     const int64_t wide = BWD ? p.m : p.n;
     const int64_t row0 = (int64_t)blockIdx.x * ROWS;
-    const bool lane_token = lane < ROWS && row0 + lane < p.b;
-    TileAdapters tile(p, lane_token ? p.adapter_of[row0 + lane] : -1, lane < ROWS);
+    if (wave == 0) s_id[lane] = lane < ROWS && row0 + lane < p.b ? p.adapter_of[row0 + lane] : -1;
+    __syncthreads();
+    TileAdapters tile(p, s_id[lane], lane < ROWS);
+    const uint64_t bare = __ballot(lane < ROWS && row0 + lane < p.b) & ~tile.todo;
     const int64_t f_first = ((int64_t)blockIdx.y * kWideWaves + wave) * FB, f_step = (int64_t)gridDim.y * kWideWaves * FB;
-
-    // the thin values of the lane's tokens, in pieces
     const int r_lane = STACK ? 8 * (kg & 1) : 8 * kg;
-    v4u bp[MT][RC][NP];
+
+    // the work of this wavefront: the blocks of features for one adapter after the other
+    unsigned seen = 0;
+    int a = -1, rank = 0;
+    uint64_t mine = 0;
+    const auto next_adapter = [&]() {
+        a = -1;
+        while (tile.todo) {
+            uint64_t m;
+            const int b = tile.next(m);
+            if (seen++ % gridDim.z == blockIdx.z) { a = b; mine = m; rank = rank_of(p, b); return; }
+        }
+    };
+    // Every lane loads, from a place that exists; what is not the adapter's is cleared in finish().
+    struct Block {
+        v4u w[RC][4];                                    // as loaded; after finish(): operand q of rank chunk c
+        __device__ __forceinline__ void load(const AdapterPool& p, int a, int64_t wide, int64_t f0, int lr, int r_lane) {
+            const int R = p.max_rank;
+            const uint16_t* b = (BWD ? p.U : p.V) + (int64_t)a * wide * R;   // of at most 2^30 bytes
+            if constexpr (!BWD) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        int64_t t = row0 + i * 16 + lr;
-        const bool real = t < p.b;
-        if (!real) t = p.b - 1;
-        const int a = __shfl(tile.id, i * 16 + lr);
-        const float scale = !BWD && is_adapter(p, a) ? scale_of(p, a) : 1.0f;
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t f = (uint32_t)f0 + 32 * (q >> 1) + 8 * (lr >> 2) + 4 * (q & 1) + (lr & 3);
+                    if (f >= (uint32_t)wide) f = (uint32_t)wide - 1;         // its results are not stored
 #pragma unroll
-        for (int c = 0; c < RC; ++c) {
-            const int r = 32 * c + r_lane;
-            float x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = 0.0f;
-            if (r < R) {                                 // R is a multiple of eight
-                const float* q = g.part + t * R + r;
-                v4f lo = *reinterpret_cast<const v4f*>(q), hi = *reinterpret_cast<const v4f*>(q + 4);
-                for (int s = 1; s < g.splits; ++s) {
-                    q += p.b * R;
-                    lo += *reinterpret_cast<const v4f*>(q);
-                    hi += *reinterpret_cast<const v4f*>(q + 4);
+                    for (int c = 0; c < RC; ++c) {
+                        const int r = 32 * c + r_lane;
+                        w[c][q] = load_at<v4u>(b, 2 * (f * R + (r < R ? r : 0)));
+                    }
                 }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { x[j] = lo[j]; x[4 + j] = hi[j]; }
-                if (g.splits > 1 && blockIdx.y == 0 && blockIdx.z == 0 && wave == 0 && real && !(STACK && kg > 1)) {
-                    float* o = g.thin + t * R + r;
-                    *reinterpret_cast<v4f*>(o) = lo;
-                    *reinterpret_cast<v4f*>(o + 4) = hi;
-                }
-            }
-            uint32_t piece[3][8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) split3(x[j] * scale, piece[0][j], piece[1][j], piece[2][j]);
-            v4u q[3];
-#pragma unroll
-            for (int k = 0; k < 3; ++k)
-                q[k] = v4u{pack_hi(piece[k][0], piece[k][1]), pack_hi(piece[k][2], piece[k][3]), pack_hi(piece[k][4], piece[k][5]),
-                           pack_hi(piece[k][6], piece[k][7])};
-            if constexpr (STACK) {
-                bp[i][c][0] = kg < 2 ? q[0] : q[1];
-                bp[i][c][1] = kg < 2 ? q[2] : v4u{0, 0, 0, 0};
             } else {
+                uint32_t col = (uint32_t)f0 + 4 * lr;
+                if (col >= (uint32_t)wide) col = 0;                          // its results are not stored
 #pragma unroll
-                for (int k = 0; k < 3; ++k) bp[i][c][k] = q[k];
+                for (int c = 0; c < RC; ++c) {
+                    const int r = 32 * c + r_lane;                           // R is a multiple of eight
+                    uint32_t at = 2 * ((r < R ? r : 0) * (uint32_t)wide + col);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u, at += 2 * (uint32_t)wide) {
+                        const uint2 x = load_at<uint2>(b, at);
+                        w[c][u >> 1][2 * (u & 1)] = x.x;
+                        w[c][u >> 1][2 * (u & 1) + 1] = x.y;
+                    }
+                }
             }
         }
+        __device__ __forceinline__ void finish(int rank, int r_lane) {
+            if (rank < (STACK ? 16 : 32 * RC)) {
+#pragma unroll
+                for (int c = 0; c < RC; ++c) {
+                    const int r = 32 * c + r_lane;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if constexpr (!BWD) {            // dword j of every operand: the ranks r + 2 j, r + 2 j + 1
+                            const uint32_t keep = (r + 2 * j < rank ? 0xFFFFu : 0u) | (r + 2 * j + 1 < rank ? 0xFFFF0000u : 0u);
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) w[c][q][j] &= keep;
+                        } else {                         // two dwords of the rank row r + 2 j, two of the next
+                            const uint32_t even = r + 2 * j < rank ? ~0u : 0u, odd = r + 2 * j + 1 < rank ? ~0u : 0u;
+                            w[c][j] &= v4u{even, even, odd, odd};
+                        }
+                    }
+                }
+            }
+            if constexpr (BWD) {                         // eight rows of four columns become four columns
+#pragma unroll
+                for (int c = 0; c < RC; ++c) {
+                    v4u y[4];
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const int d = v >> 1;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            y[v][j] = (v & 1) ? pack_hi(w[c][j][d], w[c][j][2 + d]) : pack_lo(w[c][j][d], w[c][j][2 + d]);
+                    }
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) w[c][v] = y[v];
+                }
+            }
+        }
+    };
+    // feature of run q of the lane in the block at f0
+    const auto run_at = [&](int64_t f0, int q) { return f0 + (BWD ? 16 * kg + 8 * q : 32 * q + 8 * kg); };
+    // a lane whose token has another adapter takes one of this adapter's own
+    const auto load_base = [&](BaseEight<F32> (&x)[NQ], int i, int64_t f0) {
+        if (!g.base) return;
+        const int64_t t = row0 + ((mine >> (i * 16 + lr)) & 1 ? i * 16 + lr : __builtin_ctzll(mine));
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const int64_t f = run_at(f0, q);
+            x[q].load(g.base, t * g.ld_base + (f < wide ? f : 0));
+        }
+    };
+
+    next_adapter();
+    Block now;
+    if (a >= 0 && f_first < wide) now.load(p, a, wide, f_first, lr, r_lane);
+
+    // the thin values of the tile's tokens, in pieces
+    for (int j = wave; j < MT * RC; j += kWideWaves) {
+        const int i = j / RC, r = 32 * (j % RC) + r_lane;
+        const int64_t t = row0 + i * 16 + lr;
+        const int id = s_id[i * 16 + lr];
+        const float scale = !BWD && is_adapter(p, id) ? scale_of(p, id) : 1.0f;
+        v4f lo = v4f{0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
+        if (r < R && t < p.b) {                          // R is a multiple of eight
+            sum_parts(g.part, g.splits, p.b * R, t * R + r, lo, hi);
+            if (g.thin && blockIdx.y == 0 && blockIdx.z == 0 && !(STACK && kg > 1)) {
+                *reinterpret_cast<v4f*>(g.thin + t * R + r) = lo;
+                *reinterpret_cast<v4f*>(g.thin + t * R + r + 4) = hi;
+            }
+        }
+        uint32_t piece[3][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) split3((e < 4 ? lo[e & 3] : hi[e & 3]) * scale, piece[0][e], piece[1][e], piece[2][e]);
+        v4u q[3];
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            q[k] = v4u{pack_hi(piece[k][0], piece[k][1]), pack_hi(piece[k][2], piece[k][3]), pack_hi(piece[k][4], piece[k][5]),
+                       pack_hi(piece[k][6], piece[k][7])};
+        if constexpr (STACK) {
+            s_thin[j * NP][lane] = kg < 2 ? q[0] : q[1];
+            s_thin[j * NP + 1][lane] = kg < 2 ? q[2] : v4u{0, 0, 0, 0};
+        } else {
+#pragma unroll
+            for (int k = 0; k < NP; ++k) s_thin[j * NP + k][lane] = q[k];
+        }
     }
+    __syncthreads();
 
     if (blockIdx.z == 0 && g.base != g.out) {            // tokens without an adapter: the base as it is
-        const uint64_t bare = __ballot(lane_token) & ~tile.todo;
         for (uint64_t todo = bare; todo; todo &= todo - 1) {
             const int64_t t = row0 + __builtin_ctzll(todo);
             for (int64_t f0 = f_first; f0 < wide; f0 += f_step) {
                 const int64_t f = f0 + 8 * lane;
                 if (8 * lane >= FB || f >= wide) continue;
+                BaseEight<F32> x;
                 float y[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                add_base_and_store<F32>(g, t, f, y);
+                if (g.base) { x.load(g.base, t * g.ld_base + f); x.add(y); }
+                store_eight<F32>(g.out, t * g.ld_out + f, y);
             }
         }
     }
 
-    for (unsigned seen = 0; tile.todo; ++seen) {
-        uint64_t mine;
-        const int a = tile.next(mine);
-        if (seen % gridDim.z != blockIdx.z) continue;
-        const int rank = rank_of(p, a);
+    for (; a >= 0; next_adapter()) {
+        if (f_first >= wide) continue;
+        if (seen > 1 + blockIdx.z) now.load(p, a, wide, f_first, lr, r_lane);       // not the first adapter of this wavefront
         for (int64_t f0 = f_first; f0 < wide; f0 += f_step) {
-            if constexpr (!BWD) {
-                v4u v[4][RC];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    int64_t f = f0 + 32 * (q >> 1) + 8 * (lr >> 2) + 4 * (q & 1) + (lr & 3);
-                    if (f >= wide) f = wide - 1;         // its results are not stored
-#pragma unroll
-                    for (int c = 0; c < RC; ++c) {
-                        const int r = 32 * c + r_lane;
-                        v[q][c] = v4u{0, 0, 0, 0};
-                        if (r < rank) {
-                            v[q][c] = *reinterpret_cast<const v4u*>(p.V + ((int64_t)a * p.n + f) * R + r);
-                            if (r + 8 > rank) {          // the adapter's rank ends inside the eight
-#pragma unroll
-                                for (int j = 0; j < 4; ++j)
-                                    v[q][c][j] &= (r + 2 * j < rank ? 0xFFFFu : 0u) | (r + 2 * j + 1 < rank ? 0xFFFF0000u : 0u);
-                            }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
+            now.finish(rank, r_lane);
+            Block ahead;
+            if (AHEAD && f0 + f_step < wide) ahead.load(p, a, wide, f0 + f_step, lr, r_lane);
+            BaseEight<F32> base[NQ], base_ahead[NQ];
+            load_base(base, 0, f0);
+#pragma unroll 1
+            for (int i = 0; i < MT; ++i) {
+                if (i + 1 < MT) load_base(base_ahead, i + 1, f0);
+                if ((mine >> (i * 16)) & 0xFFFF) {
                     v4f acc[4];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        acc[q] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int q = 0; q < 4; ++q) acc[q] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int c = 0; c < RC; ++c)
+                    for (int c = 0; c < RC; ++c)
 #pragma unroll
-                            for (int k = 0; k < NP; ++k) acc[q] = mfma(v[q][c], bp[i][c][k], acc[q]);
-                    }
-                    if (!((mine >> (i * 16 + lr)) & 1)) continue;
-                    const int64_t t = row0 + i * 16 + lr;
+                        for (int k = 0; k < NP; ++k) {
+                            const v4u b = s_thin[(i * RC + c) * NP + k][lane];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int64_t f = f0 + 32 * h + 8 * kg;
-                        if (f >= wide) continue;
-                        float y[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) y[j] = acc[2 * h + (j >> 2)][j & 3];
-                        add_base_and_store<F32>(g, t, f, y);
-                    }
-                }
-            } else {
-                v4f acc[MT][8];
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int v = 0; v < 8; ++v) acc[i][v] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-                int64_t col = f0 + 8 * lr;
-                if (col >= wide) col = 0;                // its results are not stored
-#pragma unroll
-                for (int c = 0; c < RC; ++c) {
-                    v4u raw[8];
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const int r = 32 * c + r_lane + u;
-                        raw[u] = v4u{0, 0, 0, 0};
-                        if (r < rank) raw[u] = *reinterpret_cast<const v4u*>(p.U + ((int64_t)a * R + r) * wide + col);
-                    }
-#pragma unroll
-                    for (int v = 0; v < 8; ++v) {
-                        const int d = v >> 1;
-                        const v4u x = (v & 1) ? v4u{pack_hi(raw[0][d], raw[1][d]), pack_hi(raw[2][d], raw[3][d]),
-                                                    pack_hi(raw[4][d], raw[5][d]), pack_hi(raw[6][d], raw[7][d])}
-                                              : v4u{pack_lo(raw[0][d], raw[1][d]), pack_lo(raw[2][d], raw[3][d]),
-                                                    pack_lo(raw[4][d], raw[5][d]), pack_lo(raw[6][d], raw[7][d])};
-#pragma unroll
-                        for (int i = 0; i < MT; ++i)
-#pragma unroll
-                            for (int k = 0; k < NP; ++k) acc[i][v] = mfma(x, bp[i][c][k], acc[i][v]);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    if (!((mine >> (i * 16 + lr)) & 1)) continue;
-                    const int64_t t = row0 + i * 16 + lr;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int64_t f = f0 + 8 * (4 * kg + e);
-                        if (f >= wide) continue;
-                        float y[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) y[j] = acc[i][j][e];
-                        if (g.drop.least) {
-                            const uint4 bits = dropout_bits(g.drop, (uint32_t)t, (uint32_t)(f >> 3));
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) y[j] = dropout_kept(g.drop, bits, j) ? y[j] * g.drop.factor : 0.0f;
+                            for (int q = 0; q < 4; ++q) acc[q] = mfma(now.w[c][q], b, acc[q]);
                         }
-                        add_base_and_store<F32>(g, t, f, y);
+                    if ((mine >> (i * 16 + lr)) & 1) {
+                        const int64_t t = row0 + i * 16 + lr;
+#pragma unroll
+                        for (int q = 0; q < NQ; ++q) {
+                            const int64_t f = run_at(f0, q);
+                            if (f >= wide) continue;
+                            float y[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) y[j] = BWD ? acc[j & 3][2 * q + (j >> 2)] : acc[2 * q + (j >> 2)][j & 3];
+                            if (BWD && g.drop.least) {
+                                const uint4 bits = dropout_bits(g.drop, (uint32_t)t, (uint32_t)(f >> 3));
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) y[j] = dropout_kept(g.drop, bits, j) ? y[j] * g.drop.factor : 0.0f;
+                            }
+                            if (g.base) base[q].add(y);
+                            store_eight<F32>(g.out, t * g.ld_out + f, y);
+                        }
                     }
                 }
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) base[q] = base_ahead[q];
             }
+            if (AHEAD) now = ahead;
+            else if (f0 + f_step < wide) now.load(p, a, wide, f0 + f_step, lr, r_lane);
         }
     }
 }
 
 // ------------------------------------------------------------------------------------------------ adapter gradients
-// Tokens adapter by adapter.  order: the tokens that have an adapter, by adapter and then by index; start[a] .. start[a + 1]: those of a.
-// A cut is a multiple of `chunk` in that order; a piece is what one adapter has between cuts, so adapter a's pieces are
-// 1 + (cuts strictly inside its range), at least one even without tokens.  Piece i of adapter a has the index
-// a + start[a] / chunk + i: at most slots + b / chunk of them, in order, none shared; indices that no adapter takes hold no tokens.
-struct Piece {
-    int adapter;             // -1: no piece
-    int begin, end;          // in `order`
-    int part;                // where its sum goes: -1: it is the adapter's only piece, straight to the result
-};
-
-// A workgroup per adapter: finds its tokens, writes them down and its pieces.  A piece that is not alone begins or ends at a cut k: its
-// sum goes to part k (it begins there) or cuts + k (it is the first one, and ends there).
-constexpr int kGroupThreads = 1024;
-
-__global__ void __launch_bounds__(kGroupThreads)
-group_kernel(AdapterPool p, int chunk, int* order, int* start, Piece* pieces) {
-    __shared__ int s_less[kGroupThreads / 64], s_same[kGroupThreads / 64];
-    const int a = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int b = (int)p.b, cuts = (b + chunk - 1) / chunk;
-    int less = 0, same = 0;
-    for (int t = tid; t < b; t += kGroupThreads) {
-        const int id = p.adapter_of[t];
-        less += id >= 0 && id < a;
-        same += id == a;
-    }
-    for (int h = 32; h > 0; h >>= 1) { less += __shfl_xor(less, h); same += __shfl_xor(same, h); }
-    if (lane == 0) { s_less[wave] = less; s_same[wave] = same; }
-    __syncthreads();
-    less = same = 0;
-    for (int w = 0; w < kGroupThreads / 64; ++w) { less += s_less[w]; same += s_same[w]; }
-    const int begin = less, end = less + same;
-    if (tid == 0) {
-        start[a] = begin;
-        if (a == p.slots - 1) start[p.slots] = end;
-    }
-    const int count = same ? (end + chunk - 1) / chunk - begin / chunk : 1;
-    const int index = a + begin / chunk, next = a == p.slots - 1 ? p.slots + cuts : a + 1 + end / chunk;
-    for (int i = tid; index + i < next; i += kGroupThreads) {
-        Piece q{-1, 0, 0, -1};
-        if (i < count) {
-            const int cut = begin / chunk + i;           // the piece lies between this cut and the next
-            q.adapter = a;
-            q.begin = i == 0 ? begin : cut * chunk;
-            q.end = i == count - 1 ? end : (cut + 1) * chunk;
-            q.part = count == 1 ? -1 : i == 0 ? cuts + cut + 1 : cut;
-        }
-        pieces[index + i] = q;
-    }
-    int at = begin;
-    for (int t0 = 0; t0 < b && same > 0; t0 += kGroupThreads) {
-        const int t = t0 + tid;
-        const bool hit = t < b && p.adapter_of[t] == a;
-        const uint64_t hits = __ballot(hit);
-        __syncthreads();
-        if (lane == 0) s_same[wave] = __builtin_popcountll(hits);
-        __syncthreads();
-        int before = 0, all = 0;
-        for (int w = 0; w < kGroupThreads / 64; ++w) {
-            before += w < wave ? s_same[w] : 0;
-            all += s_same[w];
-        }
-        const int to = at + before + __builtin_popcountll(hits & ((1ull << lane) - 1));
-        if (hit && to < end) order[to] = t;
-        at += all;
-    }
-}
-
-// The sum over a piece's tokens of big[t, col] * small[t, c]: big bf16 (E for G_V, drop(X) for G_U), small fp32 (T, S).  A workgroup owns 128
-// columns of `big`; its four wavefronts take groups of 32 tokens round robin.  v_mfma_f32_16x16x32_bf16 with k = token: lane l supplies,
-// for row (A) / column (B) l % 16, the eight tokens 8 (l / 16) .. + 8 of the group.  `big` is read eight neighbouring columns of a token at a
-// time; the v-th of them, packed over the eight tokens, is the A operand of the v-th instruction, which covers the columns 8 i + v.
-// `small` is split in three pieces.  NT: rank tiles of 16, from column `c_base` on.
+// The sum over a piece's tokens of big[t, col] * small[t, c]: big bf16 (E for G_V, drop(X) for G_U), small fp32 (T, S), given in pieces.  A
+// workgroup owns 128 columns of `big`; its four wavefronts take groups of 32 places round robin.  v_mfma_f32_16x16x32_bf16 with k =
+// place: lane l supplies, for row (A) / column (B) l % 16, the eight places 8 (l / 16) .. + 8 of the group.  `big` is read eight neighbouring
+// columns of a token at a time; the v-th of them, packed over the eight tokens, is the A operand of the v-th instruction, which covers
+// the columns 8 i + v.  NT: rank tiles of 16, from tile blockIdx.z * NT on.
 constexpr int kGradWaves = 4;
 
 struct GradJob {
     const uint16_t* big;
     int64_t ld;
-    const float* small;
+    const v4u* small;        // PieceArgs::out
     float* out;              // [slots][wide x R], or [slots][R x wide] with rank_major
     float* part;             // [parts] of the same
     int64_t wide;
@@ -579,91 +740,83 @@ struct GradArgs {
     AdapterPool p;
     GradJob job[2];          // G_V, G_U
     const int* order;
-    const Piece* pieces;
+    const Segment* segments;
+    int rank_tiles;
     DropoutMask drop;
 };
 
 template <int NT>
-__global__ void __launch_bounds__(64 * kGradWaves)
+__global__ void __launch_bounds__(64 * kGradWaves, 2)
 grad_kernel(GradArgs g) {
     __shared__ float s_sum[kGradWaves][32][64];          // one rank tile of every wavefront: [v * 4 + e][lane]
-    const Piece piece = g.pieces[blockIdx.y];
-    if (piece.adapter < 0) return;
+    const Segment seg = g.segments[blockIdx.y];
+    if (seg.adapter < 0) return;
     const bool second = (int)blockIdx.x >= g.job[0].tiles;
     const GradJob& job = g.job[second ? 1 : 0];
     const AdapterPool& p = g.p;
-    const int R = p.max_rank, c_base = blockIdx.z * (16 * NT);
+    const int R = p.max_rank, tile0 = blockIdx.z * NT;
     const int64_t wide = job.wide;
     const int64_t c0 = (int64_t)((int)blockIdx.x - (second ? g.job[0].tiles : 0)) * 128;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int i16 = lane & 15, kq = lane >> 4;
     const int64_t col = c0 + 8 * i16;
     const int64_t colc = col < wide ? col : 0;           // columns beyond the matrix are not stored
-    const int rank = rank_of(p, piece.adapter);
     const bool masked = second && g.drop.least != 0;
-    const uint16_t* big = job.big;
-    const float* small = job.small;
+    const uint16_t* big = job.big + colc;
 
     v4f acc[NT][8];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int v = 0; v < 8; ++v) acc[t][v] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int t0 = piece.begin + wave * 32; t0 < piece.end; t0 += kGradWaves * 32) {
-        v4u raw[8];
-        float sv[NT][8];
-        int token[8];
+    int token[8];
+    v4u raw[8];
+    const auto load_group = [&](int place) {             // a multiple of 32; places without a token are negative
+        const int* o = g.order + place + 8 * kq;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) token[u] = o[u];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const int at = t0 + 8 * kq + u;
-            const int t = g.order[at < piece.end ? at : piece.end - 1];
-            token[u] = (unsigned)t < (unsigned)p.b ? t : 0;      // adapter_of may have changed under way; nothing is read beyond the matrices
+            raw[u] = v4u{0, 0, 0, 0};
+            if ((uint64_t)(int64_t)token[u] < (uint64_t)p.b) raw[u] = *reinterpret_cast<const v4u*>(big + token[u] * job.ld);
         }
+    };
+    int place = seg.begin + wave * 32;
+    if (place < seg.end) load_group(place);
+    for (; place < seg.end; place += kGradWaves * 32) {
+        v4u x[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            raw[u] = *reinterpret_cast<const v4u*>(big + token[u] * job.ld + colc);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int c = c_base + t * 16 + i16;
-                sv[t][u] = small[(int64_t)token[u] * R + (c < R ? c : 0)];
-            }
+            x[u] = raw[u];
+            if (masked) x[u] = drop_eight(g.drop, x[u], (uint32_t)token[u], (uint32_t)(colc >> 3));
         }
+        if (place + kGradWaves * 32 < seg.end) load_group(place + kGradWaves * 32);
+        transpose8(x);
+        const v4u* small = job.small + ((int64_t)(place >> 5) * g.rank_tiles + tile0) * 3 * 64;
+        v4u b[3], b_ahead[3];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if (masked) raw[u] = drop_eight(g.drop, raw[u], (uint32_t)token[u], (uint32_t)(colc >> 3));
-            if (t0 + 8 * kq + u >= piece.end) {          // tokens beyond the piece count as zero
-                raw[u] = v4u{0, 0, 0, 0};
-#pragma unroll
-                for (int t = 0; t < NT; ++t) sv[t][u] = 0.0f;
-            }
-        }
-        v4u bp[NT][3];
+        for (int k = 0; k < 3; ++k) b[k] = small[k * 64 + lane];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            uint32_t q[3][8];
+            if (tile0 + t >= g.rank_tiles) break;
+            if (t + 1 < NT && tile0 + t + 1 < g.rank_tiles) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) split3(sv[t][u], q[0][u], q[1][u], q[2][u]);
+                for (int k = 0; k < 3; ++k) b_ahead[k] = small[((t + 1) * 3 + k) * 64 + lane];
+            }
+            __builtin_amdgcn_sched_barrier(0);           // the loads of two rank tiles at a time: all of them would take too many registers
 #pragma unroll
             for (int k = 0; k < 3; ++k)
-                bp[t][k] = v4u{pack_hi(q[k][0], q[k][1]), pack_hi(q[k][2], q[k][3]), pack_hi(q[k][4], q[k][5]), pack_hi(q[k][6], q[k][7])};
-        }
 #pragma unroll
-        for (int v = 0; v < 8; ++v) {
-            const int d = v >> 1;
-            const v4u a = (v & 1) ? v4u{pack_hi(raw[0][d], raw[1][d]), pack_hi(raw[2][d], raw[3][d]), pack_hi(raw[4][d], raw[5][d]),
-                                        pack_hi(raw[6][d], raw[7][d])}
-                                  : v4u{pack_lo(raw[0][d], raw[1][d]), pack_lo(raw[2][d], raw[3][d]), pack_lo(raw[4][d], raw[5][d]),
-                                        pack_lo(raw[6][d], raw[7][d])};
+                for (int v = 0; v < 8; ++v) acc[t][v] = mfma(x[v], b[k], acc[t][v]);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int k = 0; k < 3; ++k) acc[t][v] = mfma(a, bp[t][k], acc[t][v]);
+            for (int k = 0; k < 3; ++k) b[k] = b_ahead[k];
         }
     }
     // The wavefronts' sums meet in LDS, one rank tile at a time, and are added in wavefront order; wavefront w then stores the columns
     // v = 2 w, 2 w + 1 of every eight.
-    const float factor = second ? (masked ? g.drop.factor : 1.0f) : scale_of(p, piece.adapter);
-    float* dst = piece.part < 0 ? job.out + (int64_t)piece.adapter * wide * R : job.part + (int64_t)piece.part * wide * R;
+    const int rank = rank_of(p, seg.adapter);
+    const float factor = second ? (masked ? g.drop.factor : 1.0f) : scale_of(p, seg.adapter);
+    float* dst = seg.part < 0 ? job.out + (int64_t)seg.adapter * wide * R : job.part + (int64_t)seg.part * wide * R;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         if (t > 0) __syncthreads();
@@ -672,7 +825,7 @@ grad_kernel(GradArgs g) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) s_sum[wave][v * 4 + e][lane] = acc[t][v][e];
         __syncthreads();
-        const int c = c_base + t * 16 + i16;
+        const int c = (tile0 + t) * 16 + i16;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float o[2];
@@ -696,12 +849,12 @@ grad_kernel(GradArgs g) {
     }
 }
 
-// Adds up the pieces of every adapter that has several, in order; four neighbouring elements per thread.
+// Adds up the segments of every adapter that has several, in order; four neighbouring elements per thread.
 __global__ void __launch_bounds__(256)
-grad_join_kernel(AdapterPool p, int chunk, const int* start, GradJob v, GradJob u) {
+grad_join_kernel(AdapterPool p, GroupArgs group, GradJob v, GradJob u) {
     const int a = blockIdx.y;
-    const int begin = start[a], end = start[a + 1], cuts = ((int)p.b + chunk - 1) / chunk;
-    const int first = begin / chunk, count = end > begin ? (end + chunk - 1) / chunk - first : 1;
+    const int2 range = group.range[a];
+    const int first = range.x / group.chunk, count = range.y > range.x ? (range.y + group.chunk - 1) / group.chunk - first : 1;
     if (count == 1) return;
     const int64_t size_v = v.tiles ? v.wide * p.max_rank : 0, size_u = u.tiles ? u.wide * p.max_rank : 0;
     int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -710,7 +863,7 @@ grad_join_kernel(AdapterPool p, int chunk, const int* start, GradJob v, GradJob 
     if (second) i -= size_v;
     const GradJob& job = second ? u : v;
     const int64_t size = second ? size_u : size_v;
-    float4 sum = *reinterpret_cast<const float4*>(job.part + (int64_t)(cuts + first + 1) * size + i);
+    float4 sum = *reinterpret_cast<const float4*>(job.part + (int64_t)(group.cuts + first + 1) * size + i);
     for (int k = 1; k < count; ++k) {
         const float4 q = *reinterpret_cast<const float4*>(job.part + (int64_t)(first + k) * size + i);
         sum.x += q.x; sum.y += q.y; sum.z += q.z; sum.w += q.w;
@@ -721,6 +874,8 @@ grad_join_kernel(AdapterPool p, int chunk, const int* start, GradJob v, GradJob 
 // ------------------------------------------------------------------------------------------------ launches
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t round256(size_t v) { return (v + 255) & ~size_t(255); }
+
+constexpr int64_t kWideFill = 1024;                   // workgroups of wide_kernel
 
 // How thin_kernel is laid over b tokens, a reduction of K and the adapters.
 struct ThinPlan {
@@ -746,76 +901,87 @@ ThinPlan thin_plan(int64_t b, int64_t K, int slots, int max_rank) {
 }
 
 template <int NT, int MT, bool KMAJOR>
-void launch_thin_as(const ThinArgs& g, const ThinPlan& q, hipStream_t s) {
-    const dim3 grid((unsigned)ceil_div(g.p.b, 16 * MT), q.splits, q.lanes), block(64 * kThinWaves);
+void launch_thin_as(ThinArgs g, int extra, const ThinPlan& q, hipStream_t s) {
+    g.tiles = (int)ceil_div(g.p.b, 16 * MT);
+    const dim3 grid((unsigned)(g.tiles + extra), q.splits, q.lanes), block(64 * kThinWaves);
     if (!KMAJOR && g.drop.least)
         hipLaunchKernelGGL((thin_kernel<NT, MT, KMAJOR, !KMAJOR>), grid, block, 0, s, g);
     else
         hipLaunchKernelGGL((thin_kernel<NT, MT, KMAJOR, false>), grid, block, 0, s, g);
 }
 
+// extra: workgroups that write down the tokens by adapter.
 template <bool KMAJOR>
-hipError_t launch_thin(const ThinArgs& g, const ThinPlan& q, hipStream_t s) {
+hipError_t launch_thin(const ThinArgs& g, int extra, const ThinPlan& q, hipStream_t s) {
     const int R = g.p.max_rank;
     const bool big = q.mt > 1;
-    if (R <= 16) big ? launch_thin_as<1, 4, KMAJOR>(g, q, s) : launch_thin_as<1, 1, KMAJOR>(g, q, s);
-    else if (R <= 32) big ? launch_thin_as<2, 4, KMAJOR>(g, q, s) : launch_thin_as<2, 1, KMAJOR>(g, q, s);
-    else if (R <= 64) big ? launch_thin_as<4, 4, KMAJOR>(g, q, s) : launch_thin_as<4, 1, KMAJOR>(g, q, s);
-    else big ? launch_thin_as<8, 2, KMAJOR>(g, q, s) : launch_thin_as<8, 1, KMAJOR>(g, q, s);
+    if (R <= 16) big ? launch_thin_as<1, 4, KMAJOR>(g, extra, q, s) : launch_thin_as<1, 1, KMAJOR>(g, extra, q, s);
+    else if (R <= 32) big ? launch_thin_as<2, 4, KMAJOR>(g, extra, q, s) : launch_thin_as<2, 1, KMAJOR>(g, extra, q, s);
+    else if (R <= 64) big ? launch_thin_as<4, 4, KMAJOR>(g, extra, q, s) : launch_thin_as<4, 1, KMAJOR>(g, extra, q, s);
+    else big ? launch_thin_as<8, 2, KMAJOR>(g, extra, q, s) : launch_thin_as<8, 1, KMAJOR>(g, extra, q, s);
     return hipGetLastError();
 }
 
 template <int RC, int MT, bool BWD>
-void launch_wide_as(const WideArgs& g, int f32, int lanes, hipStream_t s) {
+void launch_wide_as(WideArgs g, int f32, int lanes, int64_t groups, hipStream_t s) {
     const int64_t wide = BWD ? g.p.m : g.p.n, tiles = ceil_div(g.p.b, 16 * MT);
-    const int64_t blocks = ceil_div(wide, (BWD ? 128 : 64) * kWideWaves);
-    // as many workgroups as fill the chip twice over, each with several blocks of features where there are more
-    int64_t y = ceil_div(2048, tiles * lanes);
+    const int64_t blocks = ceil_div(wide, 64 * kWideWaves);
+    // as many workgroups as fill the chip, each with several blocks of features where there are more
+    int64_t y = ceil_div(kWideFill, tiles * lanes);
     if (y > blocks) y = blocks;
     y = ceil_div(blocks, ceil_div(blocks, y));
-    const dim3 grid((unsigned)tiles, (unsigned)y, lanes), block(64 * kWideWaves);
+    g.tiles = (int)tiles;
+    const dim3 grid((unsigned)(tiles + ceil_div(groups, y)), (unsigned)y, lanes), block(64 * kWideWaves);
     if (f32) hipLaunchKernelGGL((wide_kernel<RC, MT, BWD, true>), grid, block, 0, s, g);
     else hipLaunchKernelGGL((wide_kernel<RC, MT, BWD, false>), grid, block, 0, s, g);
 }
 
+// groups: of 32 places, whose pieces are written in the same launch.
 template <bool BWD>
-hipError_t launch_wide(const WideArgs& g, int f32, int lanes, hipStream_t s) {
+hipError_t launch_wide(const WideArgs& g, int f32, int lanes, int64_t groups, hipStream_t s) {
     const int R = g.p.max_rank;
-    const bool big = g.p.b > 512;
-    if (R <= 16) big ? launch_wide_as<0, BWD ? 2 : 4, BWD>(g, f32, lanes, s) : launch_wide_as<0, 1, BWD>(g, f32, lanes, s);
-    else if (R <= 32) big ? launch_wide_as<1, BWD ? 2 : 4, BWD>(g, f32, lanes, s) : launch_wide_as<1, 1, BWD>(g, f32, lanes, s);
-    else if (R <= 64) big ? launch_wide_as<2, BWD ? 2 : 4, BWD>(g, f32, lanes, s) : launch_wide_as<2, 1, BWD>(g, f32, lanes, s);
-    else big ? launch_wide_as<4, 2, BWD>(g, f32, lanes, s) : launch_wide_as<4, 1, BWD>(g, f32, lanes, s);
+    const int64_t wide = BWD ? g.p.m : g.p.n;
+    const bool big = ceil_div(g.p.b, 64) * ceil_div(wide, 64 * kWideWaves) >= 512;
+    if (R <= 16) big ? launch_wide_as<0, 4, BWD>(g, f32, lanes, groups, s) : launch_wide_as<0, 1, BWD>(g, f32, lanes, groups, s);
+    else if (R <= 32) big ? launch_wide_as<1, 4, BWD>(g, f32, lanes, groups, s) : launch_wide_as<1, 1, BWD>(g, f32, lanes, groups, s);
+    else if (R <= 64) big ? launch_wide_as<2, 4, BWD>(g, f32, lanes, groups, s) : launch_wide_as<2, 1, BWD>(g, f32, lanes, groups, s);
+    else big ? launch_wide_as<4, 4, BWD>(g, f32, lanes, groups, s) : launch_wide_as<4, 1, BWD>(g, f32, lanes, groups, s);
     return hipGetLastError();
 }
 
-// Tokens between two cuts of the gradient sums: few enough that the column tiles fill the chip, so many that the partial sums stay small
+// Places between two cuts of the gradient sums: few enough that the column tiles fill the chip, so many that the partial sums stay small
 // next to what is read for them.
-int grad_chunk(int64_t b, int64_t m, int64_t n, int max_rank) {
+int grad_chunk(int64_t places, int64_t m, int64_t n, int max_rank) {
     const int64_t tiles = ceil_div(m, 128) + ceil_div(n, 128);
-    int64_t chunk = ceil_div(b * tiles, 1024), least = 8 * max_rank < 256 ? 256 : 8 * max_rank;
+    int64_t chunk = ceil_div(places * tiles, 1024), least = 8 * max_rank < 256 ? 256 : 8 * max_rank;
     if (chunk < least) chunk = least;
     return (int)(ceil_div(chunk, 128) * 128);
 }
 
 struct BwdLayout {
-    size_t part, thin, order, start, pieces, part_v, part_u, total;
-    int chunk, cuts;
+    size_t part, order, range, segments, small_v, small_u, part_v, part_u, total;
+    int64_t groups;          // of 32 places
+    int chunk, cuts, rank_tiles;
     ThinPlan plan;
 };
 
 BwdLayout bwd_layout(int64_t b, int64_t m, int64_t n, int slots, int R) {
     BwdLayout L;
+    const int64_t places = (b + 31) / 32 * 32 + 32 * (int64_t)slots;
+    L.groups = places / 32;
     L.plan = thin_plan(b, n, slots, R);
-    L.chunk = grad_chunk(b, m, n, R);
-    L.cuts = (int)ceil_div(b, L.chunk);
+    L.chunk = grad_chunk(places, m, n, R);
+    L.cuts = (int)ceil_div(places, L.chunk);
+    L.rank_tiles = (int)ceil_div(R, 16);
     size_t at = 0;
     const auto take = [&at](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
     L.part = take((size_t)L.plan.splits * b * R * 4);
-    L.thin = L.plan.splits > 1 ? take((size_t)b * R * 4) : L.part;
-    L.order = take((size_t)b * 4);
-    L.start = take(((size_t)slots + 1) * 4);
-    L.pieces = take(((size_t)slots + L.cuts) * sizeof(Piece));
+    L.order = take((size_t)places * 4);
+    L.range = take((size_t)slots * sizeof(int2));
+    L.segments = take(((size_t)slots + L.cuts) * sizeof(Segment));
+    const size_t small = (size_t)L.groups * L.rank_tiles * 3 * 64 * sizeof(v4u);
+    L.small_v = take(small);
+    L.small_u = take(small);
     const size_t parts = L.cuts > 1 ? 2 * (size_t)L.cuts + 1 : 0;
     L.part_v = take(parts * n * R * 4);
     L.part_u = take(parts * m * R * 4);
@@ -838,9 +1004,14 @@ hipError_t launch_adapters_fwd(const AdaptersFwd& a, hipStream_t s) {
     const AdapterPool& p = a.pool;
     const ThinPlan q = thin_plan(p.b, p.m, p.slots, p.max_rank);
     float* part = q.splits > 1 ? reinterpret_cast<float*>(a.workspace) : a.T;
-    hipError_t e = launch_thin<false>(ThinArgs{p, a.X, a.ld_x, part, a.drop}, q, s);
+    ThinArgs t{};
+    t.p = p; t.in = a.X; t.ld = a.ld_x; t.part = part; t.drop = a.drop;
+    const hipError_t e = launch_thin<false>(t, 0, q, s);
     if (e != hipSuccess) return e;
-    return launch_wide<false>(WideArgs{p, part, q.splits, a.T, a.base, a.ld_base, a.Y, a.ld_y, a.drop}, a.out_f32, q.lanes, s);
+    WideArgs w{};
+    w.p = p; w.part = part; w.splits = q.splits; w.thin = q.splits > 1 ? a.T : nullptr;
+    w.base = a.base; w.ld_base = a.ld_base; w.out = a.Y; w.ld_out = a.ld_y;
+    return launch_wide<false>(w, a.out_f32, q.lanes, 0, s);
 }
 
 hipError_t launch_adapters_bwd(const AdaptersBwd& a, hipStream_t s) {
@@ -848,35 +1019,49 @@ hipError_t launch_adapters_bwd(const AdaptersBwd& a, hipStream_t s) {
     const int64_t b = p.b;
     const BwdLayout L = bwd_layout(b, p.m, p.n, p.slots, p.max_rank);
     unsigned char* ws = reinterpret_cast<unsigned char*>(a.workspace);
-    float *part = reinterpret_cast<float*>(ws + L.part), *S = reinterpret_cast<float*>(ws + L.thin);
+    float* part = reinterpret_cast<float*>(ws + L.part);
+    const GroupArgs group{L.chunk, L.cuts, reinterpret_cast<int*>(ws + L.order), reinterpret_cast<int2*>(ws + L.range),
+                          reinterpret_cast<Segment*>(ws + L.segments)};
+    v4u* small[2] = {reinterpret_cast<v4u*>(ws + L.small_v), reinterpret_cast<v4u*>(ws + L.small_u)};
+    const bool grads = a.GU || a.GV, thin = b > 0 && (a.EX || a.GU);
     hipError_t e = hipSuccess;
-    if (b > 0 && (a.EX || a.GU)) {
-        e = launch_thin<true>(ThinArgs{p, a.E, a.ld_e, part, DropoutMask{}}, L.plan, s);
-        if (e != hipSuccess) return e;
+    // S, and the tokens by their adapters
+    if (thin) {
+        ThinArgs t{};
+        t.p = p; t.in = a.E; t.ld = a.ld_e; t.part = part; t.group = group;
+        e = launch_thin<true>(t, grads ? p.slots : 0, L.plan, s);
+    } else if (grads) {
+        hipLaunchKernelGGL(group_kernel, dim3(p.slots), dim3(512), 0, s, p, group);
+        e = hipGetLastError();
     }
+    if (e != hipSuccess) return e;
+    // E_X, and the pieces of T and S
+    PieceArgs pieces{};
+    pieces.b = b; pieces.groups = L.groups; pieces.R = p.max_rank; pieces.tiles = L.rank_tiles; pieces.order = group.order;
+    pieces.thin[0] = a.GV ? a.T : nullptr; pieces.splits[0] = 1; pieces.out[0] = small[0];
+    pieces.thin[1] = a.GU ? part : nullptr; pieces.splits[1] = L.plan.splits; pieces.out[1] = small[1];
     if (b > 0 && a.EX) {
-        e = launch_wide<true>(WideArgs{p, part, L.plan.splits, S, a.base, a.ld_base, a.EX, a.ld_ex, a.drop}, a.out_f32, L.plan.lanes, s);
-        if (e != hipSuccess) return e;
-    } else if (b > 0 && a.GU && L.plan.splits > 1) {
-        const int64_t total = b * p.max_rank;
-        hipLaunchKernelGGL(thin_join_kernel, dim3((unsigned)ceil_div(total, 1024)), dim3(256), 0, s, part, L.plan.splits, total, S);
+        WideArgs w{};
+        w.p = p; w.part = part; w.splits = L.plan.splits;
+        w.base = a.base; w.ld_base = a.ld_base; w.out = a.EX; w.ld_out = a.ld_ex; w.drop = a.drop; w.pieces = pieces;
+        e = launch_wide<true>(w, a.out_f32, L.plan.lanes, grads ? L.groups : 0, s);
+    } else if (grads) {
+        hipLaunchKernelGGL(pieces_kernel, dim3((unsigned)L.groups), dim3(256), 0, s, pieces);
+        e = hipGetLastError();
     }
-    if (!a.GU && !a.GV) return hipGetLastError();
-    int *order = reinterpret_cast<int*>(ws + L.order), *start = reinterpret_cast<int*>(ws + L.start);
-    Piece* pieces = reinterpret_cast<Piece*>(ws + L.pieces);
-    hipLaunchKernelGGL(group_kernel, dim3(p.slots), dim3(kGroupThreads), 0, s, p, L.chunk, order, start, pieces);
+    if (e != hipSuccess || !grads) return e;
     GradArgs g{};
-    g.p = p; g.order = order; g.pieces = pieces; g.drop = a.drop;
-    if (a.GV) g.job[0] = GradJob{a.E, a.ld_e, a.T, a.GV, reinterpret_cast<float*>(ws + L.part_v), p.n, (int)ceil_div(p.n, 128), 0};
-    if (a.GU) g.job[1] = GradJob{a.X, a.ld_x, S, a.GU, reinterpret_cast<float*>(ws + L.part_u), p.m, (int)ceil_div(p.m, 128), 1};
-    const int R = p.max_rank, nt = R <= 16 ? 1 : R <= 32 ? 2 : 4;
-    const dim3 grid(g.job[0].tiles + g.job[1].tiles, p.slots + L.cuts, (unsigned)ceil_div(R, 16 * nt)), block(64 * kGradWaves);
+    g.p = p; g.order = group.order; g.segments = group.segments; g.rank_tiles = L.rank_tiles; g.drop = a.drop;
+    if (a.GV) g.job[0] = GradJob{a.E, a.ld_e, small[0], a.GV, reinterpret_cast<float*>(ws + L.part_v), p.n, (int)ceil_div(p.n, 128), 0};
+    if (a.GU) g.job[1] = GradJob{a.X, a.ld_x, small[1], a.GU, reinterpret_cast<float*>(ws + L.part_u), p.m, (int)ceil_div(p.m, 128), 1};
+    const int nt = L.rank_tiles <= 1 ? 1 : L.rank_tiles <= 2 ? 2 : 4;
+    const dim3 grid(g.job[0].tiles + g.job[1].tiles, p.slots + L.cuts, (unsigned)ceil_div(L.rank_tiles, nt)), block(64 * kGradWaves);
     if (nt == 1) hipLaunchKernelGGL(grad_kernel<1>, grid, block, 0, s, g);
     else if (nt == 2) hipLaunchKernelGGL(grad_kernel<2>, grid, block, 0, s, g);
     else hipLaunchKernelGGL(grad_kernel<4>, grid, block, 0, s, g);
     if (L.cuts > 1) {
-        const int64_t size = ((a.GV ? p.n : 0) + (a.GU ? p.m : 0)) * R;
-        hipLaunchKernelGGL(grad_join_kernel, dim3((unsigned)ceil_div(size, 1024), p.slots), dim3(256), 0, s, p, L.chunk, start, g.job[0], g.job[1]);
+        const int64_t size = ((a.GV ? p.n : 0) + (a.GU ? p.m : 0)) * p.max_rank;
+        hipLaunchKernelGGL(grad_join_kernel, dim3((unsigned)ceil_div(size, 1024), p.slots), dim3(256), 0, s, p, group, g.job[0], g.job[1]);
     }
     return hipGetLastError();
 }
