@@ -437,7 +437,7 @@ pieces_kernel(PieceArgs g) { write_pieces(g, blockIdx.x); }
 // lanes hold them, split in pieces.  Its wavefronts go over blocks of features, the rows: 64 with 16-byte loads of V, or 64 columns of U,
 // loaded four neighbouring columns of eight rank rows at a time and packed, so that instruction v covers the columns 4 i + v.  Either way a
 // lane ends up with runs of eight neighbouring features of one token: 16-byte loads of base and stores.  The next block's adapter values and
-// the next token tile's base are on their way while one is worked on.
+// base are on their way while one is worked on.
 // RC: rank chunks of 32.  RC == 0 (rank up to 16): the halves of the instruction's 32 products hold the pieces (high, middle) and (low,
 // nothing), two instructions instead of three.
 constexpr int kWideWaves = 4;
@@ -520,7 +520,11 @@ wide_kernel(WideArgs g) {
     __syncthreads();
     TileAdapters tile(p, s_id[lane], lane < ROWS);
     const uint64_t bare = __ballot(lane < ROWS && row0 + lane < p.b) & ~tile.todo;
-    const int64_t f_first = ((int64_t)blockIdx.y * kWideWaves + wave) * FB, f_step = (int64_t)gridDim.y * kWideWaves * FB;
+    // This workgroup's strips of features, one block per wavefront each: a range of them, begun at another one by every tile of tokens.
+    const int strips = (int)((wide + FB * kWideWaves - 1) / (FB * kWideWaves)), per = (strips + (int)gridDim.y - 1) / (int)gridDim.y;
+    const int strip0 = (int)blockIdx.y * per, count = strips - strip0 < per ? strips - strip0 : per;     // count > 0
+    const int turn = (int)(blockIdx.x % (unsigned)count);
+    const auto block_at = [&](int j) { return ((int64_t)(strip0 + (j + turn < count ? j + turn : j + turn - count)) * kWideWaves + wave) * FB; };
     const int r_lane = STACK ? 8 * (kg & 1) : 8 * kg;
 
     // the work of this wavefront: the blocks of features for one adapter after the other
@@ -618,7 +622,7 @@ wide_kernel(WideArgs g) {
 
     next_adapter();
     Block now;
-    if (a >= 0 && f_first < wide) now.load(p, a, wide, f_first, lr, r_lane);
+    if (a >= 0) now.load(p, a, wide, block_at(0), lr, r_lane);
 
     // the thin values of the tile's tokens, in pieces
     for (int j = wave; j < MT * RC; j += kWideWaves) {
@@ -655,8 +659,8 @@ wide_kernel(WideArgs g) {
     if (blockIdx.z == 0 && g.base != g.out) {            // tokens without an adapter: the base as it is
         for (uint64_t todo = bare; todo; todo &= todo - 1) {
             const int64_t t = row0 + __builtin_ctzll(todo);
-            for (int64_t f0 = f_first; f0 < wide; f0 += f_step) {
-                const int64_t f = f0 + 8 * lane;
+            for (int j = 0; j < count; ++j) {
+                const int64_t f = block_at(j) + 8 * lane;
                 if (8 * lane >= FB || f >= wide) continue;
                 BaseEight<F32> x;
                 float y[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
@@ -667,17 +671,18 @@ wide_kernel(WideArgs g) {
     }
 
     for (; a >= 0; next_adapter()) {
-        if (f_first >= wide) continue;
-        if (seen > 1 + blockIdx.z) now.load(p, a, wide, f_first, lr, r_lane);       // not the first adapter of this wavefront
-        for (int64_t f0 = f_first; f0 < wide; f0 += f_step) {
+        if (seen > 1 + blockIdx.z) now.load(p, a, wide, block_at(0), lr, r_lane);    // not the first adapter of this wavefront
+        BaseEight<F32> base[MT][NQ];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) load_base(base[i], i, block_at(0));
+#pragma unroll 1
+        for (int j = 0; j < count; ++j) {
+            const int64_t f0 = block_at(j), f1 = block_at(j + 1 < count ? j + 1 : j);
             now.finish(rank, r_lane);
             Block ahead;
-            if (AHEAD && f0 + f_step < wide) ahead.load(p, a, wide, f0 + f_step, lr, r_lane);
-            BaseEight<F32> base[NQ], base_ahead[NQ];
-            load_base(base, 0, f0);
-#pragma unroll 1
+            if (AHEAD && j + 1 < count) ahead.load(p, a, wide, f1, lr, r_lane);
+#pragma unroll
             for (int i = 0; i < MT; ++i) {
-                if (i + 1 < MT) load_base(base_ahead, i + 1, f0);
                 if ((mine >> (i * 16)) & 0xFFFF) {
                     v4f acc[4];
 #pragma unroll
@@ -698,22 +703,22 @@ wide_kernel(WideArgs g) {
                             if (f >= wide) continue;
                             float y[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) y[j] = BWD ? acc[j & 3][2 * q + (j >> 2)] : acc[2 * q + (j >> 2)][j & 3];
+                            for (int e = 0; e < 8; ++e) y[e] = BWD ? acc[e & 3][2 * q + (e >> 2)] : acc[2 * q + (e >> 2)][e & 3];
                             if (BWD && g.drop.least) {
                                 const uint4 bits = dropout_bits(g.drop, (uint32_t)t, (uint32_t)(f >> 3));
 #pragma unroll
-                                for (int j = 0; j < 8; ++j) y[j] = dropout_kept(g.drop, bits, j) ? y[j] * g.drop.factor : 0.0f;
+                                for (int e = 0; e < 8; ++e) y[e] = dropout_kept(g.drop, bits, e) ? y[e] * g.drop.factor : 0.0f;
                             }
-                            if (g.base) base[q].add(y);
+                            if (g.base) base[i][q].add(y);
                             store_eight<F32>(g.out, t * g.ld_out + f, y);
                         }
                     }
+                    if (j + 1 < count) load_base(base[i], i, f1);
                 }
-#pragma unroll
-                for (int q = 0; q < NQ; ++q) base[q] = base_ahead[q];
+                __builtin_amdgcn_sched_barrier(0);       // one token tile's values in registers at a time
             }
             if (AHEAD) now = ahead;
-            else if (f0 + f_step < wide) now.load(p, a, wide, f0 + f_step, lr, r_lane);
+            else if (j + 1 < count) now.load(p, a, wide, f1, lr, r_lane);
         }
     }
 }
