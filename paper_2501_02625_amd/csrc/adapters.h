@@ -51,7 +51,7 @@ struct AdaptersBwd {
 };
 
 size_t adapters_fwd_workspace(int64_t b, int64_t m, int64_t n, int slots, int max_rank);
-size_t adapters_bwd_workspace(int64_t b, int64_t m, int64_t n, int slots, int max_rank);
+size_t adapters_bwd_workspace(int64_t b, int64_t m, int64_t n, int slots, int max_rank, bool drop);
 hipError_t launch_adapters_fwd(const AdaptersFwd& a, hipStream_t s);
 hipError_t launch_adapters_bwd(const AdaptersBwd& a, hipStream_t s);
 

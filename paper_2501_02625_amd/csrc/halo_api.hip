@@ -989,7 +989,8 @@ size_t halo_adapters_fwd_workspace_bytes(const halo_adapters_desc* desc) {
 }
 
 size_t halo_adapters_bwd_workspace_bytes(const halo_adapters_desc* desc) {
-    return check_adapters(desc) == HALO_OK ? adapters_bwd_workspace(desc->b, desc->m, desc->n, desc->slots, desc->max_rank) : 0;
+    return check_adapters(desc) == HALO_OK
+               ? adapters_bwd_workspace(desc->b, desc->m, desc->n, desc->slots, desc->max_rank, desc->dropout_p > 0.0) : 0;
 }
 
 halo_status halo_adapters_fwd(const halo_adapters_desc* desc, const void* X, int64_t ld_x, const void* U, const void* V,
@@ -1040,7 +1041,7 @@ halo_status halo_adapters_bwd(const halo_adapters_desc* desc, const void* E, int
     if (!aligned16(E) || !aligned16(X) || !aligned16(T) || !aligned16(U) || !aligned16(V) || !aligned16(base) || !aligned16(EX) ||
         !aligned16(GU) || !aligned16(GV) || !aligned4(ranks) || !aligned4(scale) || !aligned4(adapter_of))
         return HALO_EALIGN;
-    const size_t need = adapters_bwd_workspace(b, m, n, desc->slots, desc->max_rank);
+    const size_t need = halo_adapters_bwd_workspace_bytes(desc);
     if (need && (!workspace || workspace_bytes < need)) return HALO_EWORKSPACE;
     if (need && !aligned16(workspace)) return HALO_EALIGN;
     AdaptersBwd a{};
