@@ -90,6 +90,9 @@ __device__ __forceinline__ uint2 keep_four(uint2 x, uint32_t kept) {
     return make_uint2(x.x & pack_lo(bit(0), bit(1)), x.y & pack_lo(bit(2), bit(3)));
 }
 
+// Nothing is moved across: loads stay ahead of what would otherwise be drawn in front of them, or pushed behind, to save registers.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
 // The wavefront's place in its workgroup, in a scalar register: what is decided by it is decided for the wavefront.
 __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
@@ -490,11 +493,21 @@ thin_rows_kernel(ThinArgs g) {
                 for (int h = 0; h < 4; ++h)
                     if (k0 + h * 32 + kg * 8 >= (uint32_t)K) x[h] = v4u{0, 0, 0, 0};
             }
+            v4u q[2][NT];                                // one instruction's operands while the other's are multiplied
+            const int slot = operand_slot(lr, kg);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) q[0][t] = s_b[j & 1][0][t][slot];
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
+                if (h < 3) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) q[(h + 1) & 1][t] = s_b[j & 1][h + 1][t][slot];
+                }
+                in_order();
                 if (DROP) x[h] = drop_eight(g.drop, x[h], token, ((k0 + h * 32) >> 3) + kg);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[t] = mfma(x[h], s_b[j & 1][h][t][operand_slot(lr, kg)], acc[t]);
+                for (int t = 0; t < NT; ++t) acc[t] = mfma(x[h], q[h & 1][t], acc[t]);
+                in_order();
             }
         };
         // Step j: the adapter's part, on its way since the step before, goes to LDS, that of the next step is asked for, and the rows of the
@@ -507,7 +520,8 @@ thin_rows_kernel(ThinArgs g) {
             load_x(x, j + 2 < count ? j + 2 : j);
         };
         __syncthreads();                                 // the adapter before may still be read
-        load_staged(0);
+        load_staged(0);                                  // first: it is waited for first
+        in_order();
         load_x(x[0], 0);
         load_x(x[1], count > 1 ? 1 : 0);
 #pragma unroll 1
@@ -519,9 +533,14 @@ thin_rows_kernel(ThinArgs g) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][e] = t * 16 + lr < rank ? acc[t][e] * factor : 0.0f;
+        in_order();                                      // what is loaded for it is waited for here, not again at each of the stores
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = wave * 16 + 4 * kg + e, c = t * 16 + lr;
-                if (((mine >> r) & 1) && c < R) part[(row0 + r) * R + c] = c < rank ? acc[t][e] * factor : 0.0f;
+                if (((mine >> r) & 1) && c < R) part[(row0 + r) * R + c] = acc[t][e];
             }
     }
 }
@@ -1039,14 +1058,21 @@ wide_tall_kernel(WideArgs g) {
             v4f acc[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) acc[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            v4u b[2][NP];                                // one rank chunk's operands while the other's are multiplied
 #pragma unroll
-            for (int c = 0; c < RC; ++c)
+            for (int k = 0; k < NP; ++k) b[0][k] = s_thin[i * RC * NP + k][lane];
 #pragma unroll
-                for (int k = 0; k < NP; ++k) {
-                    const v4u b = s_thin[(i * RC + c) * NP + k][lane];
+            for (int c = 0; c < RC; ++c) {
+                if (c + 1 < RC) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[e] = mfma(now.w[c][e], b, acc[e]);
+                    for (int k = 0; k < NP; ++k) b[(c + 1) & 1][k] = s_thin[(i * RC + c + 1) * NP + k][lane];
                 }
+                in_order();
+#pragma unroll
+                for (int k = 0; k < NP; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[e] = mfma(now.w[c][e], b[c & 1][k], acc[e]);
+            }
             if (!((own >> i) & 1)) return;
             const int64_t t = row0 + i * 16 + lr, f0 = f_of(q.j);
 #pragma unroll
@@ -1198,14 +1224,22 @@ grad_kernel(GradArgs g) {
             a[2][e] = pack_lo(x[2 * e].y, x[2 * e + 1].y);
             a[3][e] = pack_hi(x[2 * e].y, x[2 * e + 1].y);
         }
+        v4u b[2][3];                                     // one rank tile's operands while the other's are multiplied
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int k = 0; k < 3; ++k) b[0][k] = s_small[j & 1][k * 64 + lane];
 #pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                const v4u b = s_small[j & 1][(t * 3 + k) * 64 + lane];
+        for (int t = 0; t < NT; ++t) {
+            if (t + 1 < NT) {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[t][v] = mfma(a[v], b, acc[t][v]);
+                for (int k = 0; k < 3; ++k) b[(t + 1) & 1][k] = s_small[j & 1][((t + 1) * 3 + k) * 64 + lane];
             }
+            in_order();
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[t][v] = mfma(a[v], b[t & 1][k], acc[t][v]);
+            in_order();
+        }
     };
     int token[8];                                        // of the step whose rows are asked for next
     Step even, odd;
@@ -1218,19 +1252,20 @@ grad_kernel(GradArgs g) {
         __syncthreads();
         load_staged(j + 1);
         multiply(q, j);
-        int next[8];
-        load_order(next, j + 3);
         load_rows(q, token);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) token[u] = next[u];
+        load_order(token, j + 3);
+        in_order();
     };
     if (steps > 0) {                                     // the same for the workgroup
         load_order(token, 0);
         load_staged(0);
+        in_order();
         load_rows(even, token);
         load_order(token, 1);
+        in_order();
         load_rows(odd, token);
         load_order(token, 2);
+        in_order();
 #pragma unroll 1
         for (int j = 0; j < steps; j += 2) {
             step(even, j);
@@ -1240,22 +1275,26 @@ grad_kernel(GradArgs g) {
     const int rank = rank_of(p, seg.adapter);
     const float factor = second ? (masked ? g.drop.factor : 1.0f) : scale_of(p, seg.adapter);
     float* dst = seg.part < 0 ? job.out + (int64_t)seg.adapter * wide * R : job.part + (int64_t)seg.part * wide * R;
+    const bool rank_major = job.rank_major != 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][v][e] = (tile0 + t) * 16 + i16 < rank ? acc[t][v][e] * factor : 0.0f;
+    in_order();                                          // what is loaded for it is waited for here, not again at each of the stores
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int c = (tile0 + t) * 16 + i16;
-        if (c >= R) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int64_t oc = c0 + 4 * (4 * kq + e);
-            if (oc >= wide) continue;
-            float o[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) o[v] = c < rank ? acc[t][v][e] * factor : 0.0f;
-            if (job.rank_major) {
-                *reinterpret_cast<v4f*>(dst + (int64_t)c * wide + oc) = v4f{o[0], o[1], o[2], o[3]};
+            if (oc >= wide || c >= R) continue;
+            if (rank_major) {
+                *reinterpret_cast<v4f*>(dst + (int64_t)c * wide + oc) = v4f{acc[t][0][e], acc[t][1][e], acc[t][2][e], acc[t][3][e]};
             } else {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) dst[(oc + v) * R + c] = o[v];
+                for (int v = 0; v < 4; ++v) dst[(oc + v) * R + c] = acc[t][v][e];
             }
         }
     }
