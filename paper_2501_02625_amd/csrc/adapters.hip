@@ -645,12 +645,12 @@ struct WideArgs {
     PieceArgs pieces;
 };
 
-// The mask of dropout on eight neighbouring elements of row t.
-__device__ __forceinline__ void drop_run(const WideArgs& g, int64_t t, int64_t f, float (&y)[8]) {
-    const uint32_t kept = kept_eight(g.drop, (uint32_t)t, (uint32_t)(f >> 3));
+// The mask of dropout on eight neighbouring elements of row t; returns its bits.
+__device__ __forceinline__ uint32_t drop_run(const DropoutMask& d, int64_t t, int64_t f, float (&y)[8]) {
+    const uint32_t kept = kept_eight(d, (uint32_t)t, (uint32_t)(f >> 3));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = (kept >> e) & 1 ? y[e] * g.drop.factor : 0.0f;
-    if (g.kept) g.kept[t * (g.p.m >> 3) + (f >> 3)] = (uint8_t)kept;
+    for (int e = 0; e < 8; ++e) y[e] = (kept >> e) & 1 ? y[e] * d.factor : 0.0f;
+    return kept;
 }
 
 // Two values rounded to bf16, side by side.
@@ -660,7 +660,7 @@ __device__ __forceinline__ uint32_t round_two(float x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{x, y}, v2bf));
 }
 
-// Eight neighbouring elements of base, as they are in memory.
+// Eight neighbouring elements of base or result, as they are in memory.
 template <bool F32>
 struct BaseEight {
     v4u q[F32 ? 2 : 1];
@@ -668,6 +668,11 @@ struct BaseEight {
         const v4u* s = reinterpret_cast<const v4u*>(reinterpret_cast<const char*>(base) + at * (F32 ? 4 : 2));
         q[0] = s[0];
         if constexpr (F32) q[1] = s[1];
+    }
+    __device__ __forceinline__ void store(void* out, int64_t at) const {
+        v4u* o = reinterpret_cast<v4u*>(reinterpret_cast<char*>(out) + at * (F32 ? 4 : 2));
+        o[0] = q[0];
+        if constexpr (F32) o[1] = q[1];
     }
     // keep: all ones, or 0 for nothing
     __device__ __forceinline__ void add(float (&y)[8], uint32_t keep = ~0u) const {
@@ -682,20 +687,33 @@ struct BaseEight {
             }
         }
     }
+    __device__ __forceinline__ void set(const float (&y)[8]) {
+        if constexpr (F32) {
+            q[0] = __builtin_bit_cast(v4u, v4f{y[0], y[1], y[2], y[3]});
+            q[1] = __builtin_bit_cast(v4u, v4f{y[4], y[5], y[6], y[7]});
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) q[0][j] = round_two(y[2 * j], y[2 * j + 1]);
+        }
+    }
+    // Of (this, other): even lanes keep this one and odd lanes the other; what they do not keep changes place with the neighbour's.
+    __device__ __forceinline__ void exchange(BaseEight& other, bool odd) {
+#pragma unroll
+        for (int i = 0; i < (F32 ? 2 : 1); ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t give = odd ? q[i][j] : other.q[i][j];
+                const uint32_t got = (uint32_t)__builtin_amdgcn_mov_dpp((int)give, 0xB1, 0xF, 0xF, true);   // quad_perm [1,0,3,2]
+                q[i][j] = odd ? got : q[i][j];
+                other.q[i][j] = odd ? other.q[i][j] : got;
+            }
+    }
 };
 template <bool F32>
 __device__ __forceinline__ void store_eight(void* out, int64_t at, const float (&y)[8]) {
-    v4u* o = reinterpret_cast<v4u*>(reinterpret_cast<char*>(out) + at * (F32 ? 4 : 2));
-    if constexpr (F32) {
-        o[0] = __builtin_bit_cast(v4u, v4f{y[0], y[1], y[2], y[3]});
-        o[1] = __builtin_bit_cast(v4u, v4f{y[4], y[5], y[6], y[7]});
-    } else {
-        v4u w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            w[j] = round_two(y[2 * j], y[2 * j + 1]);
-        o[0] = w;
-    }
+    BaseEight<F32> x;
+    x.set(y);
+    x.store(out, at);
 }
 
 // A block of 64 features of an adapter, the first operand of the matrix instructions: 16-byte loads of V, or four neighbouring columns of eight
@@ -914,7 +932,10 @@ wide_kernel(WideArgs g) {
                             float y[8];
 #pragma unroll
                             for (int e = 0; e < 8; ++e) y[e] = Block::result(acc, q, e);
-                            if (BWD && g.drop.least) drop_run(g, t, f, y);
+                            if (BWD && g.drop.least) {
+                                const uint32_t kept = drop_run(g.drop, t, f, y);
+                                if (g.kept) g.kept[t * (wide >> 3) + (f >> 3)] = (uint8_t)kept;
+                            }
                             if (g.base) base[i][q].add(y);
                             store_eight<F32>(g.out, t * g.ld_out + f, y);
                         }
@@ -953,6 +974,8 @@ wide_tall_kernel(WideArgs g) {
     const int64_t wide = BWD ? p.m : p.n;
     const int64_t row0 = (int64_t)blockIdx.x * ROWS;
     typedef AdapterBlock<RC_, BWD> Block;
+    const bool odd = lr & 1;
+    const int pair = lr & 14, run = Block::run(kg, lr & 1);
     for (int r = tid; r < ROWS; r += 64 * kTallWaves) s_id[r] = row0 + r < p.b ? p.adapter_of[row0 + r] : -1;
     __syncthreads();
     const int r_lane = STACK ? 8 * (kg & 1) : 8 * kg;
@@ -1023,7 +1046,7 @@ wide_tall_kernel(WideArgs g) {
             if (todo[w]) first = w * 64 + __builtin_ctzll(todo[w]);
         if (first < 0) break;
         const int a = __builtin_amdgcn_readfirstlane(s_id[first]), rank = rank_of(p, a);
-        uint32_t own = 0, steps = 0;                     // bit i: the lane's token of step i is a's; any token of step i is
+        uint32_t own[2] = {0, 0}, steps = 0;             // bit i: the even (odd) token of the lane's pair in step i is a's; any of the step is
 #pragma unroll
         for (int w = 0; w < WORDS; ++w) {
             const uint64_t mine = __ballot(s_id[w * 64 + lane] == a) & todo[w];
@@ -1031,7 +1054,8 @@ wide_tall_kernel(WideArgs g) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t sixteen = (uint32_t)(mine >> (16 * i)) & 0xFFFFu;
-                own |= ((sixteen >> lr) & 1u) << (4 * w + i);
+                own[0] |= ((sixteen >> pair) & 1u) << (4 * w + i);
+                own[1] |= ((sixteen >> (pair + 1)) & 1u) << (4 * w + i);
                 steps |= (sixteen ? 1u : 0u) << (4 * w + i);
             }
         }
@@ -1041,15 +1065,16 @@ wide_tall_kernel(WideArgs g) {
             if (!q.left) { ++q.j; q.left = steps; }
             return q;
         };
+        // Base and result go a pair of tokens at a time: lane (i, g) has run i % 2 of the even token, then of the odd one, so that eight lanes
+        // take 128 bytes of a row at once.  (Token by token, each half of a line was a request of its own.)
         BaseEight<F32> base[DEPTH][2];
         const auto load_base = [&](BaseEight<F32> (&x)[2], const Place& q) {
             const int i = __builtin_ctz(q.left);
-            const int64_t t = row0 + ((own >> i) & 1 ? i * 16 + lr : first);     // other adapters' tokens: one of this one's
-            const int64_t f0 = f_of(q.j < count ? q.j : 0);
+            const int64_t f = f_of(q.j < count ? q.j : 0) + run;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int64_t f = f0 + Block::run(kg, k);
-                x[k].load(base_at, t * base_ld + (f < wide ? f : 0));
+            for (int k = 0; k < 2; ++k) {                // other adapters' tokens, features beyond: the first of this one's
+                const bool ok = (own[k] >> i) & 1 && f < wide;
+                x[k].load(base_at, (row0 + (ok ? i * 16 + pair + k : first)) * base_ld + (ok ? f : 0));
             }
         };
         Block now, ahead;
@@ -1073,19 +1098,26 @@ wide_tall_kernel(WideArgs g) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[e] = mfma(now.w[c][e], b[c & 1][k], acc[e]);
             }
-            if (!((own >> i) & 1)) return;
-            const int64_t t = row0 + i * 16 + lr, f0 = f_of(q.j);
+            x[0].exchange(x[1], odd);
+            BaseEight<F32> y[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const int64_t f = f0 + Block::run(kg, k);
-                if (f >= wide) continue;
-                float y[8];
+                float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = Block::result(acc, k, e);
-                if (BWD && g.drop.least) drop_run(g, t, f, y);
-                x[k].add(y, base_keep);
-                store_eight<F32>(g.out, t * g.ld_out + f, y);
+                for (int e = 0; e < 8; ++e) v[e] = Block::result(acc, k, e);
+                if (BWD && g.drop.least) {
+                    const int64_t f = f_of(q.j) + Block::run(kg, k);
+                    const uint32_t kept = drop_run(g.drop, row0 + i * 16 + lr, f, v);
+                    if (g.kept && (own[lr & 1] >> i) & 1 && f < wide) g.kept[(row0 + i * 16 + lr) * (wide >> 3) + (f >> 3)] = (uint8_t)kept;
+                }
+                x[k].add(v, base_keep);
+                y[k].set(v);
             }
+            y[0].exchange(y[1], odd);
+            const int64_t f = f_of(q.j) + run;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if ((own[k] >> i) & 1 && f < wide) y[k].store(g.out, (row0 + i * 16 + pair + k) * g.ld_out + f);
         };
         Place at{0, steps}, next = at;
         now.load(p, a, wide, f_of(0), lr, r_lane);
