@@ -18,7 +18,7 @@ NATIVE_PATH = os.path.join(PKG_DIR, "_halo_native.so")
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 
 SOURCES = ["halo_api.hip", "row_transform.hip", "col_ops.hip", "gemm_i8.hip", "gemm_mx6.hip", "row_kron.hip", "lowrank.hip",
-           "adapters.hip", "dropout.hip"]
+           "adapters.hip", "adapters_thin.hip", "adapters_wide.hip", "adapters_grad.hip", "dropout.hip"]
 
 # -ffp-contract=off: every fp32 add/mul of the rotation and the quantiser is rounded on its own, which is
 # what makes the INT8 codes reproducible bit for bit.  Packed fp32 instructions are switched off.

@@ -1,0 +1,232 @@
+// What the kernels of the low-rank adapters share (adapters_thin.hip, adapters_wide.hip, adapters_grad.hip).
+//
+// Token t has the adapter a = adapter_of[t] with U_a [rank x m], V_a [n x rank] and the scale s_a:
+//   T = drop(X) U_a^T        Y = base + s_a T V_a^T
+//   S = s_a E V_a            E_X = base + drop'(S U_a)       G_U = sum over a's tokens of S_t drop(X)_t       G_V = s_a sum of E_t T_t
+// All matrices but T, S and the gradients are bf16; bf16 matrix instructions accumulate in fp32.  T and S stay fp32: where they are
+// operands they are split exactly into three bf16 pieces, so the sums are those of fp32 products.
+//
+// The kernels of T, S, Y and E_X take tiles of tokens as they lie; a tile is worked on once for each different adapter among its tokens, so
+// tokens may come in any order and nothing has to be sorted.  The gradients' kernel takes the tokens adapter by adapter, in an order that is
+// written down first.  No two adapters meet in one accumulator: what one holds (infinities, NaN) reaches its own tokens only.
+//
+// v_mfma_f32_16x16x32_bf16: lane l supplies row (first operand) or column (second) l % 16, elements 8 (l / 16) .. + 8 of the 32 that are
+// summed over; result lane l holds column l % 16, rows 4 (l / 16) .. + 4.
+//
+// Loads wait in the order in which they were issued, and where a load may or may not have been issued the compiler waits for all before it.  So
+// loads ahead of use always happen, at a place that is clamped to one that exists, and never move from register to register.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "adapters.h"
+
+namespace halo {
+namespace adapters {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint16_t v2us __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ v4f mfma(v4u a, v4u b, v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+
+// (high half of y) << 16 | (high half of x), and the same for the low halves.
+__device__ __forceinline__ uint32_t pack_hi(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); }
+__device__ __forceinline__ uint32_t pack_lo(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05040100u); }
+
+// Eight rows of four neighbouring bf16 values, two dwords each, become four columns of eight.
+__device__ __forceinline__ void columns_of(const uint2 (&x)[8], v4u (&y)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        y[0][e] = pack_lo(x[2 * e].x, x[2 * e + 1].x);
+        y[1][e] = pack_hi(x[2 * e].x, x[2 * e + 1].x);
+        y[2][e] = pack_lo(x[2 * e].y, x[2 * e + 1].y);
+        y[3][e] = pack_hi(x[2 * e].y, x[2 * e + 1].y);
+    }
+}
+
+// x = hi + mid + lo exactly, each piece an fp32 value whose low 16 bits are zero (a bf16): the mantissa's top 8 bits, the next 8, the
+// last 8.  An infinity is its own top piece.
+__device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+    hi = __float_as_uint(x) & 0xFFFF0000u;
+    const float h = __uint_as_float(hi), r = h == x ? 0.0f : x - h;
+    mid = __float_as_uint(r) & 0xFFFF0000u;
+    lo = __float_as_uint(r - __uint_as_float(mid));
+}
+
+// The three pieces of eight values, as operands.
+__device__ __forceinline__ void split_eight(const float (&x)[8], v4u (&q)[3]) {
+    uint32_t piece[3][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) split3(x[e], piece[0][e], piece[1][e], piece[2][e]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        q[k] = v4u{pack_hi(piece[k][0], piece[k][1]), pack_hi(piece[k][2], piece[k][3]), pack_hi(piece[k][4], piece[k][5]),
+                   pack_hi(piece[k][6], piece[k][7])};
+}
+
+// Loads at a 32-bit byte offset from an address that is the same for the wavefront: one register of address.
+template <typename V>
+__device__ __forceinline__ V load_at(const void* base, uint32_t offset) {
+    return *reinterpret_cast<const V*>(reinterpret_cast<const char*>(base) + offset);
+}
+
+__device__ __forceinline__ bool is_adapter(const AdapterPool& p, int a) { return (unsigned)a < (unsigned)p.slots; }
+__device__ __forceinline__ int rank_of(const AdapterPool& p, int a) {
+    if (!p.ranks) return p.max_rank;
+    const int r = p.ranks[a];
+    return r < 0 ? 0 : r > p.max_rank ? p.max_rank : r;
+}
+__device__ __forceinline__ float scale_of(const AdapterPool& p, int a) { return p.scale ? p.scale[a] : 1.0f; }
+
+// Of two random 16-bit halves: 1 where they are at least `least` (saturating difference to least - 1, at most 1).
+__device__ __forceinline__ v2us kept_pair(uint32_t bits, uint32_t least) {
+    const uint16_t below = (uint16_t)(least - 1);
+    return __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(v2us, bits), v2us{below, below}), v2us{1, 1});
+}
+
+// Eight bf16 values with the dropped ones set to zero.
+__device__ __forceinline__ v4u drop_eight(const DropoutMask& d, v4u x, uint32_t row, uint32_t group) {
+    const uint4 q = dropout_bits(d, row, group);
+    const uint32_t bits[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] &= __builtin_bit_cast(uint32_t, (v2us)(v2us{0, 0} - kept_pair(bits[i], d.least)));
+    return x;
+}
+
+// Which of eight elements are kept, a bit each.
+__device__ __forceinline__ uint32_t kept_eight(const DropoutMask& d, uint32_t row, uint32_t group) {
+    const uint4 q = dropout_bits(d, row, group);
+    const uint32_t bits[4] = {q.x, q.y, q.z, q.w};
+    uint32_t kept = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t one = __builtin_bit_cast(uint32_t, kept_pair(bits[i], d.least));
+        kept |= ((one | one >> 15) & 3u) << (2 * i);
+    }
+    return kept;
+}
+
+// All ones where bit i is set, else zero.
+__device__ __forceinline__ uint32_t bit_mask(uint32_t bits, int i) { return (uint32_t)((int32_t)(bits << (31 - i)) >> 31); }
+
+// The mask's bits for one backward call: rows of whole 64-bit words, a bit per element.
+__host__ __device__ inline int64_t kept_pitch(int64_t m) { return (m + 63) / 64 * 8; }
+
+// Nothing is moved across: loads stay ahead of what would otherwise be drawn in front of them, or pushed behind, to save registers.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// The wavefront's place in its workgroup, in a scalar register: what is decided by it is decided for the wavefront.
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+
+// Where the operand of lane (l % 16 = i, l / 16 = g) lies among an instruction's 64 in LDS: turned by g, so that threads that write neighbouring
+// eighths of a row, one g after the other, do not meet in a bank.
+__device__ __forceinline__ int operand_slot(int i, int g) { return g * 16 + (i ^ (g * 4)); }
+
+// Eight neighbouring values of the parts' sum, the parts in order; four of them on their way at once.
+__device__ __forceinline__ void sum_parts(const float* part, int splits, int64_t size, int64_t at, v4f& lo, v4f& hi) {
+    lo = hi = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = 0; s0 < splits; s0 += 4) {
+        v4f l[4], h[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float* q = part + (s0 + u < splits ? s0 + u : s0) * size + at;
+            l[u] = *reinterpret_cast<const v4f*>(q);
+            h[u] = *reinterpret_cast<const v4f*>(q + 4);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (s0 + u < splits) { lo += l[u]; hi += h[u]; }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ tokens by their adapters
+// The gradients take the tokens adapter by adapter.  order: places for tokens, adapter a's, by index, from range[a].x on, a multiple of 32, to
+// range[a].y; a place without a token holds -1.  With `before` tokens of lower adapters the range begins at before, rounded up to 32, plus
+// 32 a: so each finds its own alone, and none overlap.  places: b rounded up to 32, plus 32 slots.
+// A cut is a multiple of `chunk` (of 32) of places; a segment is what one adapter has between cuts, so adapter a has 1 + (cuts strictly inside
+// its range) of them, at least one even without tokens.  Segment i of adapter a has the index a + range[a].x / chunk + i: at most slots + cuts
+// of them, in order, none shared; indices that no adapter takes hold no adapter.
+struct Segment {
+    int adapter;             // -1: none
+    int begin, end;          // places
+    int part;                // where its sum goes: -1: it is the adapter's only segment, straight to the result
+};
+
+struct GroupArgs {
+    int chunk, cuts;         // cuts: ceil(places / chunk)
+    int* order;
+    int2* range;             // [slots]
+    Segment* segments;       // [slots + cuts]
+};
+
+// ------------------------------------------------------------------------------------------------ launches of the three files
+// What a backward call does besides S in that launch: workgroups that write down the tokens by adapter (one per slot, if wanted), and such
+// that draw the mask (if wanted).
+struct BackwardExtras {
+    GroupArgs group;
+    int groups;              // slots, or 0
+    uint8_t* kept;           // [b] rows of kept_pitch(m) bytes; null: no mask
+    DropoutMask drop;
+};
+
+// T (of drop(X) and U) or, backward, S (of E and V), in `splits` parts [b x max_rank].
+struct ThinPlan {
+    bool rows;               // the kernel for many tokens
+    int lanes;               // workgroups that share a tile's different adapters
+    int splits;              // of the reduction
+};
+ThinPlan thin_plan(int64_t b, int64_t K, int slots, int max_rank);
+hipError_t launch_thin(const AdapterPool& p, bool backward, const uint16_t* in, int64_t ld, float* part, const DropoutMask& drop,
+                       const ThinPlan& plan, const BackwardExtras& extras, hipStream_t s);
+// The extras alone.
+hipError_t launch_extras(const AdapterPool& p, const BackwardExtras& extras, hipStream_t s);
+
+struct WideArgs {
+    AdapterPool p;
+    const float* part;       // [splits][b][max_rank]
+    int splits;
+    float* thin;             // the sum of the parts is written here (not if null)
+    const void* base;
+    int64_t ld_base;
+    void* out;
+    int64_t ld_out;
+    const uint8_t* kept;     // backward: BackwardExtras::kept; null: no mask
+    float factor;            // and the kept elements' factor
+};
+hipError_t launch_wide(const WideArgs& g, bool backward, bool f32, hipStream_t s);
+
+struct GradJob {
+    const uint16_t* big;
+    int64_t ld;
+    const float* small;      // [b x max_rank]
+    float* out;              // [slots][wide x max_rank], or [slots][max_rank x wide] with rank_major
+    float* part;             // [parts] of the same
+    int64_t wide;
+    int tiles;               // of kGradCols columns; 0: no such job
+    int rank_major;          // G_U
+};
+constexpr int kGradWaves = 4;
+constexpr int kGradCols = 64 * kGradWaves;
+
+struct GradArgs {
+    AdapterPool p;
+    GradJob job[2];          // G_V, G_U
+    GroupArgs group;
+    const uint8_t* kept;     // for job[1]; null: no mask
+    float factor;
+};
+// Places between two cuts.
+int grad_chunk(int64_t places, int64_t m, int64_t n, int max_rank);
+// Sums that have a place of their own among a job's parts.
+inline int64_t grad_parts(int64_t cuts) { return cuts > 1 ? 2 * cuts + 1 : 0; }
+hipError_t launch_grads(const GradArgs& g, hipStream_t s);
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace adapters
+}  // namespace halo

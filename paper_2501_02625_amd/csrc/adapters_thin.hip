@@ -1,0 +1,496 @@
+// The thin results of the low-rank adapters, T = drop(X) U_a^T and S = s_a E V_a, and what a backward call prepares beside them: the tokens by
+// their adapters and the mask's bits (adapters_device.h has the formulas).
+#pragma clang fp contract(off)
+
+#include <type_traits>
+
+#include "adapters_device.h"
+
+namespace halo {
+namespace adapters {
+namespace {
+
+// The tokens of a tile by their adapters.  todo: tokens (a bit each) that have one and are not done; next() takes the adapter of the first
+// and all tokens that share it.
+struct TileAdapters {
+    int id;                  // of the lane's token
+    uint64_t todo;
+    __device__ __forceinline__ TileAdapters(const AdapterPool& p, int id_) : id(id_), todo(__ballot(is_adapter(p, id_))) {}
+    __device__ __forceinline__ int next(uint64_t& mine) {
+        const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
+        mine = __ballot(id == a) & todo;
+        todo &= ~mine;
+        return a;
+    }
+};
+
+// One adapter's tokens, written down by a workgroup.  A segment that is not alone begins or ends at a cut k: its sum goes to part k (it begins
+// there) or cuts + k (it is the first one, and ends there).
+template <int THREADS>
+__device__ __forceinline__ void group_tokens(const AdapterPool& p, const GroupArgs& g, int a) {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ int s_less[WAVES], s_same[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
+    const int b = (int)p.b, chunk = g.chunk;
+    int less = 0, same = 0;
+    for (int t = tid; t < b; t += THREADS) {
+        const int id = p.adapter_of[t];
+        less += id >= 0 && id < a;
+        same += id == a;
+    }
+    for (int h = 32; h > 0; h >>= 1) { less += __shfl_xor(less, h); same += __shfl_xor(same, h); }
+    if (lane == 0) { s_less[wave] = less; s_same[wave] = same; }
+    __syncthreads();
+    less = same = 0;
+    for (int w = 0; w < WAVES; ++w) { less += s_less[w]; same += s_same[w]; }
+    const int begin = (less + 31) / 32 * 32 + 32 * a, end = begin + same;
+    if (tid == 0) g.range[a] = make_int2(begin, end);
+    const int after = (less + same + 31) / 32 * 32 + 32 * (a + 1);     // where the next adapter begins
+    const int count = same ? (end + chunk - 1) / chunk - begin / chunk : 1;
+    const int index = a + begin / chunk, next = a == p.slots - 1 ? p.slots + g.cuts : a + 1 + after / chunk;
+    for (int i = tid; index + i < next; i += THREADS) {
+        Segment q{-1, 0, 0, -1};
+        if (i < count) {
+            const int cut = begin / chunk + i;           // the segment lies between this cut and the next
+            q.adapter = a;
+            q.begin = i == 0 ? begin : cut * chunk;
+            q.end = i == count - 1 ? end : (cut + 1) * chunk;
+            q.part = count == 1 ? -1 : i == 0 ? g.cuts + cut + 1 : cut;
+        }
+        g.segments[index + i] = q;
+    }
+    if (tid < after - end) g.order[end + tid] = -1;      // fewer than 64 places
+    int at = begin;
+    for (int t0 = 0; t0 < b && same > 0; t0 += THREADS) {
+        const int t = t0 + tid;
+        const bool hit = t < b && p.adapter_of[t] == a;
+        const uint64_t hits = __ballot(hit);
+        __syncthreads();
+        if (lane == 0) s_same[wave] = __builtin_popcountll(hits);
+        __syncthreads();
+        int before = 0, all = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            before += w < wave ? s_same[w] : 0;
+            all += s_same[w];
+        }
+        const int to = at + before + __builtin_popcountll(hits & ((1ull << lane) - 1));
+        if (hit && to < end) g.order[to] = t;
+        at += all;
+    }
+}
+
+// 64 bits of the mask per thread.  Drawn once here and not by both of the kernels that use them: eight elements cost ten rounds of two
+// 64-bit products, and those kernels have their own work for the vector units, where the one that this rides with waits for memory.
+template <int THREADS>
+__device__ __forceinline__ void draw_mask(const AdapterPool& p, const BackwardExtras& x, int64_t block) {
+    const int64_t words = kept_pitch(p.m) / 8, at = block * THREADS + threadIdx.x;
+    const int64_t row = at / words;
+    const uint32_t word = (uint32_t)(at - row * words);
+    if (row >= p.b) return;
+    uint32_t lo = 0, hi = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        lo |= kept_eight(x.drop, (uint32_t)row, word * 8 + i) << (8 * i);
+        hi |= kept_eight(x.drop, (uint32_t)row, word * 8 + 4 + i) << (8 * i);
+    }
+    reinterpret_cast<uint2*>(x.kept)[at] = make_uint2(lo, hi);
+}
+
+template <int THREADS>
+__device__ __forceinline__ void do_extra(const AdapterPool& p, const BackwardExtras& x, int64_t i) {
+    if (i < x.groups) group_tokens<THREADS>(p, x.group, (int)i);
+    else if (x.kept) draw_mask<THREADS>(p, x, i - x.groups);
+}
+
+__global__ void __launch_bounds__(256)
+extras_kernel(AdapterPool p, BackwardExtras x) { do_extra<256>(p, x, blockIdx.x); }
+
+// ------------------------------------------------------------------------------------------------ few tokens
+// part[split][t][c] = factor * sum over the split's k of in[t, k] * B_a[k, c]; B_a = U_a^T (K-contiguous) or, with KMAJOR, V_a (rows of
+// max_rank).  factor: that of dropout, or with KMAJOR scale_a.  A workgroup owns 16 tokens and, of the different adapters among them, every
+// gridDim.z-th; its wavefronts and the splits take 64-element chunks of K round robin (a chunk is one 128-byte line of every row), so that a
+// single token is read by as many wavefronts as it has lines.  Rows of other adapters' tokens are replaced by one of the adapter's own: no
+// line is fetched for them.  KMAJOR: the lane loads NT neighbouring columns of eight rows at once and packs them, so instruction t covers the
+// columns l % 16 * NT + t.  Columns beyond the adapter's rank are summed like the others and stored as zero.
+constexpr int kFewWaves = 8;
+
+struct ThinArgs {
+    AdapterPool p;
+    const uint16_t* in;
+    int64_t ld;
+    float* part;             // [splits][b][max_rank]
+    DropoutMask drop;
+    int tiles;               // workgroups along x beyond those do the extras
+    BackwardExtras extras;
+};
+
+template <int NT, bool KMAJOR>
+__device__ __forceinline__ void load_b(v4u (&out)[NT], const void* b, const uint32_t (&at)[NT], uint32_t k, uint32_t R) {
+    if constexpr (!KMAJOR) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) out[t] = load_at<v4u>(b, at[t] + 2 * k);
+    } else {
+        typedef uint32_t row __attribute__((ext_vector_type(NT > 2 ? NT / 2 : 2)));
+        std::conditional_t<NT <= 2, uint32_t, row> e[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const uint32_t o = at[0] + 2 * R * (k + u);
+            if constexpr (NT == 1) e[u] = load_at<uint16_t>(b, o);
+            else e[u] = load_at<std::conditional_t<NT <= 2, uint32_t, row>>(b, o);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            uint32_t w[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if constexpr (NT <= 2) w[u] = e[u];
+                else w[u] = e[u][t / 2];
+            }
+            out[t] = (t & 1) ? v4u{pack_hi(w[0], w[1]), pack_hi(w[2], w[3]), pack_hi(w[4], w[5]), pack_hi(w[6], w[7])}
+                             : v4u{pack_lo(w[0], w[1]), pack_lo(w[2], w[3]), pack_lo(w[4], w[5]), pack_lo(w[6], w[7])};
+        }
+    }
+}
+
+template <int NT, bool KMAJOR, bool DROP>
+__global__ void __launch_bounds__(64 * kFewWaves)
+thin_few_kernel(ThinArgs g) {
+    __shared__ float s_part[kFewWaves][NT][4][64];       // [wavefront][rank tile][register][lane]
+    __shared__ int s_id[64];
+    const AdapterPool& p = g.p;
+    if (KMAJOR && (int)blockIdx.x >= g.tiles) {
+        do_extra<64 * kFewWaves>(p, g.extras, (((int64_t)blockIdx.x - g.tiles) * gridDim.y + blockIdx.y) * gridDim.z + blockIdx.z);
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = wave_index();
+    const int lr = lane & 15, kg = lane >> 4;
+    const int R = p.max_rank;
+    const int64_t K = KMAJOR ? p.n : p.m;
+    const int64_t row0 = (int64_t)blockIdx.x * 16;
+    const int split = blockIdx.y, splits = gridDim.y;
+    float* part = g.part + (int64_t)split * p.b * R;
+    // read once, so that all wavefronts go the same way
+    if (wave == 0) s_id[lane] = lane < 16 && row0 + lane < p.b ? p.adapter_of[row0 + lane] : -1;
+    __syncthreads();
+    TileAdapters tile(p, s_id[lane]);
+    if (blockIdx.z == 0) {                               // tokens without an adapter
+        for (uint64_t bare = __ballot(lane < 16 && row0 + lane < p.b) & ~tile.todo; bare; bare &= bare - 1)
+            for (int c = threadIdx.x; c < R; c += 64 * kFewWaves) part[(row0 + __builtin_ctzll(bare)) * R + c] = 0.0f;
+    }
+    const int chunks = (int)((K + 63) >> 6), chunk0 = split * kFewWaves + wave, step = splits * kFewWaves;
+    const int count = chunks > chunk0 ? (chunks - chunk0 + step - 1) / step : 0;
+    for (unsigned seen = 0; tile.todo; ++seen) {
+        uint64_t mine;
+        const int a = tile.next(mine);
+        if (seen % gridDim.z != blockIdx.z) continue;
+        const uint32_t token = (uint32_t)(row0 + ((mine >> lr) & 1 ? lr : __builtin_ctzll(mine)));
+        const uint16_t* row = g.in + (int64_t)token * g.ld;
+        // columns beyond the pool's are replaced by the first one and not stored
+        const uint16_t* b = (KMAJOR ? p.V : p.U) + (int64_t)a * K * R;       // an adapter has at most 2^30 bytes
+        uint32_t bat[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (KMAJOR) bat[t] = 2 * (lr * NT < R ? lr * NT : 0);
+            else bat[t] = 2 * ((uint32_t)(t * 16 + lr < R ? t * 16 + lr : 0) * (uint32_t)K);
+        }
+        v4f acc[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        struct Chunk { v4u x[2], b[2][NT]; };
+        const auto load = [&](Chunk& q, int j) {         // eights beyond K: the row's first, which count as zero
+            const uint32_t k0 = (uint32_t)(chunk0 + (j < count ? j : 0) * step) * 64;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t k = k0 + h * 32 + kg * 8, kc = k < (uint32_t)K ? k : 0;
+                q.x[h] = *reinterpret_cast<const v4u*>(row + kc);
+                load_b<NT, KMAJOR>(q.b[h], b, bat, kc, R);
+            }
+        };
+        const auto multiply = [&](Chunk& q, int j) {
+            const uint32_t k0 = (uint32_t)(chunk0 + j * step) * 64;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t k = k0 + h * 32 + kg * 8;
+                if (DROP) q.x[h] = drop_eight(g.drop, q.x[h], token, k >> 3);
+                if (k0 + 64 > (uint32_t)K && k >= (uint32_t)K) {
+                    q.x[h] = v4u{0, 0, 0, 0};
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) q.b[h][t] = v4u{0, 0, 0, 0};
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t] = mfma(q.x[h], q.b[h][t], acc[t]);
+            }
+        };
+        if (count > 0) {
+            Chunk even, odd;
+            load(even, 0);
+            if (count > 1) {
+                in_order();
+                load(odd, 1);
+#pragma unroll 1
+                for (int j = 0; j + 1 < count; j += 2) {
+                    multiply(even, j);
+                    load(even, j + 2);
+                    multiply(odd, j + 1);
+                    load(odd, j + 3);
+                }
+            }
+            if (count & 1) multiply(even, count - 1);
+        }
+        const int rank = rank_of(p, a);
+        const float factor = KMAJOR ? scale_of(p, a) : DROP ? g.drop.factor : 1.0f;
+        // the wavefronts' sums meet in LDS and are added in wavefront order
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s_part[wave][t][e][lane] = acc[t][e];
+        __syncthreads();
+        for (int idx = threadIdx.x; idx < NT * 256; idx += 64 * kFewWaves) {
+            const int t = idx >> 8, e = (idx >> 6) & 3, l = idx & 63;
+            float sum = s_part[0][t][e][l];
+#pragma unroll
+            for (int w = 1; w < kFewWaves; ++w) sum += s_part[w][t][e][l];
+            const int r = 4 * (l >> 4) + e;
+            const int c = KMAJOR ? (l & 15) * NT + t : t * 16 + (l & 15);
+            if (((mine >> r) & 1) && c < R) part[(row0 + r) * R + c] = c < rank ? sum * factor : 0.0f;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ many tokens
+// The same sums: a wavefront owns 16 tokens and all of the split's K, in steps of 128; the four of a workgroup share the step's part of the
+// adapter, which is staged in LDS as the matrix instructions' operands, two steps in turn.  What a wavefront keeps for itself is its rows of
+// the next two steps, on their way: 16 registers a step.  Each tile of tokens begins at another step: rows lie whole powers of two apart, and
+// tiles in step would ask the same few memory channels at a time.
+constexpr int kRowWaves = 4;
+constexpr int kRowTile = 16 * kRowWaves;                 // tokens of a workgroup
+
+template <int NT, bool KMAJOR, bool DROP>
+__global__ void __launch_bounds__(64 * kRowWaves, 2)
+thin_rows_kernel(ThinArgs g) {
+    constexpr int THREADS = 64 * kRowWaves, KS = 128;
+    constexpr int UNITS = KMAJOR ? 64 * NT : 256 * NT, PER = (UNITS + THREADS - 1) / THREADS;    // of staging, and per thread
+    __shared__ v4u s_b[2][KS / 32][NT][64];
+    __shared__ int s_id[kRowTile];
+    const AdapterPool& p = g.p;
+    if (KMAJOR && (int)blockIdx.x >= g.tiles) {
+        do_extra<THREADS>(p, g.extras, (((int64_t)blockIdx.x - g.tiles) * gridDim.y + blockIdx.y) * gridDim.z + blockIdx.z);
+        return;
+    }
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
+    const int lr = lane & 15, kg = lane >> 4;
+    const int R = p.max_rank;
+    const int64_t K = KMAJOR ? p.n : p.m;
+    const int64_t row0 = (int64_t)blockIdx.x * kRowTile;
+    float* part = g.part + (int64_t)blockIdx.y * p.b * R;
+    // read once, so that all wavefronts go the same way
+    if (wave == 0) s_id[lane] = row0 + lane < p.b ? p.adapter_of[row0 + lane] : -1;
+    __syncthreads();
+    TileAdapters tile(p, s_id[lane]);
+    if (blockIdx.z == 0) {                               // tokens without an adapter
+        for (uint64_t bare = __ballot(row0 + lane < p.b) & ~tile.todo; bare; bare &= bare - 1)
+            for (int c = tid; c < R; c += THREADS) part[(row0 + __builtin_ctzll(bare)) * R + c] = 0.0f;
+    }
+    const int steps = (int)((K + KS - 1) / KS), per = (steps + (int)gridDim.y - 1) / (int)gridDim.y;
+    const int step0 = (int)blockIdx.y * per, count = steps - step0 < per ? steps - step0 : per;      // count > 0
+    const int turn = (int)(blockIdx.x % (unsigned)count);
+    const auto k_of = [&](int j) { return (uint32_t)(step0 + (j + turn < count ? j + turn : j + turn - count)) * KS; };
+    for (unsigned seen = 0; tile.todo; ++seen) {
+        uint64_t mine;
+        const int a = tile.next(mine);
+        if (seen % gridDim.z != blockIdx.z) continue;
+        const int r_own = wave * 16 + lr;
+        const uint32_t token = (uint32_t)(row0 + ((mine >> r_own) & 1 ? r_own : __builtin_ctzll(mine)));
+        const uint16_t* row = g.in + (int64_t)token * g.ld;
+        const uint16_t* b = (KMAJOR ? p.V : p.U) + (int64_t)a * K * R;       // of at most 2^30 bytes
+
+        v4u x[2][4], staged[PER];
+        uint2 rows[KMAJOR ? PER : 1][8];
+        const auto load_x = [&](v4u (&q)[4], int j) {
+            const uint32_t k0 = k_of(j < count ? j : 0);
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const uint32_t k = k0 + h * 32 + kg * 8;
+                q[h] = *reinterpret_cast<const v4u*>(row + (k < (uint32_t)K ? k : 0));
+            }
+        };
+        const auto load_staged = [&](int j) {
+            const uint32_t k0 = k_of(j < count ? j : 0);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const uint32_t u = (tid + i * THREADS) % UNITS;          // threads beyond load what others do
+                if constexpr (KMAJOR) {                  // eight rows of four columns
+                    const uint32_t c = 4 * (u % (4 * NT)), k = k0 + 8 * (u / (4 * NT));
+                    uint32_t at = 2 * ((k < (uint32_t)K ? k : 0) * R + (c < (uint32_t)R ? c : 0));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e, at += 2 * R) rows[i][e] = load_at<uint2>(b, at);
+                } else {                                 // eight values of a column: 128 bytes of it by eight neighbouring threads
+                    const uint32_t c = (u >> 3) % (16 * NT), k = k0 + 8 * ((u & 7) + 8 * (u / (128 * NT)));
+                    staged[i] = load_at<v4u>(b, 2 * ((c < (uint32_t)R ? c : 0) * (uint32_t)K + (k < (uint32_t)K ? k : 0)));
+                }
+            }
+        };
+        const auto write_staged = [&](int j) {
+            const uint32_t k0 = k_of(j);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const uint32_t u = tid + i * THREADS;
+                if constexpr (KMAJOR) {
+                    const uint32_t c = 4 * (u % (4 * NT)), k8 = u / (4 * NT);
+                    const bool ok = k0 + 8 * k8 < (uint32_t)K;
+                    v4u y[4];
+                    columns_of(rows[i], y);
+                    if (UNITS % THREADS == 0 || u < UNITS) {
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            s_b[j & 1][k8 >> 2][c >> 4][operand_slot((c & 15) + v, k8 & 3)] = ok ? y[v] : v4u{0, 0, 0, 0};
+                    }
+                } else {
+                    const uint32_t c = (u >> 3) % (16 * NT), k8 = (u & 7) + 8 * (u / (128 * NT));
+                    s_b[j & 1][k8 >> 2][c >> 4][operand_slot(c & 15, k8 & 3)] = k0 + 8 * k8 < (uint32_t)K ? staged[i] : v4u{0, 0, 0, 0};
+                }
+            }
+        };
+        v4f acc[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        const auto multiply = [&](v4u (&x)[4], int j) {
+            const uint32_t k0 = k_of(j);
+            if (k0 + KS > (uint32_t)K) {
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    if (k0 + h * 32 + kg * 8 >= (uint32_t)K) x[h] = v4u{0, 0, 0, 0};
+            }
+            v4u q[2][NT];                                // one instruction's operands while the other's are multiplied
+            const int slot = operand_slot(lr, kg);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) q[0][t] = s_b[j & 1][0][t][slot];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                if (h < 3) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) q[(h + 1) & 1][t] = s_b[j & 1][h + 1][t][slot];
+                }
+                in_order();
+                if (DROP) x[h] = drop_eight(g.drop, x[h], token, ((k0 + h * 32) >> 3) + kg);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t] = mfma(x[h], q[h & 1][t], acc[t]);
+                in_order();
+            }
+        };
+        // Step j: the adapter's part, on its way since the step before, goes to LDS, that of the next step is asked for, and the rows of the
+        // step after the next as soon as this one's registers are free.
+        const auto step = [&](v4u (&x)[4], int j) {
+            write_staged(j);
+            __syncthreads();
+            load_staged(j + 1);
+            multiply(x, j);
+            load_x(x, j + 2);
+        };
+        __syncthreads();                                 // the adapter before may still be read
+        load_staged(0);                                  // first: it is waited for first
+        in_order();
+        load_x(x[0], 0);
+        load_x(x[1], 1);
+#pragma unroll 1
+        for (int j = 0; j < count; j += 2) {
+            step(x[0], j);
+            if (j + 1 < count) step(x[1], j + 1);
+        }
+        const int rank = rank_of(p, a);
+        const float factor = KMAJOR ? scale_of(p, a) : DROP ? g.drop.factor : 1.0f;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[t][e] = t * 16 + lr < rank ? acc[t][e] * factor : 0.0f;
+        in_order();                                      // what is loaded for it is waited for here, not again at each of the stores
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = wave * 16 + 4 * kg + e, c = t * 16 + lr;
+                if (((mine >> r) & 1) && c < R) part[(row0 + r) * R + c] = acc[t][e];
+            }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+constexpr int64_t kManyTokens = 1024;                    // from here on thin_rows_kernel
+constexpr int64_t kFill = 512;                           // workgroups that fill the chip
+
+int64_t extra_blocks(const AdapterPool& p, const BackwardExtras& x, int threads) {
+    return x.groups + (x.kept ? ceil_div(p.b * (kept_pitch(p.m) / 8), threads) : 0);
+}
+
+template <int NT, bool KMAJOR>
+void launch_as(ThinArgs g, const ThinPlan& q, hipStream_t s) {
+    const bool drop = !KMAJOR && g.drop.least;
+    const int threads = 64 * (q.rows ? kRowWaves : kFewWaves);
+    g.tiles = (int)ceil_div(g.p.b, q.rows ? kRowTile : 16);
+    const int64_t extra = KMAJOR ? ceil_div(extra_blocks(g.p, g.extras, threads), q.splits * q.lanes) : 0;
+    const dim3 grid((unsigned)(g.tiles + extra), q.splits, q.lanes), block(threads);
+    if (q.rows && drop) hipLaunchKernelGGL((thin_rows_kernel<NT, KMAJOR, !KMAJOR>), grid, block, 0, s, g);
+    else if (q.rows) hipLaunchKernelGGL((thin_rows_kernel<NT, KMAJOR, false>), grid, block, 0, s, g);
+    else if (drop) hipLaunchKernelGGL((thin_few_kernel<NT, KMAJOR, !KMAJOR>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((thin_few_kernel<NT, KMAJOR, false>), grid, block, 0, s, g);
+}
+
+template <bool KMAJOR>
+void launch_by_rank(const ThinArgs& g, const ThinPlan& q, hipStream_t s) {
+    const int R = g.p.max_rank;
+    if (R <= 16) launch_as<1, KMAJOR>(g, q, s);
+    else if (R <= 32) launch_as<2, KMAJOR>(g, q, s);
+    else if (R <= 64) launch_as<4, KMAJOR>(g, q, s);
+    else launch_as<8, KMAJOR>(g, q, s);
+}
+
+}  // namespace
+
+ThinPlan thin_plan(int64_t b, int64_t K, int slots, int max_rank) {
+    (void)max_rank;
+    ThinPlan q;
+    q.rows = b >= kManyTokens;
+    const int64_t tiles = ceil_div(b, q.rows ? kRowTile : 16);
+    int64_t most = q.rows ? 8 : 16;                      // different adapters in a tile that get a workgroup of their own
+    if (b < most) most = b;
+    if (slots < most) most = slots;
+    const int64_t chunks = ceil_div(K, q.rows ? 128 : 64 * kFewWaves);
+    int64_t splits = 0;
+    if (q.rows) {                                        // first the reduction is split, then the adapters are
+        splits = kFill / (tiles > 0 ? tiles : 1);
+        if (splits > 8) splits = 8;
+        if (splits > chunks) splits = chunks;
+        if (splits < 1) splits = 1;
+        int64_t lanes = kFill / ((tiles > 0 ? tiles : 1) * splits);
+        if (lanes > most) lanes = most;
+        q.lanes = lanes < 1 ? 1 : (int)lanes;
+    } else {                                             // few tokens: one for each adapter that there may be
+        q.lanes = b <= 256 ? (int)(most < 1 ? 1 : most) : 1;
+        splits = kFill / (tiles * q.lanes > 0 ? tiles * q.lanes : 1);
+        if (splits > 8) splits = 8;
+        if (splits > chunks) splits = chunks;
+        if (splits < 1) splits = 1;
+    }
+    q.splits = (int)ceil_div(chunks, ceil_div(chunks, splits));      // none without a chunk
+    if (q.splits < 1) q.splits = 1;
+    return q;
+}
+
+hipError_t launch_thin(const AdapterPool& p, bool backward, const uint16_t* in, int64_t ld, float* part, const DropoutMask& drop,
+                       const ThinPlan& plan, const BackwardExtras& extras, hipStream_t s) {
+    ThinArgs g{};
+    g.p = p; g.in = in; g.ld = ld; g.part = part; g.drop = drop; g.extras = extras;
+    if (backward) launch_by_rank<true>(g, plan, s);
+    else launch_by_rank<false>(g, plan, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_extras(const AdapterPool& p, const BackwardExtras& extras, hipStream_t s) {
+    const int64_t blocks = extra_blocks(p, extras, 256);
+    if (blocks > 0) hipLaunchKernelGGL(extras_kernel, dim3((unsigned)blocks), dim3(256), 0, s, p, extras);
+    return hipGetLastError();
+}
+
+}  // namespace adapters
+}  // namespace halo
