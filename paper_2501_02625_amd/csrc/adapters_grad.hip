@@ -31,7 +31,8 @@ grad_kernel(GradArgs g) {
     const int64_t col = c0 + 4 * i16, colc = col < wide ? col : 0;       // columns beyond the matrix are not stored
     const bool masked = MASK && second;
     const uint16_t* big = job.big + colc;
-    // (without a mask the bits of the first place are loaded and not looked at)
+    // (E has no mask: the first bits are loaded, and all are taken as set)
+    const uint32_t kept_all = masked ? 0u : 0xFFu;
     const uint8_t* kept_at = MASK ? g.kept + (masked ? colc >> 3 : 0) : nullptr;
     const int64_t pitch = masked ? kept_pitch(wide) : 0;
 
@@ -86,8 +87,8 @@ grad_kernel(GradArgs g) {
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             x[u] = exists(q.token[u]) ? q.raw[u] : make_uint2(0, 0);
-            if (masked) {
-                const uint32_t kept = q.kept[u] >> (colc & 4);
+            if (MASK) {
+                const uint32_t kept = (q.kept[u] | kept_all) >> (colc & 4);
                 x[u].x &= pack_lo(bit_mask(kept, 0), bit_mask(kept, 1));
                 x[u].y &= pack_lo(bit_mask(kept, 2), bit_mask(kept, 3));
             }
@@ -111,32 +112,39 @@ grad_kernel(GradArgs g) {
             in_order();
         }
     };
-    int token[8];                                        // of the step whose rows are asked for next
     Step even, odd;
+    int even_next[8], odd_next[8];                       // tokens of the steps whose rows are asked for next
     // Step j: its part of `small`, on its way since the step before, goes to LDS, that of the next is asked for, and the rows of the step after
-    // the next as soon as this one's are used, by places that were asked for a step ago.
-    const auto step = [&](Step& q, const Step& next, int j) {
+    // the next as soon as this one's are used, by tokens that were asked for a step ago, ahead of that step's rows.
+    const auto step = [&](Step& q, const int (&q_next)[8], const Step& other, int (&other_next)[8], int j) {
         write_staged(q.token, j);
         __syncthreads();
-        load_staged(next.token);
+        load_staged(other.token);
         multiply(q, j);
-        load_rows(q, token);
-        load_order(token, j + 3);
+        load_order(other_next, j + 3);
+        in_order();
+        load_rows(q, q_next);
         in_order();
     };
     if (steps > 0) {                                     // the same for the workgroup
-        load_order(token, 0);
-        load_rows(even, token);
-        load_staged(token);
+        load_order(even_next, 0);
+        load_order(odd_next, 1);
+        load_rows(even, even_next);
         in_order();
-        load_order(token, 1);
-        load_rows(odd, token);
-        load_order(token, 2);
+        load_staged(even.token);
+        load_order(even_next, 2);
+        in_order();
+        load_rows(odd, odd_next);
         in_order();
 #pragma unroll 1
-        for (int j = 0; j < steps; j += 2) {
-            step(even, odd, j);
-            if (j + 1 < steps) step(odd, even, j + 1);
+        for (int j = 0; j + 1 < steps; j += 2) {
+            step(even, even_next, odd, odd_next, j);
+            step(odd, odd_next, even, even_next, j + 1);
+        }
+        if (steps & 1) {
+            write_staged(even.token, steps - 1);
+            __syncthreads();
+            multiply(even, steps - 1);
         }
     }
     const int rank = rank_of(p, seg.adapter);

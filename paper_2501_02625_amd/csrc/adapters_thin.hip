@@ -394,9 +394,14 @@ thin_rows_kernel(ThinArgs g) {
         load_x(x[0], 0);
         load_x(x[1], 1);
 #pragma unroll 1
-        for (int j = 0; j < count; j += 2) {
+        for (int j = 0; j + 1 < count; j += 2) {
             step(x[0], j);
-            if (j + 1 < count) step(x[1], j + 1);
+            step(x[1], j + 1);
+        }
+        if (count & 1) {
+            write_staged(count - 1);
+            __syncthreads();
+            multiply(x[0], count - 1);
         }
         const int rank = rank_of(p, a);
         const float factor = KMAJOR ? scale_of(p, a) : DROP ? g.drop.factor : 1.0f;

@@ -146,7 +146,7 @@ template <int RC_, int MT, int WAVES, bool BWD, bool F32>
 __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || (RC_ == 4 && BWD) ? 1 : 2)
 wide_kernel(WideArgs g) {
     constexpr bool STACK = RC_ == 0;
-    constexpr int RC = STACK ? 1 : RC_, NP = STACK ? 2 : 3, ROWS = 16 * MT, WORDS = (ROWS + 63) / 64, DEPTH = F32 || RC == 4 || (RC == 2 && BWD) ? 2 : 4;
+    constexpr int RC = STACK ? 1 : RC_, NP = STACK ? 2 : 3, ROWS = 16 * MT, WORDS = (ROWS + 63) / 64, DEPTH = MT == 1 ? 1 : F32 || RC == 4 || (RC == 2 && BWD) ? 2 : 4;
     constexpr bool AHEAD = RC <= 2;                      // registers for two blocks of the adapter
     __shared__ v4u s_thin[MT * RC * NP][64];
     __shared__ int s_id[64 * WORDS];
@@ -161,7 +161,67 @@ wide_kernel(WideArgs g) {
     const int64_t row0 = (int64_t)blockIdx.x * ROWS;
     for (int r = tid; r < 64 * WORDS; r += 64 * WAVES) s_id[r] = r < ROWS && row0 + r < p.b ? p.adapter_of[row0 + r] : -1;
     __syncthreads();
+    // this wavefront's blocks of features: every WAVES-th of the workgroup's range, begun at another one by every tile of tokens
+    const int blocks = (int)((wide + 63) >> 6), per = (blocks + (int)gridDim.y - 1) / (int)gridDim.y;
+    const int block0 = (int)blockIdx.y * per, end = block0 + per < blocks ? block0 + per : blocks;
+    const int count = end - block0 > wave ? (end - block0 - wave + WAVES - 1) / WAVES : 0;
+    const int turn = count > 0 ? (int)(blockIdx.x % (unsigned)count) : 0;
+    const auto f_of = [&](int j) {                       // the first one's where there is no such block
+        j = j < count ? j : 0;
+        return count > 0 ? (uint32_t)(block0 + wave + (j + turn < count ? j + turn : j + turn - count) * WAVES) * 64 : 0u;
+    };
     const int r_lane = STACK ? 8 * (kg & 1) : 8 * kg;
+    // without a base: something that is there to be loaded, and nothing of it kept
+    const void* base_at = g.base ? g.base : g.out;
+    const int64_t base_ld = g.base ? g.ld_base : g.ld_out;
+    const uint32_t base_keep = g.base ? ~0u : 0u;
+    // and without a mask: something, of which every bit is set
+    const uint8_t* kept_at = g.kept ? g.kept : reinterpret_cast<const uint8_t*>(g.part);
+    const int64_t pitch = g.kept ? kept_pitch(wide) : 0;
+    const uint32_t kept_all = g.kept ? 0u : 0xFFFFu;
+    uint64_t todo[WORDS];                                // tokens with an adapter that are not done
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) todo[w] = __ballot(is_adapter(p, s_id[w * 64 + lane]));
+
+    // The next adapter of this workgroup: its first token, and bit i of own: the even (odd) token of the lane's pair in step i is its, of steps:
+    // any token of step i is.
+    unsigned seen = 0;
+    int first = -1, a = -1;
+    uint32_t own[2] = {0, 0}, steps = 0;
+    const auto next_adapter = [&]() {
+        a = -1;
+        while (true) {
+            first = -1;
+#pragma unroll
+            for (int w = WORDS - 1; w >= 0; --w)
+                if (todo[w]) first = w * 64 + __builtin_ctzll(todo[w]);
+            if (first < 0) return;
+            const int id = __builtin_amdgcn_readfirstlane(s_id[first]);
+            own[0] = own[1] = steps = 0;
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) {
+                const uint64_t mine = __ballot(s_id[w * 64 + lane] == id) & todo[w];
+                todo[w] &= ~mine;
+#pragma unroll
+                for (int i = 0; i < (MT < 4 ? MT : 4); ++i) {
+                    const uint32_t sixteen = (uint32_t)(mine >> (16 * i)) & 0xFFFFu;
+                    own[0] |= ((sixteen >> pair) & 1u) << (4 * w + i);
+                    own[1] |= ((sixteen >> (pair + 1)) & 1u) << (4 * w + i);
+                    steps |= (sixteen ? 1u : 0u) << (4 * w + i);
+                }
+            }
+            if (seen++ % gridDim.z == blockIdx.z) { a = id; return; }
+        }
+    };
+    const auto adapter = [&]() { return (BWD ? p.U : p.V) + (int64_t)a * wide * R; };
+    Block now, next_block;
+    uint64_t bare[WORDS];
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) bare[w] = ~todo[w];
+    next_adapter();
+    if (a < 0 && blockIdx.z > 0) return;                 // the same for the workgroup
+    if (a >= 0) now.load(adapter(), R, (uint32_t)wide, f_of(0), lr, r_lane);
+
     for (int j = wave; j < MT * RC; j += WAVES) {        // the thin values of the tile's tokens, in pieces
         const int i = j / RC, r = 32 * (j % RC) + r_lane;
         const int64_t t = row0 + i * 16 + lr;
@@ -190,31 +250,12 @@ wide_kernel(WideArgs g) {
     }
     __syncthreads();
 
-    // this wavefront's blocks of features: every WAVES-th of the workgroup's range, begun at another one by every tile of tokens
-    const int blocks = (int)((wide + 63) >> 6), per = (blocks + (int)gridDim.y - 1) / (int)gridDim.y;
-    const int block0 = (int)blockIdx.y * per, end = block0 + per < blocks ? block0 + per : blocks;
-    const int count = end - block0 > wave ? (end - block0 - wave + WAVES - 1) / WAVES : 0;
     if (count <= 0) return;
-    const int turn = (int)(blockIdx.x % (unsigned)count);
-    const auto f_of = [&](int j) {
-        j = j < count ? j : 0;
-        return (uint32_t)(block0 + wave + (j + turn < count ? j + turn : j + turn - count) * WAVES) * 64;
-    };
-    // without a base: something that is there to be loaded, and nothing of it kept
-    const void* base_at = g.base ? g.base : g.out;
-    const int64_t base_ld = g.base ? g.ld_base : g.ld_out;
-    const uint32_t base_keep = g.base ? ~0u : 0u;
-    // and without a mask: something, of which every bit is set
-    const uint8_t* kept_at = g.kept ? g.kept : reinterpret_cast<const uint8_t*>(g.part);
-    const int64_t pitch = g.kept ? kept_pitch(wide) : 0;
-    const uint32_t kept_all = g.kept ? 0u : 0xFFFFu;
-    uint64_t todo[WORDS];                                // tokens with an adapter that are not done
+    if (blockIdx.z == 0 && g.base != g.out) {            // tokens without an adapter: the base as it is
 #pragma unroll
-    for (int w = 0; w < WORDS; ++w) {
-        const int r = w * 64 + lane;
-        todo[w] = __ballot(is_adapter(p, s_id[r]));
-        if (blockIdx.z == 0 && g.base != g.out) {        // tokens without one: the base as it is
-            for (uint64_t left = __ballot(r < ROWS && row0 + r < p.b) & ~todo[w]; left; left &= left - 1) {
+        for (int w = 0; w < WORDS; ++w) {
+            const int r = w * 64 + lane;
+            for (uint64_t left = __ballot(r < ROWS && row0 + r < p.b) & bare[w]; left; left &= left - 1) {
                 const int64_t t = row0 + w * 64 + __builtin_ctzll(left);
                 for (int j = 0; j < count; ++j) {
                     const int64_t f = f_of(j) + 8 * lane;
@@ -228,30 +269,8 @@ wide_kernel(WideArgs g) {
             }
         }
     }
-    unsigned seen = 0;
 #pragma unroll 1
-    while (true) {
-        int first = -1;                                  // the next adapter's first token
-#pragma unroll
-        for (int w = WORDS - 1; w >= 0; --w)
-            if (todo[w]) first = w * 64 + __builtin_ctzll(todo[w]);
-        if (first < 0) break;
-        const int a = __builtin_amdgcn_readfirstlane(s_id[first]);
-        uint32_t own[2] = {0, 0}, steps = 0;             // bit i: the even (odd) token of the lane's pair in step i is a's; any of the step is
-#pragma unroll
-        for (int w = 0; w < WORDS; ++w) {
-            const uint64_t mine = __ballot(s_id[w * 64 + lane] == a) & todo[w];
-            todo[w] &= ~mine;
-#pragma unroll
-            for (int i = 0; i < (MT < 4 ? MT : 4); ++i) {
-                const uint32_t sixteen = (uint32_t)(mine >> (16 * i)) & 0xFFFFu;
-                own[0] |= ((sixteen >> pair) & 1u) << (4 * w + i);
-                own[1] |= ((sixteen >> (pair + 1)) & 1u) << (4 * w + i);
-                steps |= (sixteen ? 1u : 0u) << (4 * w + i);
-            }
-        }
-        if (seen++ % gridDim.z != blockIdx.z) continue;
-        const uint16_t* adapter = (BWD ? p.U : p.V) + (int64_t)a * wide * R;
+    for (bool again = false; a >= 0; next_adapter(), again = true) {
         struct Place { int j; uint32_t left; };          // block of features, and the steps left in it, this one the lowest
         const auto after = [&](Place q) {
             q.left &= q.left - 1;
@@ -280,7 +299,6 @@ wide_kernel(WideArgs g) {
                 x.kept = kept_all | *reinterpret_cast<const uint16_t*>(kept_at + (t < p.b ? t : p.b - 1) * pitch + word + 2 * kg);
             }
         };
-        Block now, next_block;
         const auto work = [&](Ahead& x, const Place& q) {
             const int i = __builtin_ctz(q.left);
             v4f acc[4];
@@ -321,11 +339,11 @@ wide_kernel(WideArgs g) {
                 if ((own[k] >> i) & 1 && f < wide) y[k].store(g.out, (row0 + i * 16 + pair + k) * g.ld_out + f);
         };
         Place at{0, steps}, next = at;
-        now.load(adapter, R, (uint32_t)wide, f_of(0), lr, r_lane);
+        if (again) now.load(adapter(), R, (uint32_t)wide, f_of(0), lr, r_lane);
         in_order();
 #pragma unroll
         for (int k = 0; k < DEPTH; ++k, next = after(next)) load_ahead(ahead[k], next);
-        if (AHEAD) next_block.load(adapter, R, (uint32_t)wide, f_of(1), lr, r_lane);
+        if (AHEAD) next_block.load(adapter(), R, (uint32_t)wide, f_of(1), lr, r_lane);
         const int rank = rank_of(p, a);
         now.finish(rank, r_lane);
 #pragma unroll 1
@@ -340,9 +358,9 @@ wide_kernel(WideArgs g) {
                 at = after(at);
                 if (at.j != j && at.j < count) {
                     if (AHEAD) now = next_block;
-                    else now.load(adapter, R, (uint32_t)wide, f_of(at.j), lr, r_lane);
+                    else now.load(adapter(), R, (uint32_t)wide, f_of(at.j), lr, r_lane);
                     now.finish(rank, r_lane);
-                    if (AHEAD) next_block.load(adapter, R, (uint32_t)wide, f_of(at.j + 1), lr, r_lane);
+                    if (AHEAD) next_block.load(adapter(), R, (uint32_t)wide, f_of(at.j + 1), lr, r_lane);
                 }
             }
         }
