@@ -29,7 +29,7 @@ BwdLayout bwd_layout(int64_t b, int64_t m, int64_t n, int slots, int R, bool dro
     L.order = take((size_t)places * 4);
     L.range = take((size_t)slots * sizeof(int2));
     L.segments = take(((size_t)slots + L.cuts) * sizeof(Segment));
-    L.kept = take(drop ? (size_t)(b * kept_pitch(m)) : 0);
+    L.kept = take(drop ? (size_t)kept_words(b, m) * 8 : 0);
     L.part_v = take((size_t)grad_parts(L.cuts) * n * R * 4);
     L.part_u = take((size_t)grad_parts(L.cuts) * m * R * 4);
     L.total = at;

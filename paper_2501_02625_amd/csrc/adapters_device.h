@@ -28,7 +28,6 @@ namespace adapters {
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-typedef uint16_t v2us __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ v4f mfma(v4u a, v4u b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
@@ -83,39 +82,42 @@ __device__ __forceinline__ int rank_of(const AdapterPool& p, int a) {
 }
 __device__ __forceinline__ float scale_of(const AdapterPool& p, int a) { return p.scale ? p.scale[a] : 1.0f; }
 
-// Of two random 16-bit halves: 1 where they are at least `least` (saturating difference to least - 1, at most 1).
-__device__ __forceinline__ v2us kept_pair(uint32_t bits, uint32_t least) {
-    const uint16_t below = (uint16_t)(least - 1);
-    return __builtin_elementwise_min(__builtin_elementwise_sub_sat(__builtin_bit_cast(v2us, bits), v2us{below, below}), v2us{1, 1});
+// Of two random 16-bit halves: 1 where they are at least `least` (saturating difference to least - 1, at most 1).  In assembly, because the
+// compiler makes two compares and two selects of it: 14 instructions for the bits of eight elements, or 35.
+__device__ __forceinline__ uint32_t kept_pair(uint32_t bits, uint32_t below, uint32_t one) {
+    uint32_t r;
+    asm("v_pk_sub_u16 %0, %1, %2 clamp\n\tv_pk_min_u16 %0, %0, %3" : "=&v"(r) : "v"(bits), "v"(below), "v"(one));
+    return r;
 }
 
 // Eight bf16 values with the dropped ones set to zero.
 __device__ __forceinline__ v4u drop_eight(const DropoutMask& d, v4u x, uint32_t row, uint32_t group) {
     const uint4 q = dropout_bits(d, row, group);
-    const uint32_t bits[4] = {q.x, q.y, q.z, q.w};
+    const uint32_t below = (d.least - 1) * 0x10001u, bits[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] &= __builtin_bit_cast(uint32_t, (v2us)(v2us{0, 0} - kept_pair(bits[i], d.least)));
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t k = kept_pair(bits[i], below, 0x10001u);
+        x[i] &= (k << 16) - k;                          // all ones in the halves that are 1
+    }
     return x;
 }
 
 // Which of eight elements are kept, a bit each.
 __device__ __forceinline__ uint32_t kept_eight(const DropoutMask& d, uint32_t row, uint32_t group) {
     const uint4 q = dropout_bits(d, row, group);
-    const uint32_t bits[4] = {q.x, q.y, q.z, q.w};
-    uint32_t kept = 0;
+    const uint32_t below = (d.least - 1) * 0x10001u, bits[4] = {q.x, q.y, q.z, q.w};
+    uint32_t kept = 0;                                   // of element 2 i in bit 2 i, of element 2 i + 1 in bit 16 + 2 i
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t one = __builtin_bit_cast(uint32_t, kept_pair(bits[i], d.least));
-        kept |= ((one | one >> 15) & 3u) << (2 * i);
-    }
-    return kept;
+    for (int i = 0; i < 4; ++i) kept |= kept_pair(bits[i], below, 0x10001u) << (2 * i);
+    return (kept | kept >> 15) & 0xFFu;
 }
 
 // All ones where bit i is set, else zero.
 __device__ __forceinline__ uint32_t bit_mask(uint32_t bits, int i) { return (uint32_t)((int32_t)(bits << (31 - i)) >> 31); }
 
-// The mask's bits for one backward call: rows of whole 64-bit words, a bit per element.
-__host__ __device__ inline int64_t kept_pitch(int64_t m) { return (m + 63) / 64 * 8; }
+// The mask's bits for one backward call: [blocks of 64 columns][b] words of 64, so that a token's word is eight bytes times the token from
+// the block's beginning.
+__host__ __device__ inline int64_t kept_words(int64_t b, int64_t m) { return (m + 63) / 64 * b; }
 
 // Nothing is moved across: loads stay ahead of what would otherwise be drawn in front of them, or pushed behind, to save registers.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
@@ -170,7 +172,7 @@ struct GroupArgs {
 struct BackwardExtras {
     GroupArgs group;
     int groups;              // slots, or 0
-    uint8_t* kept;           // [b] rows of kept_pitch(m) bytes; null: no mask
+    uint8_t* kept;           // kept_words(b, m) words of 64 bits; null: no mask
     DropoutMask drop;
 };
 

@@ -2,6 +2,8 @@
 // (adapters_device.h has the formulas).
 #pragma clang fp contract(off)
 
+#include <type_traits>
+
 #include "adapters_device.h"
 
 namespace halo {
@@ -31,122 +33,138 @@ grad_kernel(GradArgs g) {
     const int64_t col = c0 + 4 * i16, colc = col < wide ? col : 0;       // columns beyond the matrix are not stored
     const bool masked = MASK && second;
     const uint16_t* big = job.big + colc;
-    // (E has no mask: the first bits are loaded, and all are taken as set)
-    const uint32_t kept_all = masked ? 0u : 0xFFu;
-    const uint8_t* kept_at = MASK ? g.kept + (masked ? colc >> 3 : 0) : nullptr;
-    const int64_t pitch = masked ? kept_pitch(wide) : 0;
+    const uint8_t* kept_at = MASK && masked ? g.kept + (c0 < wide ? c0 >> 6 : 0) * p.b * 8 + (i16 >> 1) : nullptr;
+    const uint32_t last = (uint32_t)p.b - 1, pitch = 2 * (uint32_t)job.ld;       // bytes
 
-    struct Step {
-        int token[8];
-        uint2 raw[8];
-        uint32_t kept[8];
-    };
-    const int steps = (seg.end - seg.begin + 31) >> 5;
-    const auto load_order = [&](int (&token)[8], int j) {
-        const int4* o = reinterpret_cast<const int4*>(g.group.order + seg.begin + 32 * (j < steps ? j : 0) + 8 * kq);
-        const int4 lo = o[0], hi = o[1];
-        token[0] = lo.x; token[1] = lo.y; token[2] = lo.z; token[3] = lo.w;
-        token[4] = hi.x; token[5] = hi.y; token[6] = hi.z; token[7] = hi.w;
-    };
-    const auto exists = [&](int t) { return (uint64_t)(int64_t)t < (uint64_t)p.b; };
-    const auto load_rows = [&](Step& q, const int (&token)[8]) {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {                    // a place without a token loads the first one, which counts as zero
-            const int64_t t = exists(token[u]) ? token[u] : 0;
-            q.token[u] = token[u];
-            q.raw[u] = *reinterpret_cast<const uint2*>(big + t * job.ld);
-            if (MASK) q.kept[u] = kept_at[t * pitch];
-        }
-    };
-    // thread (rank tile, lane) stages what that lane multiplies with
-    const int unit = tid % UNITS, small_c = (tile0 + (unit >> 6)) * 16 + (unit & 15);
-    const float* small = job.small + (small_c < R ? small_c : 0);
-    float staged[8];
-    const auto load_staged = [&](const int (&token)[8]) {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) staged[u] = small[(int64_t)(exists(token[u]) ? token[u] : 0) * R];
-    };
-    const auto write_staged = [&](const int (&token)[8], int j) {
-        float x[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = exists(token[u]) ? staged[u] : 0.0f;
-        v4u q[3];
-        split_eight(x, q);
-        if (UNITS % THREADS == 0 || tid < UNITS) {
-#pragma unroll
-            for (int k = 0; k < 3; ++k) s_small[j & 1][(unit >> 6) * 3 + k][lane] = q[k];
-        }
-    };
     v4f acc[NT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int v = 0; v < 4; ++v) acc[t][v] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    const auto multiply = [&](const Step& q, int j) {
-        uint2 x[8];
+    // the sums, with the mask or without; chosen once
+    const auto sum = [&](auto with_mask) {
+        constexpr bool M = decltype(with_mask)::value;
+        struct Step {
+            int token[8];
+            uint2 raw[8];
+            uint32_t kept[8];
+        };
+        const int steps = (seg.end - seg.begin + 31) >> 5;
+        const auto load_order = [&](int (&token)[8], int j) {
+            const int4* o = reinterpret_cast<const int4*>(g.group.order + seg.begin + 32 * (j < steps ? j : 0) + 8 * kq);
+            const int4 lo = o[0], hi = o[1];
+            token[0] = lo.x; token[1] = lo.y; token[2] = lo.z; token[3] = lo.w;
+            token[4] = hi.x; token[5] = hi.y; token[6] = hi.z; token[7] = hi.w;
+        };
+        // A place without a token (-1) loads the last one's row.  Only an adapter's last step has such places; there they are set to zero.
+        const auto load_rows = [&](Step& q, const int (&token)[8]) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            x[u] = exists(q.token[u]) ? q.raw[u] : make_uint2(0, 0);
-            if (MASK) {
-                const uint32_t kept = (q.kept[u] | kept_all) >> (colc & 4);
-                x[u].x &= pack_lo(bit_mask(kept, 0), bit_mask(kept, 1));
-                x[u].y &= pack_lo(bit_mask(kept, 2), bit_mask(kept, 3));
+            for (int u = 0; u < 8; ++u) {
+                const uint32_t t = (uint32_t)token[u] < last ? (uint32_t)token[u] : last;
+                q.token[u] = token[u];
+                q.raw[u] = *reinterpret_cast<const uint2*>(reinterpret_cast<const char*>(big) + (uint64_t)t * pitch);
+                if (M) q.kept[u] = kept_at[t * 8];
             }
-        }
-        v4u a[4];
-        columns_of(x, a);
-        v4u b[2][3];                                     // one rank tile's operands while the other's are multiplied
+        };
+        // thread (rank tile, lane) stages what that lane multiplies with
+        const int unit = tid % UNITS, small_c = (tile0 + (unit >> 6)) * 16 + (unit & 15);
+        const uint32_t small_at = 4 * (small_c < R ? small_c : 0);
+        float staged[8];
+        const auto load_staged = [&](const int (&token)[8]) {
 #pragma unroll
-        for (int k = 0; k < 3; ++k) b[0][k] = s_small[j & 1][k][lane];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (t + 1 < NT) {
-#pragma unroll
-                for (int k = 0; k < 3; ++k) b[(t + 1) & 1][k] = s_small[j & 1][(t + 1) * 3 + k][lane];
+            for (int u = 0; u < 8; ++u) {
+                const uint32_t t = (uint32_t)token[u] < last ? (uint32_t)token[u] : last;
+                staged[u] = load_at<float>(job.small, __umul24(t, 4 * R) + small_at);        // at most 2^31 bytes
             }
-            in_order();
+        };
+        const auto write_staged = [&](const int (&token)[8], int j) {
+            if (j == steps - 1) {
 #pragma unroll
-            for (int k = 0; k < 3; ++k)
+                for (int u = 0; u < 8; ++u)
+                    if (token[u] < 0) staged[u] = 0.0f;
+            }
+            v4u q[3];
+            split_eight(staged, q);
+            if (UNITS % THREADS == 0 || tid < UNITS) {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[t][v] = mfma(a[v], b[t & 1][k], acc[t][v]);
-            in_order();
-        }
-    };
-    Step even, odd;
-    int even_next[8], odd_next[8];                       // tokens of the steps whose rows are asked for next
-    // Step j: its part of `small`, on its way since the step before, goes to LDS, that of the next is asked for, and the rows of the step after
-    // the next as soon as this one's are used, by tokens that were asked for a step ago, ahead of that step's rows.
-    const auto step = [&](Step& q, const int (&q_next)[8], const Step& other, int (&other_next)[8], int j) {
-        write_staged(q.token, j);
-        __syncthreads();
-        load_staged(other.token);
-        multiply(q, j);
-        load_order(other_next, j + 3);
-        in_order();
-        load_rows(q, q_next);
-        in_order();
-    };
-    if (steps > 0) {                                     // the same for the workgroup
-        load_order(even_next, 0);
-        load_order(odd_next, 1);
-        load_rows(even, even_next);
-        in_order();
-        load_staged(even.token);
-        load_order(even_next, 2);
-        in_order();
-        load_rows(odd, odd_next);
-        in_order();
-#pragma unroll 1
-        for (int j = 0; j + 1 < steps; j += 2) {
-            step(even, even_next, odd, odd_next, j);
-            step(odd, odd_next, even, even_next, j + 1);
-        }
-        if (steps & 1) {
-            write_staged(even.token, steps - 1);
+                for (int k = 0; k < 3; ++k) s_small[j & 1][(unit >> 6) * 3 + k][lane] = q[k];
+            }
+        };
+        const auto multiply = [&](const Step& q, int j) {
+            uint2 x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = q.raw[u];
+            if (M) {
+                const int low = 4 * (i16 & 1);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const uint32_t kept = q.kept[u] >> low;
+                    x[u].x &= pack_lo(bit_mask(kept, 0), bit_mask(kept, 1));
+                    x[u].y &= pack_lo(bit_mask(kept, 2), bit_mask(kept, 3));
+                }
+            }
+            if (j == steps - 1) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (q.token[u] < 0) x[u] = make_uint2(0, 0);
+            }
+            v4u a[4];
+            columns_of(x, a);
+            v4u b[2][3];                                     // one rank tile's operands while the other's are multiplied
+#pragma unroll
+            for (int k = 0; k < 3; ++k) b[0][k] = s_small[j & 1][k][lane];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if (t + 1 < NT) {
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) b[(t + 1) & 1][k] = s_small[j & 1][(t + 1) * 3 + k][lane];
+                }
+                in_order();
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[t][v] = mfma(a[v], b[t & 1][k], acc[t][v]);
+                in_order();
+            }
+        };
+        Step even, odd;
+        int even_next[8], odd_next[8];                       // tokens of the steps whose rows are asked for next
+        // Step j: its part of `small`, on its way since the step before, goes to LDS, that of the next is asked for, and the rows of the step after
+        // the next as soon as this one's are used, by tokens that were asked for a step ago, ahead of that step's rows.
+        const auto step = [&](Step& q, const int (&q_next)[8], const Step& other, int (&other_next)[8], int j) {
+            write_staged(q.token, j);
             __syncthreads();
-            multiply(even, steps - 1);
+            load_staged(other.token);
+            multiply(q, j);
+            load_order(other_next, j + 3);
+            in_order();
+            load_rows(q, q_next);
+            in_order();
+        };
+        if (steps > 0) {                                     // the same for the workgroup
+            load_order(even_next, 0);
+            load_order(odd_next, 1);
+            load_rows(even, even_next);
+            in_order();
+            load_staged(even.token);
+            load_order(even_next, 2);
+            in_order();
+            load_rows(odd, odd_next);
+            in_order();
+#pragma unroll 1
+            for (int j = 0; j + 1 < steps; j += 2) {
+                step(even, even_next, odd, odd_next, j);
+                step(odd, odd_next, even, even_next, j + 1);
+            }
+            if (steps & 1) {
+                write_staged(even.token, steps - 1);
+                __syncthreads();
+                multiply(even, steps - 1);
+            }
         }
-    }
+    };
+    if (MASK && second) sum(std::bool_constant<MASK>());
+    else sum(std::false_type());
     const int rank = rank_of(p, seg.adapter);
     const float factor = second ? (masked ? g.factor : 1.0f) : scale_of(p, seg.adapter);
     float* dst = seg.part < 0 ? job.out + (int64_t)seg.adapter * wide * R : job.part + (int64_t)seg.part * wide * R;

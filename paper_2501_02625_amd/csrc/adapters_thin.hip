@@ -83,15 +83,13 @@ __device__ __forceinline__ void group_tokens(const AdapterPool& p, const GroupAr
 // 64-bit products, and those kernels have their own work for the vector units, where the one that this rides with waits for memory.
 template <int THREADS>
 __device__ __forceinline__ void draw_mask(const AdapterPool& p, const BackwardExtras& x, int64_t block) {
-    const int64_t words = kept_pitch(p.m) / 8, at = block * THREADS + threadIdx.x;
-    const int64_t row = at / words;
-    const uint32_t word = (uint32_t)(at - row * words);
-    if (row >= p.b) return;
+    const int64_t at = block * THREADS + threadIdx.x, word = at / p.b, row = at - word * p.b;
+    if (at >= kept_words(p.b, p.m)) return;
     uint32_t lo = 0, hi = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        lo |= kept_eight(x.drop, (uint32_t)row, word * 8 + i) << (8 * i);
-        hi |= kept_eight(x.drop, (uint32_t)row, word * 8 + 4 + i) << (8 * i);
+        lo |= kept_eight(x.drop, (uint32_t)row, (uint32_t)word * 8 + i) << (8 * i);
+        hi |= kept_eight(x.drop, (uint32_t)row, (uint32_t)word * 8 + 4 + i) << (8 * i);
     }
     reinterpret_cast<uint2*>(x.kept)[at] = make_uint2(lo, hi);
 }
@@ -425,7 +423,7 @@ constexpr int64_t kManyTokens = 1024;                    // from here on thin_ro
 constexpr int64_t kFill = 512;                           // workgroups that fill the chip
 
 int64_t extra_blocks(const AdapterPool& p, const BackwardExtras& x, int threads) {
-    return x.groups + (x.kept ? ceil_div(p.b * (kept_pitch(p.m) / 8), threads) : 0);
+    return x.groups + (x.kept ? ceil_div(kept_words(p.b, p.m), threads) : 0);
 }
 
 template <int NT, bool KMAJOR>

@@ -18,13 +18,13 @@ __device__ __forceinline__ uint32_t round_two(float x, float y) {
 template <bool F32>
 struct Eight {
     v4u q[F32 ? 2 : 1];
-    __device__ __forceinline__ void load(const void* base, int64_t at) {
-        const v4u* s = reinterpret_cast<const v4u*>(reinterpret_cast<const char*>(base) + at * (F32 ? 4 : 2));
+    __device__ __forceinline__ void load(const void* from) {
+        const v4u* s = reinterpret_cast<const v4u*>(from);
         q[0] = s[0];
         if constexpr (F32) q[1] = s[1];
     }
-    __device__ __forceinline__ void store(void* out, int64_t at) const {
-        v4u* o = reinterpret_cast<v4u*>(reinterpret_cast<char*>(out) + at * (F32 ? 4 : 2));
+    __device__ __forceinline__ void store(void* to) const {
+        v4u* o = reinterpret_cast<v4u*>(to);
         o[0] = q[0];
         if constexpr (F32) o[1] = q[1];
     }
@@ -146,7 +146,8 @@ template <int RC_, int MT, int WAVES, bool BWD, bool F32>
 __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || (RC_ == 4 && BWD) ? 1 : 2)
 wide_kernel(WideArgs g) {
     constexpr bool STACK = RC_ == 0;
-    constexpr int RC = STACK ? 1 : RC_, NP = STACK ? 2 : 3, ROWS = 16 * MT, WORDS = (ROWS + 63) / 64, DEPTH = MT == 1 ? 1 : F32 || RC == 4 || (RC == 2 && BWD) ? 2 : 4;
+    constexpr int RC = STACK ? 1 : RC_, NP = STACK ? 2 : 3, ROWS = 16 * MT, WORDS = (ROWS + 63) / 64;
+    constexpr int DEPTH = MT == 1 ? 1 : F32 || RC == 4 || (RC == 2 && BWD) ? 2 : 4;     // steps whose base is on its way
     constexpr bool AHEAD = RC <= 2;                      // registers for two blocks of the adapter
     __shared__ v4u s_thin[MT * RC * NP][64];
     __shared__ int s_id[64 * WORDS];
@@ -177,8 +178,17 @@ wide_kernel(WideArgs g) {
     const uint32_t base_keep = g.base ? ~0u : 0u;
     // and without a mask: something, of which every bit is set
     const uint8_t* kept_at = g.kept ? g.kept : reinterpret_cast<const uint8_t*>(g.part);
-    const int64_t pitch = g.kept ? kept_pitch(wide) : 0;
-    const uint32_t kept_all = g.kept ? 0u : 0xFFFFu;
+    const int64_t kept_block = g.kept ? p.b * 8 : 0;     // bytes from one block of 64 columns to the next
+    const uint32_t kept_token = g.kept ? 8 : 0, kept_all = g.kept ? 0u : 0xFFFFu;
+    // where the lane's runs of the tile's first pair of tokens begin
+    const char* base_lane[2];
+    char* out_lane[2];
+    constexpr int SIZE = F32 ? 4 : 2;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        base_lane[k] = reinterpret_cast<const char*>(base_at) + ((row0 + pair + k) * base_ld + run) * SIZE;
+        out_lane[k] = reinterpret_cast<char*>(g.out) + ((row0 + pair + k) * g.ld_out + run) * SIZE;
+    }
     uint64_t todo[WORDS];                                // tokens with an adapter that are not done
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) todo[w] = __ballot(is_adapter(p, s_id[w * 64 + lane]));
@@ -261,10 +271,10 @@ wide_kernel(WideArgs g) {
                     const int64_t f = f_of(j) + 8 * lane;
                     if (lane >= 8 || f >= wide) continue;
                     Eight<F32> x;
-                    x.load(base_at, t * base_ld + f);
+                    x.load(reinterpret_cast<const char*>(base_at) + (t * base_ld + f) * SIZE);
                     x.q[0] &= base_keep;
                     if constexpr (F32) x.q[1] &= base_keep;
-                    x.store(g.out, t * g.ld_out + f);
+                    x.store(reinterpret_cast<char*>(g.out) + (t * g.ld_out + f) * SIZE);
                 }
             }
         }
@@ -287,16 +297,17 @@ wide_kernel(WideArgs g) {
         Ahead ahead[DEPTH];
         const auto load_ahead = [&](Ahead& x, const Place& q) {
             const int i = __builtin_ctz(q.left);
-            const int64_t f = f_of(q.j) + run;
+            const uint32_t f0 = f_of(q.j);
+            const int64_t at = (16 * i * base_ld + f0) * SIZE;
+            const char* instead = reinterpret_cast<const char*>(base_at) + (row0 + first) * base_ld * SIZE;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {                // other adapters' tokens, features beyond: the first of this one's
-                const bool ok = (own[k] >> i) & 1 && f < wide;
-                x.base[k].load(base_at, (row0 + (ok ? i * 16 + pair + k : first)) * base_ld + (ok ? f : 0));
+                const bool ok = (own[k] >> i) & 1 && f0 + run < (uint32_t)wide;
+                x.base[k].load(ok ? base_lane[k] + at : instead);
             }
             if constexpr (BWD) {
-                const int64_t t = row0 + i * 16 + lr;
-                const uint32_t word = pitch ? f_of(q.j) / 8 : 0;
-                x.kept = kept_all | *reinterpret_cast<const uint16_t*>(kept_at + (t < p.b ? t : p.b - 1) * pitch + word + 2 * kg);
+                const uint32_t t = (uint32_t)(row0 + i * 16 + lr), tc = t < (uint32_t)p.b ? t : (uint32_t)p.b - 1;
+                x.kept = kept_all | load_at<uint16_t>(kept_at + (f0 >> 6) * kept_block, tc * kept_token + 2 * kg);
             }
         };
         const auto work = [&](Ahead& x, const Place& q) {
@@ -333,10 +344,11 @@ wide_kernel(WideArgs g) {
                 y[k].set(v);
             }
             y[0].exchange(y[1], odd);
-            const int64_t f = f_of(q.j) + run;
+            const uint32_t f0 = f_of(q.j);
+            const int64_t at = (16 * i * g.ld_out + f0) * SIZE;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
-                if ((own[k] >> i) & 1 && f < wide) y[k].store(g.out, (row0 + i * 16 + pair + k) * g.ld_out + f);
+                if ((own[k] >> i) & 1 && f0 + run < (uint32_t)wide) y[k].store(out_lane[k] + at);
         };
         Place at{0, steps}, next = at;
         if (again) now.load(adapter(), R, (uint32_t)wide, f_of(0), lr, r_lane);

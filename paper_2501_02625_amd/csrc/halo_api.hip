@@ -1036,6 +1036,7 @@ halo_status halo_adapters_bwd(const halo_adapters_desc* desc, const void* E, int
         if (ld_e < n || (GU && ld_x < m) || (EX && ld_ex < m) || (EX && base && ld_base < m) || (EX && base == EX && ld_base != ld_ex))
             return HALO_ESHAPE;
         const int64_t per16 = f32 ? 4 : 8;
+        if (ld_e > INT32_MAX || (GU && ld_x > INT32_MAX)) return HALO_EUNSUPPORTED;      // row pitches in bytes are 32-bit numbers
         if (ld_e % 8 || (GU && ld_x % 8) || (EX && ld_ex % per16) || (EX && base && ld_base % per16)) return HALO_EALIGN;
     }
     if (!aligned16(E) || !aligned16(X) || !aligned16(T) || !aligned16(U) || !aligned16(V) || !aligned16(base) || !aligned16(EX) ||
