@@ -19,8 +19,8 @@ struct BwdLayout {
 BwdLayout bwd_layout(int64_t b, int64_t m, int64_t n, int slots, int R, bool drop) {
     BwdLayout L;
     const int64_t places = (b + 31) / 32 * 32 + 32 * (int64_t)slots;
-    L.plan = thin_plan(b, n, slots, R);
-    L.chunk = grad_chunk(places, m, n, R);
+    L.plan = thin_plan(b, n, slots);
+    L.chunk = grad_chunk(places, m, n, slots, R);
     L.cuts = (int)ceil_div(places, L.chunk);
     size_t at = 0;
     const auto take = [&at](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
@@ -39,7 +39,7 @@ BwdLayout bwd_layout(int64_t b, int64_t m, int64_t n, int slots, int R, bool dro
 }  // namespace
 
 size_t adapters_fwd_workspace(int64_t b, int64_t m, int64_t, int slots, int max_rank) {
-    const ThinPlan q = thin_plan(b, m, slots, max_rank);
+    const ThinPlan q = thin_plan(b, m, slots);
     return q.splits > 1 ? round256((size_t)q.splits * b * max_rank * 4) : 0;
 }
 
@@ -49,7 +49,7 @@ size_t adapters_bwd_workspace(int64_t b, int64_t m, int64_t n, int slots, int ma
 
 hipError_t launch_adapters_fwd(const AdaptersFwd& a, hipStream_t s) {
     const AdapterPool& p = a.pool;
-    const ThinPlan q = thin_plan(p.b, p.m, p.slots, p.max_rank);
+    const ThinPlan q = thin_plan(p.b, p.m, p.slots);
     float* part = q.splits > 1 ? reinterpret_cast<float*>(a.workspace) : a.T;
     const hipError_t e = launch_thin(p, false, a.X, a.ld_x, part, a.drop, q, BackwardExtras{}, s);
     if (e != hipSuccess) return e;

@@ -129,6 +129,17 @@ __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstl
 // eighths of a row, one g after the other, do not meet in a bank.
 __device__ __forceinline__ int operand_slot(int i, int g) { return g * 16 + (i ^ (g * 4)); }
 
+// Of two blocks of four rows of sixteen 16-bit values in LDS, of which lane l of sixteen names the eight bytes l % 4 of row l / 4: column l, the
+// first block's rows and then the second's.
+__device__ __forceinline__ v4u read_transposed(const char* lo, const char* hi) {
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4s* place;
+    const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(uintptr_t)(__attribute__((address_space(3))) const char*)lo);
+    const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(uintptr_t)(__attribute__((address_space(3))) const char*)hi);
+    const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
+    return v4u{x.x, x.y, y.x, y.y};
+}
+
 // Eight neighbouring values of the parts' sum, the parts in order; four of them on their way at once.
 __device__ __forceinline__ void sum_parts(const float* part, int splits, int64_t size, int64_t at, v4f& lo, v4f& hi) {
     lo = hi = v4f{0.0f, 0.0f, 0.0f, 0.0f};
@@ -182,7 +193,7 @@ struct ThinPlan {
     int lanes;               // workgroups that share a tile's different adapters
     int splits;              // of the reduction
 };
-ThinPlan thin_plan(int64_t b, int64_t K, int slots, int max_rank);
+ThinPlan thin_plan(int64_t b, int64_t K, int slots);
 hipError_t launch_thin(const AdapterPool& p, bool backward, const uint16_t* in, int64_t ld, float* part, const DropoutMask& drop,
                        const ThinPlan& plan, const BackwardExtras& extras, hipStream_t s);
 // The extras alone.
@@ -223,7 +234,7 @@ struct GradArgs {
     float factor;
 };
 // Places between two cuts.
-int grad_chunk(int64_t places, int64_t m, int64_t n, int max_rank);
+int grad_chunk(int64_t places, int64_t m, int64_t n, int slots, int max_rank);
 // Sums that have a place of their own among a job's parts.
 inline int64_t grad_parts(int64_t cuts) { return cuts > 1 ? 2 * cuts + 1 : 0; }
 hipError_t launch_grads(const GradArgs& g, hipStream_t s);

@@ -219,7 +219,7 @@ grad_join_kernel(AdapterPool p, GroupArgs group, GradJob v, GradJob u) {
     *reinterpret_cast<v4f*>(job.out + (int64_t)a * size + i) = sum;
 }
 
-constexpr int64_t kFill = 768;                           // workgroups
+constexpr int64_t kFill = 512;                           // workgroups that the chip holds at once
 
 template <int NT>
 void launch_as(const GradArgs& g, hipStream_t s) {
@@ -231,12 +231,16 @@ void launch_as(const GradArgs& g, hipStream_t s) {
 
 }  // namespace
 
-// Few enough that the column tiles fill the chip, so many that the partial sums stay small next to what is read for them.
-int grad_chunk(int64_t places, int64_t m, int64_t n, int max_rank) {
-    const int64_t tiles = ceil_div(m, kGradCols) + ceil_div(n, kGradCols);
-    int64_t chunk = ceil_div(places * tiles, kFill), least = 8 * max_rank < 256 ? 256 : 8 * max_rank;
+// Segments there are as many as adapters with tokens plus cuts, less one; together with the column tiles they should fill the chip once: every
+// further one costs a partial sum that is written and read again.  How many adapters have tokens is not known here: as if all had, but cut
+// at least half as often as one adapter alone would be.  A segment is at least 256 places and long next to its partial sum.
+int grad_chunk(int64_t places, int64_t m, int64_t n, int slots, int max_rank) {
+    const int64_t tiles = ceil_div(m, kGradCols) + ceil_div(n, kGradCols), wanted = kFill > tiles ? kFill / tiles : 1;
+    int64_t cuts = wanted - slots + 1;
+    if (cuts < (wanted + 1) / 2) cuts = (wanted + 1) / 2;
+    int64_t chunk = ceil_div(places, cuts), least = 8 * max_rank < 256 ? 256 : 8 * max_rank;
     if (chunk < least) chunk = least;
-    return (int)(ceil_div(chunk, 128) * 128);
+    return (int)(ceil_div(chunk, 32) * 32);
 }
 
 hipError_t launch_grads(const GradArgs& g, hipStream_t s) {

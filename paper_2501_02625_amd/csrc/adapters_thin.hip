@@ -28,15 +28,24 @@ struct TileAdapters {
 // there) or cuts + k (it is the first one, and ends there).
 template <int THREADS>
 __device__ __forceinline__ void group_tokens(const AdapterPool& p, const GroupArgs& g, int a) {
-    constexpr int WAVES = THREADS / 64;
-    __shared__ int s_less[WAVES], s_same[WAVES];
+    constexpr int WAVES = THREADS / 64, AHEAD = 8;       // loads on their way at once: there is nothing else to wait for them with
+    __shared__ int s_less[WAVES], s_same[WAVES], s_hits[AHEAD * WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
     const int b = (int)p.b, chunk = g.chunk;
     int less = 0, same = 0;
-    for (int t = tid; t < b; t += THREADS) {
-        const int id = p.adapter_of[t];
-        less += id >= 0 && id < a;
-        same += id == a;
+    for (int t0 = 0; t0 < b; t0 += AHEAD * THREADS) {
+        int id[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int t = t0 + i * THREADS + tid;
+            id[i] = p.adapter_of[t < b ? t : 0];
+            id[i] = t < b ? id[i] : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            less += id[i] >= 0 && id[i] < a;
+            same += id[i] == a;
+        }
     }
     for (int h = 32; h > 0; h >>= 1) { less += __shfl_xor(less, h); same += __shfl_xor(same, h); }
     if (lane == 0) { s_less[wave] = less; s_same[wave] = same; }
@@ -61,21 +70,34 @@ __device__ __forceinline__ void group_tokens(const AdapterPool& p, const GroupAr
     }
     if (tid < after - end) g.order[end + tid] = -1;      // fewer than 64 places
     int at = begin;
-    for (int t0 = 0; t0 < b && same > 0; t0 += THREADS) {
-        const int t = t0 + tid;
-        const bool hit = t < b && p.adapter_of[t] == a;
-        const uint64_t hits = __ballot(hit);
-        __syncthreads();
-        if (lane == 0) s_same[wave] = __builtin_popcountll(hits);
-        __syncthreads();
-        int before = 0, all = 0;
-        for (int w = 0; w < WAVES; ++w) {
-            before += w < wave ? s_same[w] : 0;
-            all += s_same[w];
+    for (int t0 = 0; t0 < b && same > 0; t0 += AHEAD * THREADS) {
+        uint64_t hits[AHEAD];
+        int id[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int t = t0 + i * THREADS + tid;
+            id[i] = p.adapter_of[t < b ? t : 0];
         }
-        const int to = at + before + __builtin_popcountll(hits & ((1ull << lane) - 1));
-        if (hit && to < end) g.order[to] = t;
-        at += all;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) hits[i] = __ballot(t0 + i * THREADS + tid < b && id[i] == a);
+        __syncthreads();
+        if (lane == 0) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) s_hits[i * WAVES + wave] = __builtin_popcountll(hits[i]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            int before = 0, all = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                before += w < wave ? s_hits[i * WAVES + w] : 0;
+                all += s_hits[i * WAVES + w];
+            }
+            const int to = at + before + __builtin_popcountll(hits[i] & ((1ull << lane) - 1));
+            if (((hits[i] >> lane) & 1) && to < end) g.order[to] = t0 + i * THREADS + tid;
+            at += all;
+        }
     }
 }
 
@@ -106,7 +128,7 @@ extras_kernel(AdapterPool p, BackwardExtras x) { do_extra<256>(p, x, blockIdx.x)
 // ------------------------------------------------------------------------------------------------ few tokens
 // part[split][t][c] = factor * sum over the split's k of in[t, k] * B_a[k, c]; B_a = U_a^T (K-contiguous) or, with KMAJOR, V_a (rows of
 // max_rank).  factor: that of dropout, or with KMAJOR scale_a.  A workgroup owns 16 tokens and, of the different adapters among them, every
-// gridDim.z-th; its wavefronts and the splits take 64-element chunks of K round robin (a chunk is one 128-byte line of every row), so that a
+// lanes-th; its wavefronts and the splits take 64-element chunks of K round robin (a chunk is one 128-byte line of every row), so that a
 // single token is read by as many wavefronts as it has lines.  Rows of other adapters' tokens are replaced by one of the adapter's own: no
 // line is fetched for them.  KMAJOR: the lane loads NT neighbouring columns of eight rows at once and packs them, so instruction t covers the
 // columns l % 16 * NT + t.  Columns beyond the adapter's rank are summed like the others and stored as zero.
@@ -118,9 +140,22 @@ struct ThinArgs {
     int64_t ld;
     float* part;             // [splits][b][max_rank]
     DropoutMask drop;
-    int tiles;               // workgroups along x beyond those do the extras
+    int tiles, splits, lanes;
     BackwardExtras extras;
 };
+
+// What a workgroup does.  The order in which they begin: the adapters' groups, which wait longest; each tile's first adapter, all splits of it;
+// the other adapters, most of which most tiles do not have; and the mask, for which vector units are left over until then.
+struct Place { int64_t extra; int tile, split, lane; };
+
+template <bool KMAJOR>
+__device__ __forceinline__ Place place_of(const ThinArgs& g) {
+    const unsigned groups = KMAJOR ? g.extras.groups : 0, tiles = (unsigned)(g.tiles * g.splits) * g.lanes, i = blockIdx.x - groups;
+    if (KMAJOR && blockIdx.x < groups) return Place{(int64_t)blockIdx.x, 0, 0, 0};
+    if (KMAJOR && i >= tiles) return Place{(int64_t)blockIdx.x - tiles, 0, 0, 0};
+    const unsigned j = i / (unsigned)g.tiles;
+    return Place{-1, (int)(i - j * g.tiles), (int)(j % (unsigned)g.splits), (int)(j / (unsigned)g.splits)};
+}
 
 template <int NT, bool KMAJOR>
 __device__ __forceinline__ void load_b(v4u (&out)[NT], const void* b, const uint32_t (&at)[NT], uint32_t k, uint32_t R) {
@@ -156,22 +191,23 @@ thin_few_kernel(ThinArgs g) {
     __shared__ float s_part[kFewWaves][NT][4][64];       // [wavefront][rank tile][register][lane]
     __shared__ int s_id[64];
     const AdapterPool& p = g.p;
-    if (KMAJOR && (int)blockIdx.x >= g.tiles) {
-        do_extra<64 * kFewWaves>(p, g.extras, (((int64_t)blockIdx.x - g.tiles) * gridDim.y + blockIdx.y) * gridDim.z + blockIdx.z);
+    const Place at = place_of<KMAJOR>(g);
+    if (KMAJOR && at.extra >= 0) {
+        do_extra<64 * kFewWaves>(p, g.extras, at.extra);
         return;
     }
     const int lane = threadIdx.x & 63, wave = wave_index();
     const int lr = lane & 15, kg = lane >> 4;
     const int R = p.max_rank;
     const int64_t K = KMAJOR ? p.n : p.m;
-    const int64_t row0 = (int64_t)blockIdx.x * 16;
-    const int split = blockIdx.y, splits = gridDim.y;
+    const int64_t row0 = (int64_t)at.tile * 16;
+    const int split = at.split, splits = g.splits;
     float* part = g.part + (int64_t)split * p.b * R;
     // read once, so that all wavefronts go the same way
     if (wave == 0) s_id[lane] = lane < 16 && row0 + lane < p.b ? p.adapter_of[row0 + lane] : -1;
     __syncthreads();
     TileAdapters tile(p, s_id[lane]);
-    if (blockIdx.z == 0) {                               // tokens without an adapter
+    if (at.lane == 0) {                                  // tokens without an adapter
         for (uint64_t bare = __ballot(lane < 16 && row0 + lane < p.b) & ~tile.todo; bare; bare &= bare - 1)
             for (int c = threadIdx.x; c < R; c += 64 * kFewWaves) part[(row0 + __builtin_ctzll(bare)) * R + c] = 0.0f;
     }
@@ -180,7 +216,7 @@ thin_few_kernel(ThinArgs g) {
     for (unsigned seen = 0; tile.todo; ++seen) {
         uint64_t mine;
         const int a = tile.next(mine);
-        if (seen % gridDim.z != blockIdx.z) continue;
+        if (seen % g.lanes != (unsigned)at.lane) continue;
         const uint32_t token = (uint32_t)(row0 + ((mine >> lr) & 1 ? lr : __builtin_ctzll(mine)));
         const uint16_t* row = g.in + (int64_t)token * g.ld;
         // columns beyond the pool's are replaced by the first one and not stored
@@ -258,125 +294,135 @@ thin_few_kernel(ThinArgs g) {
 
 // ------------------------------------------------------------------------------------------------ many tokens
 // The same sums: a wavefront owns 16 tokens and all of the split's K, in steps of 128; the four of a workgroup share the step's part of the
-// adapter, which is staged in LDS as the matrix instructions' operands, two steps in turn.  What a wavefront keeps for itself is its rows of
-// the next two steps, on their way: 16 registers a step.  Each tile of tokens begins at another step: rows lie whole powers of two apart, and
+// adapter, which is staged in LDS, two steps in turn, that of the next step on its way.  What a wavefront keeps for itself is its rows of the
+// next two steps, on their way: 16 registers a step.  Each tile of tokens begins at another step: rows lie whole powers of two apart, and
 // tiles in step would ask the same few memory channels at a time.
+// The vector memory unit takes as long for an instruction that brings 8 bytes a lane as for one of 16, so both are loaded 16 bytes at a time.
+// KMAJOR: the adapter's rows go to LDS as they are and are turned as they are read, for which the hardware has an instruction (eight rows of
+// four columns loaded and packed by each thread: 97 us instead of 69 at 6328 tokens, K = 14336, rank 16); and the tokens' rows are loaded by
+// whole lines, sixteen lanes 256 bytes, and turned in LDS as well (12.5 -> 9.7 us at 2048 tokens, K = 4096, rank 16; without the adapter's
+// work of turning, in the other direction, it costs more than it gives: 15.0 -> 16.4 at 1037 tokens, rank 64).
 constexpr int kRowWaves = 4;
 constexpr int kRowTile = 16 * kRowWaves;                 // tokens of a workgroup
 
 template <int NT, bool KMAJOR, bool DROP>
-__global__ void __launch_bounds__(64 * kRowWaves, 2)
+__global__ void __launch_bounds__(64 * kRowWaves, NT == 8 ? 1 : 2)
 thin_rows_kernel(ThinArgs g) {
     constexpr int THREADS = 64 * kRowWaves, KS = 128;
-    constexpr int UNITS = KMAJOR ? 64 * NT : 256 * NT, PER = (UNITS + THREADS - 1) / THREADS;    // of staging, and per thread
-    __shared__ v4u s_b[2][KS / 32][NT][64];
+    // KMAJOR: the adapter's rows as they are, 32 bytes for a tile of 16 columns and so many more that four rows of a tile lie in all the banks
+    constexpr int PITCH = 32 * NT + (NT > 1 ? 32 : 0);
+    __shared__ v4u s_b[2][KMAJOR ? KS * PITCH / 16 : KS / 32 * NT * 64], s_x[KMAJOR ? kRowWaves : 1][16][KS / 8];
     __shared__ int s_id[kRowTile];
     const AdapterPool& p = g.p;
-    if (KMAJOR && (int)blockIdx.x >= g.tiles) {
-        do_extra<THREADS>(p, g.extras, (((int64_t)blockIdx.x - g.tiles) * gridDim.y + blockIdx.y) * gridDim.z + blockIdx.z);
+    const Place at = place_of<KMAJOR>(g);
+    if (KMAJOR && at.extra >= 0) {
+        do_extra<THREADS>(p, g.extras, at.extra);
         return;
     }
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
     const int lr = lane & 15, kg = lane >> 4;
     const int R = p.max_rank;
     const int64_t K = KMAJOR ? p.n : p.m;
-    const int64_t row0 = (int64_t)blockIdx.x * kRowTile;
-    float* part = g.part + (int64_t)blockIdx.y * p.b * R;
+    const int64_t row0 = (int64_t)at.tile * kRowTile;
+    float* part = g.part + (int64_t)at.split * p.b * R;
     // read once, so that all wavefronts go the same way
     if (wave == 0) s_id[lane] = row0 + lane < p.b ? p.adapter_of[row0 + lane] : -1;
     __syncthreads();
     TileAdapters tile(p, s_id[lane]);
-    if (blockIdx.z == 0) {                               // tokens without an adapter
+    if (at.lane == 0) {                                  // tokens without an adapter
         for (uint64_t bare = __ballot(row0 + lane < p.b) & ~tile.todo; bare; bare &= bare - 1)
             for (int c = tid; c < R; c += THREADS) part[(row0 + __builtin_ctzll(bare)) * R + c] = 0.0f;
     }
-    const int steps = (int)((K + KS - 1) / KS), per = (steps + (int)gridDim.y - 1) / (int)gridDim.y;
-    const int step0 = (int)blockIdx.y * per, count = steps - step0 < per ? steps - step0 : per;      // count > 0
-    const int turn = (int)(blockIdx.x % (unsigned)count);
+    const int steps = (int)((K + KS - 1) / KS), per = (steps + g.splits - 1) / g.splits;
+    const int step0 = at.split * per, count = steps - step0 < per ? steps - step0 : per;      // count > 0
+    const int turn = (int)((unsigned)at.tile % (unsigned)count);
     const auto k_of = [&](int j) { return (uint32_t)(step0 + (j + turn < count ? j + turn : j + turn - count)) * KS; };
     for (unsigned seen = 0; tile.todo; ++seen) {
         uint64_t mine;
         const int a = tile.next(mine);
-        if (seen % gridDim.z != blockIdx.z) continue;
-        const int r_own = wave * 16 + lr;
-        const uint32_t token = (uint32_t)(row0 + ((mine >> r_own) & 1 ? r_own : __builtin_ctzll(mine)));
-        const uint16_t* row = g.in + (int64_t)token * g.ld;
+        if (seen % g.lanes != (unsigned)at.lane) continue;
+        const auto token_of = [&](int r) { return (uint32_t)(row0 + ((mine >> r) & 1 ? r : __builtin_ctzll(mine))); };
+        const uint32_t token = token_of(wave * 16 + lr);
+        const uint16_t* row[4];                          // those that the lane loads, sixteen lanes 256 bytes of each
+#pragma unroll
+        for (int h = 0; h < 4; ++h) row[h] = g.in + (int64_t)(KMAJOR ? token_of(wave * 16 + 4 * h + kg) : token) * g.ld;
         const uint16_t* b = (KMAJOR ? p.V : p.U) + (int64_t)a * K * R;       // of at most 2^30 bytes
 
-        v4u x[2][4], staged[PER];
-        uint2 rows[KMAJOR ? PER : 1][8];
-        const auto load_x = [&](v4u (&q)[4], int j) {
-            const uint32_t k0 = k_of(j < count ? j : 0);
+        v4u x[2][4], staged[NT];
+        // The adapter's eights that the thread stages, i = 0 .. NT: of a column (128 bytes of it by eight neighbouring threads), or of a row
+        uint32_t k8[NT], from[NT], to[NT];               // where it begins along K, in memory (bytes, from the step on) and in LDS
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            uint32_t u = tid + i * THREADS;
+            if constexpr (KMAJOR) {
+                if (u >= 16u * R) u = 0;                 // more columns than there are: others load the first eight too
+                k8[i] = u / (R >> 3);
+                from[i] = 16 * u;
+                to[i] = k8[i] * (PITCH / 16) + u % (R >> 3);
+            } else {
+                const uint32_t c = (u >> 3) % (16 * NT), e = (u & 7) + 8 * (u / (128 * NT));
+                k8[i] = 8 * e;
+                from[i] = 2 * ((c < (uint32_t)R ? c : 0) * (uint32_t)K + k8[i]);
+                to[i] = ((e >> 2) * NT + (c >> 4)) * 64 + operand_slot(c & 15, e & 3);
+            }
+        }
+        // of the last step again where there are no more
+        const auto load_x = [&](v4u (&x)[4], int j) {
+            const uint32_t k0 = k_of(j < count ? j : count - 1);
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
-                const uint32_t k = k0 + h * 32 + kg * 8;
-                q[h] = *reinterpret_cast<const v4u*>(row + (k < (uint32_t)K ? k : 0));
+                const uint32_t k = k0 + (KMAJOR ? lr : 4 * h + kg) * 8;
+                x[h] = *reinterpret_cast<const v4u*>(row[h] + (k < (uint32_t)K ? k : 0));
             }
         };
         const auto load_staged = [&](int j) {
-            const uint32_t k0 = k_of(j < count ? j : 0);
+            const uint32_t k0 = k_of(j < count ? j : count - 1);
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint32_t u = (tid + i * THREADS) % UNITS;          // threads beyond load what others do
-                if constexpr (KMAJOR) {                  // eight rows of four columns
-                    const uint32_t c = 4 * (u % (4 * NT)), k = k0 + 8 * (u / (4 * NT));
-                    uint32_t at = 2 * ((k < (uint32_t)K ? k : 0) * R + (c < (uint32_t)R ? c : 0));
-#pragma unroll
-                    for (int e = 0; e < 8; ++e, at += 2 * R) rows[i][e] = load_at<uint2>(b, at);
-                } else {                                 // eight values of a column: 128 bytes of it by eight neighbouring threads
-                    const uint32_t c = (u >> 3) % (16 * NT), k = k0 + 8 * ((u & 7) + 8 * (u / (128 * NT)));
-                    staged[i] = load_at<v4u>(b, 2 * ((c < (uint32_t)R ? c : 0) * (uint32_t)K + (k < (uint32_t)K ? k : 0)));
-                }
-            }
+            for (int i = 0; i < NT; ++i) staged[i] = load_at<v4u>(b, k0 + k8[i] < (uint32_t)K ? 2 * k0 * (KMAJOR ? R : 1) + from[i] : 0);
         };
         const auto write_staged = [&](int j) {
             const uint32_t k0 = k_of(j);
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const uint32_t u = tid + i * THREADS;
-                if constexpr (KMAJOR) {
-                    const uint32_t c = 4 * (u % (4 * NT)), k8 = u / (4 * NT);
-                    const bool ok = k0 + 8 * k8 < (uint32_t)K;
-                    v4u y[4];
-                    columns_of(rows[i], y);
-                    if (UNITS % THREADS == 0 || u < UNITS) {
-#pragma unroll
-                        for (int v = 0; v < 4; ++v)
-                            s_b[j & 1][k8 >> 2][c >> 4][operand_slot((c & 15) + v, k8 & 3)] = ok ? y[v] : v4u{0, 0, 0, 0};
-                    }
-                } else {
-                    const uint32_t c = (u >> 3) % (16 * NT), k8 = (u & 7) + 8 * (u / (128 * NT));
-                    s_b[j & 1][k8 >> 2][c >> 4][operand_slot(c & 15, k8 & 3)] = k0 + 8 * k8 < (uint32_t)K ? staged[i] : v4u{0, 0, 0, 0};
-                }
-            }
+            for (int i = 0; i < NT; ++i) s_b[j & 1][to[i]] = k0 + k8[i] < (uint32_t)K ? staged[i] : v4u{0, 0, 0, 0};
+        };
+        const auto operand = [&](int j, int h, int t) {
+            if constexpr (KMAJOR) {                      // sixteen lanes read four rows of the tile, each of them gets a column
+                const char* at = reinterpret_cast<const char*>(s_b[j & 1]) + (32 * h + 8 * kg + (lr >> 2)) * PITCH + 32 * t + 8 * (lr & 3);
+                return read_transposed(at, at + 4 * PITCH);
+            } else return s_b[j & 1][(h * NT + t) * 64 + operand_slot(lr, kg)];
         };
         v4f acc[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
         const auto multiply = [&](v4u (&x)[4], int j) {
             const uint32_t k0 = k_of(j);
-            if (k0 + KS > (uint32_t)K) {
-#pragma unroll
-                for (int h = 0; h < 4; ++h)
-                    if (k0 + h * 32 + kg * 8 >= (uint32_t)K) x[h] = v4u{0, 0, 0, 0};
-            }
             v4u q[2][NT];                                // one instruction's operands while the other's are multiplied
-            const int slot = operand_slot(lr, kg);
+            // from as they are loaded to as they are multiplied, through the wavefront's own part of LDS
+            if constexpr (KMAJOR) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) q[0][t] = s_b[j & 1][0][t][slot];
+                for (int h = 0; h < 4; ++h) s_x[wave][4 * h + kg][lr ^ (kg + 4 * (h & 1))] = x[h];
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int h = 0; h < 4; ++h) x[h] = s_x[wave][lr][(4 * h + kg) ^ (lr & 7)];
+                __builtin_amdgcn_wave_barrier();
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) q[0][t] = operand(j, 0, t);
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 if (h < 3) {
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) q[(h + 1) & 1][t] = s_b[j & 1][h + 1][t][slot];
+                    for (int t = 0; t < NT; ++t) q[(h + 1) & 1][t] = operand(j, h + 1, t);
                 }
                 in_order();
+                x[h] = k0 + h * 32 + kg * 8 < (uint32_t)K ? x[h] : v4u{0, 0, 0, 0};
                 if (DROP) x[h] = drop_eight(g.drop, x[h], token, ((k0 + h * 32) >> 3) + kg);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) acc[t] = mfma(x[h], q[h & 1][t], acc[t]);
                 in_order();
             }
         };
+        __syncthreads();                                 // the adapter before may still be read
         // Step j: the adapter's part, on its way since the step before, goes to LDS, that of the next step is asked for, and the rows of the
         // step after the next as soon as this one's registers are free.
         const auto step = [&](v4u (&x)[4], int j) {
@@ -385,8 +431,8 @@ thin_rows_kernel(ThinArgs g) {
             load_staged(j + 1);
             multiply(x, j);
             load_x(x, j + 2);
+            in_order();
         };
-        __syncthreads();                                 // the adapter before may still be read
         load_staged(0);                                  // first: it is waited for first
         in_order();
         load_x(x[0], 0);
@@ -420,7 +466,7 @@ thin_rows_kernel(ThinArgs g) {
 
 // ------------------------------------------------------------------------------------------------ launches
 constexpr int64_t kManyTokens = 1024;                    // from here on thin_rows_kernel
-constexpr int64_t kFill = 512;                           // workgroups that fill the chip
+constexpr int64_t kFill = 512, kCompute = 256;           // workgroups that fill the chip, and its compute units
 
 int64_t extra_blocks(const AdapterPool& p, const BackwardExtras& x, int threads) {
     return x.groups + (x.kept ? ceil_div(kept_words(p.b, p.m), threads) : 0);
@@ -431,8 +477,10 @@ void launch_as(ThinArgs g, const ThinPlan& q, hipStream_t s) {
     const bool drop = !KMAJOR && g.drop.least;
     const int threads = 64 * (q.rows ? kRowWaves : kFewWaves);
     g.tiles = (int)ceil_div(g.p.b, q.rows ? kRowTile : 16);
-    const int64_t extra = KMAJOR ? ceil_div(extra_blocks(g.p, g.extras, threads), q.splits * q.lanes) : 0;
-    const dim3 grid((unsigned)(g.tiles + extra), q.splits, q.lanes), block(threads);
+    g.splits = q.splits;
+    g.lanes = q.lanes;
+    const int64_t all = (int64_t)g.tiles * q.splits * q.lanes + (KMAJOR ? extra_blocks(g.p, g.extras, threads) : 0);
+    const dim3 grid((unsigned)all), block(threads);
     if (q.rows && drop) hipLaunchKernelGGL((thin_rows_kernel<NT, KMAJOR, !KMAJOR>), grid, block, 0, s, g);
     else if (q.rows) hipLaunchKernelGGL((thin_rows_kernel<NT, KMAJOR, false>), grid, block, 0, s, g);
     else if (drop) hipLaunchKernelGGL((thin_few_kernel<NT, KMAJOR, !KMAJOR>), grid, block, 0, s, g);
@@ -450,8 +498,7 @@ void launch_by_rank(const ThinArgs& g, const ThinPlan& q, hipStream_t s) {
 
 }  // namespace
 
-ThinPlan thin_plan(int64_t b, int64_t K, int slots, int max_rank) {
-    (void)max_rank;
+ThinPlan thin_plan(int64_t b, int64_t K, int slots) {
     ThinPlan q;
     q.rows = b >= kManyTokens;
     const int64_t tiles = ceil_div(b, q.rows ? kRowTile : 16);
@@ -460,14 +507,17 @@ ThinPlan thin_plan(int64_t b, int64_t K, int slots, int max_rank) {
     if (slots < most) most = slots;
     const int64_t chunks = ceil_div(K, q.rows ? 128 : 64 * kFewWaves);
     int64_t splits = 0;
-    if (q.rows) {                                        // first the reduction is split, then the adapters are
-        splits = kFill / (tiles > 0 ? tiles : 1);
-        if (splits > 8) splits = 8;
-        if (splits > chunks) splits = chunks;
+    if (q.rows) {
+        // One workgroup a compute unit, and room beside it for a tile's other adapters, which are other workgroups' from the beginning: done
+        // by one after the other they made the tiles at the requests' borders twice as long as all (58 us instead of 39 at 8192 tokens,
+        // K = 4096, rank 64, dropout).  More splits than four cost more where their parts are summed than they give here.
+        splits = kCompute / (tiles > 0 ? tiles : 1);
+        if (splits > 4) splits = 4;
+        if (splits > chunks / 3) splits = chunks / 3;
         if (splits < 1) splits = 1;
         int64_t lanes = kFill / ((tiles > 0 ? tiles : 1) * splits);
-        if (lanes > most) lanes = most;
-        q.lanes = lanes < 1 ? 1 : (int)lanes;
+        if (lanes < 4) lanes = 4;
+        q.lanes = (int)(lanes < most ? lanes : most);
     } else {                                             // few tokens: one for each adapter that there may be
         q.lanes = b <= 256 ? (int)(most < 1 ? 1 : most) : 1;
         splits = kFill / (tiles * q.lanes > 0 ? tiles * q.lanes : 1);

@@ -147,8 +147,8 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || (RC_ == 4 && BWD) ? 
 wide_kernel(WideArgs g) {
     constexpr bool STACK = RC_ == 0;
     constexpr int RC = STACK ? 1 : RC_, NP = STACK ? 2 : 3, ROWS = 16 * MT, WORDS = (ROWS + 63) / 64;
-    constexpr int DEPTH = MT == 1 ? 1 : F32 || RC == 4 || (RC == 2 && BWD) ? 2 : 4;     // steps whose base is on its way
-    constexpr bool AHEAD = RC <= 2;                      // registers for two blocks of the adapter
+    constexpr int DEPTH = MT == 1 || (RC == 2 && BWD && F32) ? 1 : F32 || RC == 4 || (RC == 2 && BWD) ? 2 : 4;     // steps whose base is on its way
+    constexpr bool AHEAD = RC <= (MT == 1 ? 1 : 2);      // registers for two blocks of the adapter
     __shared__ v4u s_thin[MT * RC * NP][64];
     __shared__ int s_id[64 * WORDS];
     typedef AdapterBlock<RC_, BWD> Block;
@@ -228,9 +228,91 @@ wide_kernel(WideArgs g) {
     uint64_t bare[WORDS];
 #pragma unroll
     for (int w = 0; w < WORDS; ++w) bare[w] = ~todo[w];
+    struct Place { int j; uint32_t left; };          // block of features, and the steps left in it, this one the lowest
+    const auto after = [&](Place q) {
+        q.left &= q.left - 1;
+        if (!q.left) { ++q.j; q.left = steps; }
+        return q;
+    };
+    // Base and result go a pair of tokens at a time: lane (i, g) has run i % 2 of the even token, then of the odd one, so that eight lanes
+    // take 128 bytes of a row at once.  (Token by token, each half of a line was a request of its own: 137 us instead of 118 at 8192
+    // tokens, 14336 features, rank 64.)
+    struct Ahead {
+        Eight<F32> base[2];
+        uint32_t kept;                               // the lane's token's bits of both runs
+    };
+    Ahead ahead[DEPTH];
+    const auto load_ahead = [&](Ahead& x, const Place& q) {
+        const int i = __builtin_ctz(q.left);
+        const uint32_t f0 = f_of(q.j);
+        const int64_t at = (16 * i * base_ld + f0) * SIZE;
+        const char* instead = reinterpret_cast<const char*>(base_at) + (row0 + first) * base_ld * SIZE;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {                // no base, other adapters' tokens, features and steps beyond: one line for all
+            const bool ok = (own[k] & base_keep) >> i & 1 && f0 + run < (uint32_t)wide && q.j < count;
+            x.base[k].load(ok ? base_lane[k] + at : instead);
+        }
+        if constexpr (BWD) {
+            const uint32_t t = (uint32_t)(row0 + i * 16 + lr), tc = t < (uint32_t)p.b ? t : (uint32_t)p.b - 1;
+            x.kept = kept_all | load_at<uint16_t>(kept_at + (f0 >> 6) * kept_block, tc * kept_token + 2 * kg);
+        }
+    };
+    const auto work = [&](Ahead& x, const Place& q) {
+        const int i = __builtin_ctz(q.left);
+        v4f acc[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        v4u b[2][NP];                                // one rank chunk's operands while the other's are multiplied
+#pragma unroll
+        for (int k = 0; k < NP; ++k) b[0][k] = s_thin[i * RC * NP + k][lane];
+#pragma unroll
+        for (int c = 0; c < RC; ++c) {
+            if (c + 1 < RC) {
+#pragma unroll
+                for (int k = 0; k < NP; ++k) b[(c + 1) & 1][k] = s_thin[(i * RC + c + 1) * NP + k][lane];
+            }
+            in_order();
+#pragma unroll
+            for (int k = 0; k < NP; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = mfma(now.w[c][e], b[c & 1][k], acc[e]);
+        }
+        x.base[0].exchange(x.base[1], odd);
+        Eight<F32> y[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = Block::result(acc, k, e);
+                if (BWD) v[e] = __uint_as_float(__float_as_uint(v[e]) & bit_mask(x.kept, 8 * k + e));
+            }
+            x.base[k].add_to(v, base_keep);
+            y[k].set(v);
+        }
+        y[0].exchange(y[1], odd);
+        const uint32_t f0 = f_of(q.j);
+        const int64_t at = (16 * i * g.ld_out + f0) * SIZE;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if ((own[k] >> i) & 1 && f0 + run < (uint32_t)wide) y[k].store(out_lane[k] + at);
+    };
+    Place at{0, 0}, next{0, 0};
+    int rank = 0;
+    // What the adapter's first step takes, all on its way at once.
+    const auto begin = [&]() {
+        at = next = Place{0, steps};
+        now.load(adapter(), R, (uint32_t)wide, f_of(0), lr, r_lane);
+        rank = rank_of(p, a);
+        in_order();
+#pragma unroll
+        for (int k = 0; k < DEPTH; ++k, next = after(next)) load_ahead(ahead[k], next);
+        if (AHEAD) next_block.load(adapter(), R, (uint32_t)wide, f_of(1), lr, r_lane);
+    };
     next_adapter();
     if (a < 0 && blockIdx.z > 0) return;                 // the same for the workgroup
-    if (a >= 0) now.load(adapter(), R, (uint32_t)wide, f_of(0), lr, r_lane);
+    if (a >= 0) begin();
+    in_order();
 
     for (int j = wave; j < MT * RC; j += WAVES) {        // the thin values of the tile's tokens, in pieces
         const int i = j / RC, r = 32 * (j % RC) + r_lane;
@@ -280,83 +362,7 @@ wide_kernel(WideArgs g) {
         }
     }
 #pragma unroll 1
-    for (bool again = false; a >= 0; next_adapter(), again = true) {
-        struct Place { int j; uint32_t left; };          // block of features, and the steps left in it, this one the lowest
-        const auto after = [&](Place q) {
-            q.left &= q.left - 1;
-            if (!q.left) { ++q.j; q.left = steps; }
-            return q;
-        };
-        // Base and result go a pair of tokens at a time: lane (i, g) has run i % 2 of the even token, then of the odd one, so that eight lanes
-        // take 128 bytes of a row at once.  (Token by token, each half of a line was a request of its own: 137 us instead of 118 at 8192
-        // tokens, 14336 features, rank 64.)
-        struct Ahead {
-            Eight<F32> base[2];
-            uint32_t kept;                               // the lane's token's bits of both runs
-        };
-        Ahead ahead[DEPTH];
-        const auto load_ahead = [&](Ahead& x, const Place& q) {
-            const int i = __builtin_ctz(q.left);
-            const uint32_t f0 = f_of(q.j);
-            const int64_t at = (16 * i * base_ld + f0) * SIZE;
-            const char* instead = reinterpret_cast<const char*>(base_at) + (row0 + first) * base_ld * SIZE;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {                // other adapters' tokens, features beyond: the first of this one's
-                const bool ok = (own[k] >> i) & 1 && f0 + run < (uint32_t)wide;
-                x.base[k].load(ok ? base_lane[k] + at : instead);
-            }
-            if constexpr (BWD) {
-                const uint32_t t = (uint32_t)(row0 + i * 16 + lr), tc = t < (uint32_t)p.b ? t : (uint32_t)p.b - 1;
-                x.kept = kept_all | load_at<uint16_t>(kept_at + (f0 >> 6) * kept_block, tc * kept_token + 2 * kg);
-            }
-        };
-        const auto work = [&](Ahead& x, const Place& q) {
-            const int i = __builtin_ctz(q.left);
-            v4f acc[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) acc[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-            v4u b[2][NP];                                // one rank chunk's operands while the other's are multiplied
-#pragma unroll
-            for (int k = 0; k < NP; ++k) b[0][k] = s_thin[i * RC * NP + k][lane];
-#pragma unroll
-            for (int c = 0; c < RC; ++c) {
-                if (c + 1 < RC) {
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) b[(c + 1) & 1][k] = s_thin[(i * RC + c + 1) * NP + k][lane];
-                }
-                in_order();
-#pragma unroll
-                for (int k = 0; k < NP; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[e] = mfma(now.w[c][e], b[c & 1][k], acc[e]);
-            }
-            x.base[0].exchange(x.base[1], odd);
-            Eight<F32> y[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] = Block::result(acc, k, e);
-                    if (BWD) v[e] = __uint_as_float(__float_as_uint(v[e]) & bit_mask(x.kept, 8 * k + e));
-                }
-                x.base[k].add_to(v, base_keep);
-                y[k].set(v);
-            }
-            y[0].exchange(y[1], odd);
-            const uint32_t f0 = f_of(q.j);
-            const int64_t at = (16 * i * g.ld_out + f0) * SIZE;
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-                if ((own[k] >> i) & 1 && f0 + run < (uint32_t)wide) y[k].store(out_lane[k] + at);
-        };
-        Place at{0, steps}, next = at;
-        if (again) now.load(adapter(), R, (uint32_t)wide, f_of(0), lr, r_lane);
-        in_order();
-#pragma unroll
-        for (int k = 0; k < DEPTH; ++k, next = after(next)) load_ahead(ahead[k], next);
-        if (AHEAD) next_block.load(adapter(), R, (uint32_t)wide, f_of(1), lr, r_lane);
-        const int rank = rank_of(p, a);
+    while (a >= 0) {
         now.finish(rank, r_lane);
 #pragma unroll 1
         while (at.j < count) {
@@ -376,6 +382,8 @@ wide_kernel(WideArgs g) {
                 }
             }
         }
+        next_adapter();
+        if (a >= 0) begin();
     }
 }
 
@@ -396,6 +404,13 @@ void launch_as(const WideArgs& g, bool f32, int64_t wanted, hipStream_t s) {
     }
     int64_t y = ceil_div(wanted, tiles * lanes);
     if (y > strips) y = strips;
+    if (MT >= 4) {                                       // the shortest by the rounds of workgroups and the steps of each, its start like four
+        int64_t least = INT64_MAX;
+        for (int64_t k = 1; k <= strips && k <= 64; ++k) {
+            const int64_t cost = ceil_div(tiles * k, kFill) * (ceil_div(blocks, k) * MT + 4 * WAVES);
+            if (cost < least) { least = cost; y = k; }
+        }
+    }
     y = ceil_div(blocks, ceil_div(blocks, y));
     const dim3 grid((unsigned)tiles, (unsigned)y, (unsigned)lanes), block(64 * WAVES);
     if (f32) hipLaunchKernelGGL((wide_kernel<RC, MT, WAVES, BWD, true>), grid, block, 0, s, g);
