@@ -170,6 +170,17 @@ struct Segment {
     int part;                // where its sum goes: -1: it is the adapter's only segment, straight to the result
 };
 
+// The segments of an adapter with so many tokens: as few as are no longer than chunk, equally long but for the last.
+struct Pieces {
+    int count, size;
+    __device__ __forceinline__ Pieces(int tokens, int chunk) {
+        count = tokens > chunk ? (tokens + chunk - 1) / chunk : 1;
+        size = ((tokens + 31) / 32 + count - 1) / count * 32;
+        if (size > 0) count = (tokens + size - 1) / size;
+    }
+};
+
+
 struct GroupArgs {
     int chunk, cuts;         // cuts: ceil(places / chunk)
     int* order;
@@ -234,7 +245,7 @@ struct GradArgs {
     float factor;
 };
 // Places between two cuts.
-int grad_chunk(int64_t places, int64_t m, int64_t n, int slots, int max_rank);
+int grad_chunk(int64_t places, int64_t m, int64_t n, int max_rank);
 // Sums that have a place of their own among a job's parts.
 inline int64_t grad_parts(int64_t cuts) { return cuts > 1 ? 2 * cuts + 1 : 0; }
 hipError_t launch_grads(const GradArgs& g, hipStream_t s);

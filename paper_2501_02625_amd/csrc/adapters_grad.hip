@@ -11,15 +11,19 @@ namespace adapters {
 namespace {
 
 // The sum over a segment's tokens of big[t, col] * small[t, c]: big bf16 (E for G_V, drop(X) for G_U), small fp32 (T, S).  A workgroup owns 256
-// columns of `big`, a wavefront 64, and goes over the places 32 at a time.  k of the matrix instructions is the place: lane l supplies the
-// eight places 8 (l / 16) .. + 8 of the step.  `big` is read four neighbouring columns of a token at a time; the v-th of them, packed over
-// the eight tokens, is the first operand of the v-th instruction, which covers the columns 4 i + v.  The step's part of `small` is fetched by
-// the four wavefronts together and staged in LDS in pieces, two steps in turn.  NT: rank tiles of 16, from tile blockIdx.z * NT on.
+// columns of `big`, a wavefront 64, and goes over the places 32 at a time; k of the matrix instructions is the place.  Both operands are loaded
+// as they lie, 16 bytes a lane, and turned in LDS: a lane has eight columns of four places of `big`, masked before they go to the wavefront's
+// own part of LDS, and four columns of places of `small`, which the four wavefronts stage together, in pieces, two steps in turn.  What is
+// multiplied is read from there by the instruction that turns four rows of sixteen values.  (Loaded 8 and 4 bytes a lane as the instructions'
+// lanes want them, which needs no turning, it was XX us instead of YY at 8192 places, 14336 + 4096 columns, rank 64, masked: the vector memory
+// unit takes as long for an instruction of 4 bytes a lane as for one of 16.)  NT: rank tiles of 16, from tile blockIdx.z * NT on.
 template <int NT, bool MASK>
 __global__ void __launch_bounds__(64 * kGradWaves, 2)
 grad_kernel(GradArgs g) {
-    constexpr int THREADS = 64 * kGradWaves, UNITS = NT * 64;            // eight values of a column: staging, at most one per thread
-    __shared__ v4u s_small[2][NT * 3][64];
+    constexpr int THREADS = 64 * kGradWaves, UNITS = 128 * NT, PER = (UNITS + THREADS - 1) / THREADS;     // fours of staging, and per thread
+    // bytes from one place to the next: so many more than the values that four of a tile lie in all the banks
+    constexpr int BIG = 128 + 32, SMALL = 32 * NT + (NT > 1 ? 32 : 0);
+    __shared__ v4u s_big[kGradWaves][32 * BIG / 16], s_small[2][3][32 * SMALL / 16];
     const Segment seg = g.group.segments[blockIdx.y];
     if (seg.adapter < 0) return;
     const bool second = (int)blockIdx.x >= g.job[0].tiles;
@@ -30,11 +34,17 @@ grad_kernel(GradArgs g) {
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
     const int i16 = lane & 15, kq = lane >> 4;
     const int64_t c0 = (int64_t)((int)blockIdx.x - (second ? g.job[0].tiles : 0)) * kGradCols + wave * 64;
-    const int64_t col = c0 + 4 * i16, colc = col < wide ? col : 0;       // columns beyond the matrix are not stored
+    // loading: eight columns of the places 4 (lane / 8) .. + 4; columns beyond the matrix are not stored
+    const int c8 = lane & 7, four = lane >> 3;
+    const int64_t col = c0 + 8 * c8, colc = col < wide ? col : 0;
     const bool masked = MASK && second;
     const uint16_t* big = job.big + colc;
-    const uint8_t* kept_at = MASK && masked ? g.kept + (c0 < wide ? c0 >> 6 : 0) * p.b * 8 + (i16 >> 1) : nullptr;
+    const uint8_t* kept_at = MASK && masked ? g.kept + (c0 < wide ? c0 >> 6 : 0) * p.b * 8 + c8 : nullptr;
     const uint32_t last = (uint32_t)p.b - 1, pitch = 2 * (uint32_t)job.ld;       // bytes
+    char* const big_put = reinterpret_cast<char*>(s_big[wave]) + 4 * four * BIG + 16 * c8;
+    // turning: lane l of sixteen names the four values l % 4 of the place l / 4 and gets the l-th of all four
+    const char* const big_get = reinterpret_cast<const char*>(s_big[wave]) + (8 * kq + (i16 >> 2)) * BIG + 8 * (i16 & 3);
+    const int small_get = (8 * kq + (i16 >> 2)) * SMALL + 8 * (i16 & 3);
 
     v4f acc[NT][4];
 #pragma unroll
@@ -45,79 +55,89 @@ grad_kernel(GradArgs g) {
     const auto sum = [&](auto with_mask) {
         constexpr bool M = decltype(with_mask)::value;
         struct Step {
-            int token[8];
-            uint2 raw[8];
-            uint32_t kept[8];
+            int token[4];
+            v4u raw[4];
+            uint32_t kept[4];
         };
         const int steps = (seg.end - seg.begin + 31) >> 5;
-        const auto load_order = [&](int (&token)[8], int j) {
-            const int4* o = reinterpret_cast<const int4*>(g.group.order + seg.begin + 32 * (j < steps ? j : 0) + 8 * kq);
-            const int4 lo = o[0], hi = o[1];
-            token[0] = lo.x; token[1] = lo.y; token[2] = lo.z; token[3] = lo.w;
-            token[4] = hi.x; token[5] = hi.y; token[6] = hi.z; token[7] = hi.w;
-        };
+        const int* order = g.group.order + seg.begin;
+        const auto place0 = [&](int j) { return 32 * (j < steps ? j : 0); };
+        const auto row_of = [&](int token) { return (uint32_t)token < last ? (uint32_t)token : last; };
+        const auto load_order = [&](int4& token, int j) { token = *reinterpret_cast<const int4*>(order + place0(j) + 4 * four); };
         // A place without a token (-1) loads the last one's row.  Only an adapter's last step has such places; there they are set to zero.
-        const auto load_rows = [&](Step& q, const int (&token)[8]) {
+        const auto load_rows = [&](Step& q, const int4& token) {
+            q.token[0] = token.x; q.token[1] = token.y; q.token[2] = token.z; q.token[3] = token.w;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const uint32_t t = (uint32_t)token[u] < last ? (uint32_t)token[u] : last;
-                q.token[u] = token[u];
-                q.raw[u] = *reinterpret_cast<const uint2*>(reinterpret_cast<const char*>(big) + (uint64_t)t * pitch);
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t t = row_of(q.token[u]);
+                q.raw[u] = *reinterpret_cast<const v4u*>(reinterpret_cast<const char*>(big) + (uint64_t)t * pitch);
                 if (M) q.kept[u] = kept_at[t * 8];
             }
         };
-        // thread (rank tile, lane) stages what that lane multiplies with
-        const int unit = tid % UNITS, small_c = (tile0 + (unit >> 6)) * 16 + (unit & 15);
-        const uint32_t small_at = 4 * (small_c < R ? small_c : 0);
-        float staged[8];
-        const auto load_staged = [&](const int (&token)[8]) {
+        // the thread's fours of `small`, i = 0 .. PER
+        const int c4 = tid % (4 * NT), staged_c = 16 * tile0 + 4 * c4;
+        const uint32_t small_at = 4 * (staged_c < R ? staged_c : 0);     // columns beyond the rank are not stored
+        int staged_token[PER];
+        v4f staged[PER];
+        const auto load_staged_order = [&](int j) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const uint32_t t = (uint32_t)token[u] < last ? (uint32_t)token[u] : last;
-                staged[u] = load_at<float>(job.small, __umul24(t, 4 * R) + small_at);        // at most 2^31 bytes
+            for (int i = 0; i < PER; ++i) staged_token[i] = order[place0(j) + (tid + i * THREADS) % UNITS / (4 * NT)];
+        };
+        const auto load_staged = [&](int (&token)[PER]) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                token[i] = staged_token[i];
+                staged[i] = load_at<v4f>(job.small, __umul24(row_of(token[i]), 4 * R) + small_at);         // at most 2^31 bytes
             }
         };
-        const auto write_staged = [&](const int (&token)[8], int j) {
-            if (j == steps - 1) {
+        const auto write_staged = [&](const int (&token)[PER], int j) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    if (token[u] < 0) staged[u] = 0.0f;
-            }
-            v4u q[3];
-            split_eight(staged, q);
-            if (UNITS % THREADS == 0 || tid < UNITS) {
+            for (int i = 0; i < PER; ++i) {
+                v4f x = staged[i];
+                if (j == steps - 1) {
 #pragma unroll
-                for (int k = 0; k < 3; ++k) s_small[j & 1][(unit >> 6) * 3 + k][lane] = q[k];
-            }
-        };
-        const auto multiply = [&](const Step& q, int j) {
-            uint2 x[8];
+                    for (int e = 0; e < 4; ++e) x[e] = token[i] < 0 ? 0.0f : x[e];
+                }
+                uint32_t piece[3][4];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = q.raw[u];
-            if (M) {
-                const int low = 4 * (i16 & 1);
+                for (int e = 0; e < 4; ++e) split3(x[e], piece[0][e], piece[1][e], piece[2][e]);
+                const int at = (tid + i * THREADS) / (4 * NT) * SMALL + 8 * c4;
+                if (UNITS % THREADS == 0 || tid < UNITS) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const uint32_t kept = q.kept[u] >> low;
-                    x[u].x &= pack_lo(bit_mask(kept, 0), bit_mask(kept, 1));
-                    x[u].y &= pack_lo(bit_mask(kept, 2), bit_mask(kept, 3));
+                    for (int k = 0; k < 3; ++k)
+                        *reinterpret_cast<uint2*>(reinterpret_cast<char*>(s_small[j & 1][k]) + at) =
+                            make_uint2(pack_hi(piece[k][0], piece[k][1]), pack_hi(piece[k][2], piece[k][3]));
                 }
             }
-            if (j == steps - 1) {
+        };
+        const auto operand = [&](int j, int k, int t) {
+            const char* at = reinterpret_cast<const char*>(s_small[j & 1][k]) + small_get + 32 * t;
+            return read_transposed(at, at + 4 * SMALL);
+        };
+        const auto multiply = [&](const Step& q, int j) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    if (q.token[u] < 0) x[u] = make_uint2(0, 0);
+            for (int u = 0; u < 4; ++u) {
+                v4u x = q.raw[u];
+                if (M) {
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) x[d] &= pack_lo(bit_mask(q.kept[u], 2 * d), bit_mask(q.kept[u], 2 * d + 1));
+                }
+                if (j == steps - 1) x = q.token[u] < 0 ? v4u{0, 0, 0, 0} : x;
+                *reinterpret_cast<v4u*>(big_put + u * BIG) = x;
             }
+            __builtin_amdgcn_wave_barrier();
             v4u a[4];
-            columns_of(x, a);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) a[v] = read_transposed(big_get + 32 * v, big_get + 32 * v + 4 * BIG);
             v4u b[2][3];                                     // one rank tile's operands while the other's are multiplied
 #pragma unroll
-            for (int k = 0; k < 3; ++k) b[0][k] = s_small[j & 1][k][lane];
+            for (int k = 0; k < 3; ++k) b[0][k] = operand(j, k, 0);
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 if (t + 1 < NT) {
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) b[(t + 1) & 1][k] = s_small[j & 1][(t + 1) * 3 + k][lane];
+                    for (int k = 0; k < 3; ++k) b[(t + 1) & 1][k] = operand(j, k, t + 1);
                 }
                 in_order();
 #pragma unroll
@@ -128,13 +148,15 @@ grad_kernel(GradArgs g) {
             }
         };
         Step even, odd;
-        int even_next[8], odd_next[8];                       // tokens of the steps whose rows are asked for next
+        int4 even_next, odd_next;                            // tokens of the steps whose rows are asked for next
+        int staged_now[PER];
         // Step j: its part of `small`, on its way since the step before, goes to LDS, that of the next is asked for, and the rows of the step after
         // the next as soon as this one's are used, by tokens that were asked for a step ago, ahead of that step's rows.
-        const auto step = [&](Step& q, const int (&q_next)[8], const Step& other, int (&other_next)[8], int j) {
-            write_staged(q.token, j);
+        const auto step = [&](Step& q, const int4& q_next, int4& other_next, int j) {
+            write_staged(staged_now, j);
             __syncthreads();
-            load_staged(other.token);
+            load_staged(staged_now);
+            load_staged_order(j + 2);
             multiply(q, j);
             load_order(other_next, j + 3);
             in_order();
@@ -142,22 +164,24 @@ grad_kernel(GradArgs g) {
             in_order();
         };
         if (steps > 0) {                                     // the same for the workgroup
+            load_staged_order(0);
             load_order(even_next, 0);
             load_order(odd_next, 1);
+            load_staged(staged_now);
+            load_staged_order(1);
             load_rows(even, even_next);
             in_order();
-            load_staged(even.token);
             load_order(even_next, 2);
             in_order();
             load_rows(odd, odd_next);
             in_order();
 #pragma unroll 1
             for (int j = 0; j + 1 < steps; j += 2) {
-                step(even, even_next, odd, odd_next, j);
-                step(odd, odd_next, even, even_next, j + 1);
+                step(even, even_next, odd_next, j);
+                step(odd, odd_next, even_next, j + 1);
             }
             if (steps & 1) {
-                write_staged(even.token, steps - 1);
+                write_staged(staged_now, steps - 1);
                 __syncthreads();
                 multiply(even, steps - 1);
             }
@@ -180,14 +204,14 @@ grad_kernel(GradArgs g) {
     for (int t = 0; t < NT; ++t) {
         const int c = (tile0 + t) * 16 + i16;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t oc = c0 + 4 * (4 * kq + e);
+        for (int v = 0; v < 4; ++v) {
+            const int64_t oc = c0 + 16 * v + 4 * kq;
             if (oc >= wide || c >= R) continue;
             if (rank_major) {
-                *reinterpret_cast<v4f*>(dst + (int64_t)c * wide + oc) = v4f{acc[t][0][e], acc[t][1][e], acc[t][2][e], acc[t][3][e]};
+                *reinterpret_cast<v4f*>(dst + (int64_t)c * wide + oc) = acc[t][v];
             } else {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) dst[(oc + v) * R + c] = acc[t][v][e];
+                for (int e = 0; e < 4; ++e) dst[(oc + e) * R + c] = acc[t][v][e];
             }
         }
     }
@@ -198,7 +222,7 @@ __global__ void __launch_bounds__(256)
 grad_join_kernel(AdapterPool p, GroupArgs group, GradJob v, GradJob u) {
     const int a = blockIdx.y;
     const int2 range = group.range[a];
-    const int first = range.x / group.chunk, count = range.y > range.x ? (range.y + group.chunk - 1) / group.chunk - first : 1;
+    const int first = range.x / group.chunk, count = Pieces(range.y - range.x, group.chunk).count;
     if (count == 1) return;
     const int64_t size_v = v.tiles ? v.wide * p.max_rank : 0, size_u = u.tiles ? u.wide * p.max_rank : 0;
     int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -231,14 +255,11 @@ void launch_as(const GradArgs& g, hipStream_t s) {
 
 }  // namespace
 
-// Segments there are as many as adapters with tokens plus cuts, less one; together with the column tiles they should fill the chip once: every
-// further one costs a partial sum that is written and read again.  How many adapters have tokens is not known here: as if all had, but cut
-// at least half as often as one adapter alone would be.  A segment is at least 256 places and long next to its partial sum.
-int grad_chunk(int64_t places, int64_t m, int64_t n, int slots, int max_rank) {
+// Segments are cut so that together with the column tiles they fill the chip once: every further one costs a partial sum that is written and
+// read again.  A segment of several is at least 256 places and long next to its partial sum.
+int grad_chunk(int64_t places, int64_t m, int64_t n, int max_rank) {
     const int64_t tiles = ceil_div(m, kGradCols) + ceil_div(n, kGradCols), wanted = kFill > tiles ? kFill / tiles : 1;
-    int64_t cuts = wanted - slots + 1;
-    if (cuts < (wanted + 1) / 2) cuts = (wanted + 1) / 2;
-    int64_t chunk = ceil_div(places, cuts), least = 8 * max_rank < 256 ? 256 : 8 * max_rank;
+    int64_t chunk = ceil_div(places, wanted), least = 8 * max_rank < 256 ? 256 : 8 * max_rank;
     if (chunk < least) chunk = least;
     return (int)(ceil_div(chunk, 32) * 32);
 }

@@ -24,8 +24,9 @@ struct TileAdapters {
     }
 };
 
-// One adapter's tokens, written down by a workgroup.  A segment that is not alone begins or ends at a cut k: its sum goes to part k (it begins
-// there) or cuts + k (it is the first one, and ends there).
+// One adapter's tokens, written down by a workgroup.  There is a cut at every chunk-th place, and an adapter of several segments, which are
+// equally long, has at least as many cuts among its places as segments but the first: these sum into the parts of those cuts k, in order, and
+// the first one into cuts + k of the first of them.
 template <int THREADS>
 __device__ __forceinline__ void group_tokens(const AdapterPool& p, const GroupArgs& g, int a) {
     constexpr int WAVES = THREADS / 64, AHEAD = 8;       // loads on their way at once: there is nothing else to wait for them with
@@ -55,16 +56,16 @@ __device__ __forceinline__ void group_tokens(const AdapterPool& p, const GroupAr
     const int begin = (less + 31) / 32 * 32 + 32 * a, end = begin + same;
     if (tid == 0) g.range[a] = make_int2(begin, end);
     const int after = (less + same + 31) / 32 * 32 + 32 * (a + 1);     // where the next adapter begins
-    const int count = same ? (end + chunk - 1) / chunk - begin / chunk : 1;
+    const Pieces pieces(same, chunk);
     const int index = a + begin / chunk, next = a == p.slots - 1 ? p.slots + g.cuts : a + 1 + after / chunk;
     for (int i = tid; index + i < next; i += THREADS) {
         Segment q{-1, 0, 0, -1};
-        if (i < count) {
-            const int cut = begin / chunk + i;           // the segment lies between this cut and the next
+        if (i < pieces.count) {
+            const int cut = begin / chunk + i;
             q.adapter = a;
-            q.begin = i == 0 ? begin : cut * chunk;
-            q.end = i == count - 1 ? end : (cut + 1) * chunk;
-            q.part = count == 1 ? -1 : i == 0 ? g.cuts + cut + 1 : cut;
+            q.begin = begin + i * pieces.size;
+            q.end = i == pieces.count - 1 ? end : q.begin + pieces.size;
+            q.part = pieces.count == 1 ? -1 : i == 0 ? g.cuts + cut + 1 : cut;
         }
         g.segments[index + i] = q;
     }
