@@ -20,7 +20,7 @@ BwdLayout bwd_layout(int64_t b, int64_t m, int64_t n, int slots, int R, bool dro
     BwdLayout L;
     const int64_t places = (b + 31) / 32 * 32 + 32 * (int64_t)slots;
     L.plan = thin_plan(b, n, slots);
-    L.chunk = grad_chunk(places, m, n, R);
+    L.chunk = grad_chunk(b, places, m, n, R);
     L.cuts = (int)ceil_div(places, L.chunk);
     size_t at = 0;
     const auto take = [&at](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };

@@ -245,7 +245,7 @@ struct GradArgs {
     float factor;
 };
 // Places between two cuts.
-int grad_chunk(int64_t places, int64_t m, int64_t n, int max_rank);
+int grad_chunk(int64_t b, int64_t places, int64_t m, int64_t n, int max_rank);
 // Sums that have a place of their own among a job's parts.
 inline int64_t grad_parts(int64_t cuts) { return cuts > 1 ? 2 * cuts + 1 : 0; }
 hipError_t launch_grads(const GradArgs& g, hipStream_t s);

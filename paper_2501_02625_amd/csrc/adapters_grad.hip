@@ -256,11 +256,12 @@ void launch_as(const GradArgs& g, hipStream_t s) {
 }  // namespace
 
 // Segments are cut so that together with the column tiles they fill the chip once: every further one costs a partial sum that is written and
-// read again.  A segment of several is at least 256 places and long next to its partial sum.
-int grad_chunk(int64_t places, int64_t m, int64_t n, int max_rank) {
+// read again.  Few tokens have little to be read: a segment of several is at least 64 places, and its partial sum as much as what it reads.
+int grad_chunk(int64_t b, int64_t places, int64_t m, int64_t n, int max_rank) {
     const int64_t tiles = ceil_div(m, kGradCols) + ceil_div(n, kGradCols), wanted = kFill > tiles ? kFill / tiles : 1;
-    int64_t chunk = ceil_div(places, wanted), least = 8 * max_rank < 256 ? 256 : 8 * max_rank;
+    int64_t chunk = ceil_div(places, wanted), least = 2 * max_rank < 64 ? 64 : 2 * max_rank;
     if (chunk < least) chunk = least;
+    if (b <= 256) chunk = places;                        // the sums' own launch would cost more
     return (int)(ceil_div(chunk, 32) * 32);
 }
 

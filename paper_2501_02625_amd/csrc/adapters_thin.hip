@@ -151,9 +151,10 @@ struct Place { int64_t extra; int tile, split, lane; };
 
 template <bool KMAJOR>
 __device__ __forceinline__ Place place_of(const ThinArgs& g) {
-    const unsigned groups = KMAJOR ? g.extras.groups : 0, tiles = (unsigned)(g.tiles * g.splits) * g.lanes, i = blockIdx.x - groups;
-    if (KMAJOR && blockIdx.x < groups) return Place{(int64_t)blockIdx.x, 0, 0, 0};
-    if (KMAJOR && i >= tiles) return Place{(int64_t)blockIdx.x - tiles, 0, 0, 0};
+    if (!KMAJOR) return Place{-1, (int)blockIdx.x, (int)blockIdx.y, (int)blockIdx.z};      // the same order, and nothing to divide by
+    const unsigned groups = g.extras.groups, tiles = (unsigned)(g.tiles * g.splits) * g.lanes, i = blockIdx.x - groups;
+    if (blockIdx.x < groups) return Place{(int64_t)blockIdx.x, 0, 0, 0};
+    if (i >= tiles) return Place{(int64_t)blockIdx.x - tiles, 0, 0, 0};
     const unsigned j = i / (unsigned)g.tiles;
     return Place{-1, (int)(i - j * g.tiles), (int)(j % (unsigned)g.splits), (int)(j / (unsigned)g.splits)};
 }
@@ -480,8 +481,8 @@ void launch_as(ThinArgs g, const ThinPlan& q, hipStream_t s) {
     g.tiles = (int)ceil_div(g.p.b, q.rows ? kRowTile : 16);
     g.splits = q.splits;
     g.lanes = q.lanes;
-    const int64_t all = (int64_t)g.tiles * q.splits * q.lanes + (KMAJOR ? extra_blocks(g.p, g.extras, threads) : 0);
-    const dim3 grid((unsigned)all), block(threads);
+    const int64_t all = (int64_t)g.tiles * q.splits * q.lanes + extra_blocks(g.p, g.extras, threads);
+    const dim3 grid = KMAJOR ? dim3((unsigned)all) : dim3(g.tiles, q.splits, q.lanes), block(threads);
     if (q.rows && drop) hipLaunchKernelGGL((thin_rows_kernel<NT, KMAJOR, !KMAJOR>), grid, block, 0, s, g);
     else if (q.rows) hipLaunchKernelGGL((thin_rows_kernel<NT, KMAJOR, false>), grid, block, 0, s, g);
     else if (drop) hipLaunchKernelGGL((thin_few_kernel<NT, KMAJOR, !KMAJOR>), grid, block, 0, s, g);
@@ -519,9 +520,11 @@ ThinPlan thin_plan(int64_t b, int64_t K, int slots) {
         int64_t lanes = kFill / ((tiles > 0 ? tiles : 1) * splits);
         if (lanes < 4) lanes = 4;
         q.lanes = (int)(lanes < most ? lanes : most);
-    } else {                                             // few tokens: one for each adapter that there may be
-        q.lanes = b <= 256 ? (int)(most < 1 ? 1 : most) : 1;
-        splits = kFill / (tiles * q.lanes > 0 ? tiles * q.lanes : 1);
+    } else {                                             // few tokens: one for each adapter that there may be; or for the second
+        if (b > 256 && most > 2) most = 2;
+        q.lanes = (int)(most < 1 ? 1 : most);
+        const int64_t busy = b <= 256 ? tiles * q.lanes : tiles;
+        splits = kFill / (busy > 0 ? busy : 1);
         if (splits > 8) splits = 8;
         if (splits > chunks) splits = chunks;
         if (splits < 1) splits = 1;

@@ -399,6 +399,7 @@ void launch_as(const WideArgs& g, bool f32, int64_t wanted, hipStream_t s) {
         if (g.p.b < most) most = g.p.b;
         if (g.p.slots < most) most = g.p.slots;
         lanes = g.p.b <= 256 ? most : wanted / (tiles * strips);
+        if (MT == 1 && lanes < 2) lanes = 2;             // for the tiles with a request's border
         if (lanes > most) lanes = most;
         if (lanes < 1) lanes = 1;
     }
@@ -423,7 +424,7 @@ void launch_by_size(const WideArgs& g, bool f32, hipStream_t s) {
     const int64_t strips = ceil_div(BWD ? g.p.m : g.p.n, 512);
     constexpr int WAVES = RC == 4 && BWD ? 4 : 8;        // registers
     if (ceil_div(g.p.b, 16 * TALL) * strips >= kFill) launch_as<RC, TALL, WAVES, BWD>(g, f32, kFill, s);
-    else if (ceil_div(g.p.b, 64) * strips >= kFill / 2) launch_as<RC, 4, WAVES, BWD>(g, f32, 2 * kFill, s);
+    else if (ceil_div(g.p.b, 64) * strips >= 2 * kFill) launch_as<RC, 4, WAVES, BWD>(g, f32, 2 * kFill, s);
     else launch_as<RC, 1, 4, BWD>(g, f32, 4 * kFill, s);
 }
 
