@@ -1,0 +1,113 @@
+"""Several low-rank adapters trained and served together on one frozen INT8 projection.
+
+Every request has its own adapter, all of them share the projection, which is quantised once:
+
+    training    Y = X W^T (INT8) + the tokens' adapters of drop(X);  out = residual + drop(Y); and back, for all adapters in one call
+    serving     the same without dropout, a batch of single tokens, each with its own adapter
+
+Run: python examples/many_adapters.py
+"""
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2501_02625_amd import binding  # noqa: E402
+
+
+class Layer:
+    """residual + drop(X W^T + scale_a drop(X) U_a^T V_a^T), W frozen, a the adapter of each token."""
+
+    def __init__(self, W, slots, rank, p, seed):
+        n, m = W.shape
+        g = torch.Generator(device=W.device).manual_seed(seed)
+        self.m, self.n, self.p, self.seed, self.step = m, n, p, seed, 0
+        # fp32 masters of the adapters; the kernels take them in bf16
+        self.U = (torch.rand(slots, rank, m, generator=g, device=W.device) * 2 - 1) * m ** -0.5
+        self.V = torch.zeros(slots, n, rank, device=W.device)
+        self.scale = torch.full((slots,), 1.0, device=W.device)
+        # the frozen weight's codes and scales, from one call; X is quantised again in every call
+        self.state = binding.halo_linear_fwd(self.desc(16), torch.zeros(16, m, dtype=torch.bfloat16, device=W.device), W)[1]
+
+    def desc(self, tokens):
+        return binding.make_desc(tokens, self.m, self.n, 0)
+
+    def adapters(self):
+        return self.U.to(torch.bfloat16), self.V.to(torch.bfloat16)
+
+    def frozen(self, X):
+        """X W^T, and what its backward pass needs."""
+        state = binding.LinearState(*binding.halo_hadamard_quant(X), self.state.Wq, self.state.s_w)
+        # the layer's own product, which takes any number of tokens
+        Y = binding.halo_gemm_i8(state.Xq, state.Wq, trans_b=True, row_scale=state.s_x, col_scale=state.s_w, out_dtype=torch.bfloat16)[0]
+        return Y, state
+
+    def forward(self, X, adapter_of, residual=None, train=False):
+        """Out, and what backward() takes.  Every training pass draws masks of its own: two offsets a step."""
+        U, V = self.adapters()
+        p = self.p if train else 0.0
+        Y, state = self.frozen(X)
+        Y, T = binding.halo_adapters_fwd(X, U, V, adapter_of, scale=self.scale, base=Y, dropout_p=p, seed=self.seed, offset=2 * self.step, Y=Y)
+        if residual is not None:
+            Y = binding.halo_dropout(Y, p, self.seed, 2 * self.step + 1, residual=residual)
+        return Y, (X, T, U, V, adapter_of, state)
+
+    def backward(self, E, saved):
+        """Gradients of X and of all adapters, of the training pass that `saved` comes from."""
+        X, T, U, V, adapter_of, state = saved
+        E = binding.halo_dropout(E, self.p, self.seed, 2 * self.step + 1)
+        EX = binding.halo_linear_bwd(self.desc(E.shape[0]), E, state, want_g=False)[0]
+        grads = binding.halo_adapters_bwd(E, X, T, U, V, adapter_of, scale=self.scale, base=EX, dropout_p=self.p, seed=self.seed,
+                                          offset=2 * self.step)
+        self.step += 1
+        return grads
+
+
+def run(steps=60, tokens=1024, width=256, slots=4, rank=8, device="cuda", say=lambda *a: None):
+    """Trains the adapters of `slots` tasks, then serves.  Returns the tasks' losses before and after, without dropout, and the largest
+    difference of a token served alone from the same token in its batch, in units of a bf16 result's spacing."""
+    g = torch.Generator(device=device).manual_seed(5)
+    normal = lambda *shape: torch.randn(*shape, generator=g, device=device)
+    W = (normal(width, width) * width ** -0.5).to(torch.bfloat16)
+    layer = Layer(W, slots, rank, p=0.05, seed=11)
+    X, residual = normal(tokens, width).to(torch.bfloat16), normal(tokens, width).to(torch.bfloat16)
+    # requests one after the other, each a quarter of a task's tokens; the last one has no adapter
+    adapter_of = (torch.arange(tokens, device=device) * (4 * slots + 1) // tokens % (slots + 1)).to(torch.int32)
+    adapter_of[adapter_of == slots] = -1
+    # what task a is to learn: a map of the same rank
+    A, B = normal(slots, rank, width) * width ** -0.5, normal(slots, width, rank) * rank ** -0.5
+    target = layer.forward(X, adapter_of, residual)[0].float()
+    for a in range(slots):
+        target[adapter_of == a] += X[adapter_of == a].float() @ A[a].t() @ B[a].t()
+
+    def losses():
+        out = layer.forward(X, adapter_of, residual)[0].float()
+        return [float(((out - target)[adapter_of == a] ** 2).mean()) for a in range(slots)]
+
+    before = losses()
+    optimizer = torch.optim.Adam([layer.U, layer.V], lr=2e-2)
+    for k in range(steps):
+        out, saved = layer.forward(X, adapter_of, residual, train=True)
+        E = (out.float() - target).to(torch.bfloat16)
+        _, layer.U.grad, layer.V.grad = layer.backward(E, saved)
+        optimizer.step()
+        if k % 20 == 0:
+            say("step %3d  losses %s" % (k, " ".join("%.4f" % x for x in losses())))
+    after = losses()
+    say("before %s\nafter  %s" % (" ".join("%.4f" % x for x in before), " ".join("%.4f" % x for x in after)))
+
+    # serving: each call one token of each of several requests, in any order
+    batch = layer.forward(X, adapter_of)[0].float()
+    worst = 0.0
+    for at in (torch.tensor([tokens - 1]), torch.tensor([0, tokens // 2, 3, tokens // 3, 9])):
+        at = at.to(device)
+        alone = layer.forward(X[at].contiguous(), adapter_of[at].contiguous())[0].float()
+        spacing = torch.exp2(torch.floor(torch.log2(batch[at].abs().clamp_min(2.0 ** -10))) - 7)
+        worst = max(worst, float(((alone - batch[at]).abs() / spacing).max()))
+    say("a token alone and in its batch: at most %.2f spacings of bf16 apart" % worst)
+    return before, after, worst
+
+
+if __name__ == "__main__":
+    run(say=print)

@@ -161,9 +161,10 @@ __device__ __forceinline__ void sum_parts(const float* part, int splits, int64_t
 // The gradients take the tokens adapter by adapter.  order: places for tokens, adapter a's, by index, from range[a].x on, a multiple of 32, to
 // range[a].y; a place without a token holds -1.  With `before` tokens of lower adapters the range begins at before, rounded up to 32, plus
 // 32 a: so each finds its own alone, and none overlap.  places: b rounded up to 32, plus 32 slots.
-// A cut is a multiple of `chunk` (of 32) of places; a segment is what one adapter has between cuts, so adapter a has 1 + (cuts strictly inside
-// its range) of them, at least one even without tokens.  Segment i of adapter a has the index a + range[a].x / chunk + i: at most slots + cuts
-// of them, in order, none shared; indices that no adapter takes hold no adapter.
+// A cut is a multiple of `chunk` (of 32) of places.  An adapter's range is worked on in equal segments no longer than chunk, at least one even
+// without tokens, so it has no more of them but the first than there are cuts in it.  Segment i of adapter a has the index
+// a + range[a].x / chunk + i: at most slots + cuts of them, in order, none shared; indices that no adapter takes hold no adapter.  (Segments
+// that end where the cuts lie are found as easily, but one may be 64 tokens long and its neighbour 2000.)
 struct Segment {
     int adapter;             // -1: none
     int begin, end;          // places
@@ -179,7 +180,6 @@ struct Pieces {
         if (size > 0) count = (tokens + size - 1) / size;
     }
 };
-
 
 struct GroupArgs {
     int chunk, cuts;         // cuts: ceil(places / chunk)

@@ -14,9 +14,12 @@ namespace {
 // columns of `big`, a wavefront 64, and goes over the places 32 at a time; k of the matrix instructions is the place.  Both operands are loaded
 // as they lie, 16 bytes a lane, and turned in LDS: a lane has eight columns of four places of `big`, masked before they go to the wavefront's
 // own part of LDS, and four columns of places of `small`, which the four wavefronts stage together, in pieces, two steps in turn.  What is
-// multiplied is read from there by the instruction that turns four rows of sixteen values.  (Loaded 8 and 4 bytes a lane as the instructions'
-// lanes want them, which needs no turning, it was XX us instead of YY at 8192 places, 14336 + 4096 columns, rank 64, masked: the vector memory
-// unit takes as long for an instruction of 4 bytes a lane as for one of 16.)  NT: rank tiles of 16, from tile blockIdx.z * NT on.
+// multiplied is read from there by the instruction that turns four rows of sixteen values.  (Loaded 8 and 4 bytes a lane, as the matrix
+// instructions' lanes want them, it was 68 us instead of 41 at 6328 places, 1024 + 14336 columns, rank 16: the vector memory unit takes as long
+// for an instruction of 4 bytes a lane as for one of 16.)  NT: rank tiles of 16, from tile blockIdx.z * NT on.
+// Measured: rank 16, those sizes, 194 MB of `big`: 4.7 TB/s, memory.  Rank 64, 8192 places, 14336 + 4096 columns, masked, 302 MB: 114 us,
+// 2.7 TB/s; matrix instructions (three for each product of fp32 by bf16), LDS and vector instructions each take a quarter of the time of the
+// eight wavefronts that registers leave to a compute unit, and what they do not cover of each other bounds it.
 template <int NT, bool MASK>
 __global__ void __launch_bounds__(64 * kGradWaves, 2)
 grad_kernel(GradArgs g) {

@@ -304,6 +304,8 @@ thin_few_kernel(ThinArgs g) {
 // four columns loaded and packed by each thread: 97 us instead of 69 at 6328 tokens, K = 14336, rank 16); and the tokens' rows are loaded by
 // whole lines, sixteen lanes 256 bytes, and turned in LDS as well (12.5 -> 9.7 us at 2048 tokens, K = 4096, rank 16; without the adapter's
 // work of turning, in the other direction, it costs more than it gives: 15.0 -> 16.4 at 1037 tokens, rank 64).
+// Measured: forward, dropout, 8192 tokens, K = 4096, rank 64: 38 us, where drawing as many bits and nothing else takes 8; backward, 6328
+// tokens, K = 14336, rank 16: 58 us, 3.1 TB/s; what bounds it is each step's chain of LDS reads and writes, and workgroups of uneven work.
 constexpr int kRowWaves = 4;
 constexpr int kRowTile = 16 * kRowWaves;                 // tokens of a workgroup
 
@@ -467,7 +469,9 @@ thin_rows_kernel(ThinArgs g) {
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-constexpr int64_t kManyTokens = 1024;                    // from here on thin_rows_kernel
+// From here on thin_rows_kernel: at 1021 tokens, K = 960, rank 16 it takes 7.8 us and thin_few_kernel 5.4, at 777, K = 1336, rank 40 11.7 and
+// 10.4; at 2603, K = 4096, rank 24 12.4 and 16.0, at 8192, K = 4096, rank 64 with dropout 38 and 72.
+constexpr int64_t kManyTokens = 1024;
 constexpr int64_t kFill = 512, kCompute = 256;           // workgroups that fill the chip, and its compute units
 
 int64_t extra_blocks(const AdapterPool& p, const BackwardExtras& x, int threads) {
@@ -518,9 +522,9 @@ ThinPlan thin_plan(int64_t b, int64_t K, int slots) {
         if (splits > chunks / 3) splits = chunks / 3;
         if (splits < 1) splits = 1;
         int64_t lanes = kFill / ((tiles > 0 ? tiles : 1) * splits);
-        if (lanes < 4) lanes = 4;
+        if (lanes < 4) lanes = tiles * splits <= 4 * kFill ? 4 : 1;      // so many tiles are several rounds of workgroups anyway
         q.lanes = (int)(lanes < most ? lanes : most);
-    } else {                                             // few tokens: one for each adapter that there may be; or for the second
+    } else {                                             // few tokens: one for each adapter that there may be; or for a second one
         if (b > 256 && most > 2) most = 2;
         q.lanes = (int)(most < 1 ? 1 : most);
         const int64_t busy = b <= 256 ? tiles * q.lanes : tiles;

@@ -116,6 +116,18 @@ def test_sizes_and_orders(b, m, n, slots, rank, odt, p):
         c.check(*c.run())
 
 
+@pytest.mark.parametrize("b,m,n,slots,rank,length", [
+    (1024, 72, 4104, 3, 8, 100), (1100, 136, 1000, 70, 24, 1), (1500, 520, 520, 9, 56, 37), (2100, 264, 2056, 4, 104, 700),
+    (3000, 2056, 72, 1, 16, 3000), (4100, 640, 136, 2, 40, 1300), (2048, 512, 8, 12, 128, 5),
+])
+@pytest.mark.parametrize("p", [0.0, 0.2])
+def test_many_tokens(b, m, n, slots, rank, length, p):
+    """Tiles with one adapter, at requests' borders and with more adapters than workgroups that share them; adapters with several segments,
+    whole ones and the last, which is shorter; reductions that end inside a step."""
+    c = Case(b, m, n, slots, rank, runs(b, slots, length), ranks=[rank - (5 * s) % rank for s in range(slots)], p=p, seed=b + n)
+    c.check(*c.run())
+
+
 @pytest.mark.parametrize("ranks", [[1, 16, 7, 0, 9], [16, 16, 16, 16, 16], [0, 0, 0, 0, 0], [3, -4, 15, 99, 8]])
 @pytest.mark.parametrize("p", [0.0, 0.3])
 def test_ranks_of_their_own(ranks, p):
