@@ -17,11 +17,11 @@ namespace {
 // multiplied is read from there by the instruction that turns four rows of sixteen values.  (Loaded 8 and 4 bytes a lane, as the matrix
 // instructions' lanes want them, it was 68 us instead of 41 at 6328 places, 1024 + 14336 columns, rank 16: the vector memory unit takes as long
 // for an instruction of 4 bytes a lane as for one of 16.)  NT: rank tiles of 16, from tile blockIdx.z * NT on.
-// Measured: rank 16, those sizes, 194 MB of `big`: 4.7 TB/s, memory.  Rank 64, 8192 places, 14336 + 4096 columns, masked, 302 MB: 114 us,
-// 2.7 TB/s; matrix instructions (three for each product of fp32 by bf16), LDS and vector instructions each take a quarter of the time of the
-// eight wavefronts that registers leave to a compute unit, and what they do not cover of each other bounds it.
+// Measured: rank 16, those sizes, 194 MB of `big`: 4.7 TB/s, memory.  Rank 64, 8192 places, 14336 + 4096 columns, masked, 302 MB: 107 us,
+// 2.8 TB/s; matrix instructions (three for each product of fp32 by bf16), LDS and vector instructions each take a quarter of the time, and
+// what they do not cover of each other bounds it.  Registers for three workgroups a compute unit: with two it is 114 us.
 template <int NT, bool MASK>
-__global__ void __launch_bounds__(64 * kGradWaves, 2)
+__global__ void __launch_bounds__(64 * kGradWaves, 3)
 grad_kernel(GradArgs g) {
     constexpr int THREADS = 64 * kGradWaves, UNITS = 128 * NT, PER = (UNITS + THREADS - 1) / THREADS;     // fours of staging, and per thread
     // bytes from one place to the next: so many more than the values that four of a tile lie in all the banks

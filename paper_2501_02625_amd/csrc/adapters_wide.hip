@@ -407,11 +407,14 @@ void launch_as(const WideArgs& g, bool f32, int64_t wanted, hipStream_t s) {
     }
     int64_t y = ceil_div(wanted, tiles * lanes);
     if (y > strips) y = strips;
-    // The shortest by the rounds of workgroups, one a compute unit, and the steps of each, its start like four.  (To fill the chip at least:
-    // 133 us instead of 67 at 6813 x 7096, rank 64, fp32, where that was 270 workgroups.)
+    // As many as one round of workgroups holds, one a compute unit, or several rounds, if that is shorter by the steps of each, its start like
+    // four.  (To fill the chip at least: 133 us instead of 67 at 6813 x 7096, rank 64, fp32, where that was 270 workgroups.)
     if (MT >= 4) {
         int64_t least = INT64_MAX;
-        for (int64_t k = 1; k <= strips && k <= 64; ++k) {
+        for (int rounds = 1; rounds <= 8; ++rounds) {
+            int64_t k = rounds * kFill / tiles;
+            if (k < 1) k = 1;
+            if (k > strips) k = strips;
             const int64_t cost = ceil_div(tiles * k, kFill) * (ceil_div(blocks, k) * MT + 4 * WAVES);
             if (cost < least) { least = cost; y = k; }
         }
