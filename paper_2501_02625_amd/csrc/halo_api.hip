@@ -984,13 +984,15 @@ halo_status halo_dropout(const void* in, halo_dtype dt, int64_t rows, int64_t co
     return from_hip(launch_dropout(a, reinterpret_cast<hipStream_t>(stream)));
 }
 
+// Without in- or out-features there is nothing to do, and nothing to plan with: the plans divide by the numbers of tiles.
 size_t halo_adapters_fwd_workspace_bytes(const halo_adapters_desc* desc) {
-    return check_adapters(desc) == HALO_OK ? adapters_fwd_workspace(desc->b, desc->m, desc->n, desc->slots, desc->max_rank) : 0;
+    if (check_adapters(desc) != HALO_OK || desc->m == 0 || desc->n == 0) return 0;
+    return adapters_fwd_workspace(desc->b, desc->m, desc->n, desc->slots, desc->max_rank);
 }
 
 size_t halo_adapters_bwd_workspace_bytes(const halo_adapters_desc* desc) {
-    return check_adapters(desc) == HALO_OK
-               ? adapters_bwd_workspace(desc->b, desc->m, desc->n, desc->slots, desc->max_rank, desc->dropout_p > 0.0) : 0;
+    if (check_adapters(desc) != HALO_OK || desc->m == 0 || desc->n == 0) return 0;
+    return adapters_bwd_workspace(desc->b, desc->m, desc->n, desc->slots, desc->max_rank, desc->dropout_p > 0.0);
 }
 
 halo_status halo_adapters_fwd(const halo_adapters_desc* desc, const void* X, int64_t ld_x, const void* U, const void* V,
