@@ -452,7 +452,7 @@ def halo_adapters_fwd(X: torch.Tensor, U: torch.Tensor, V: torch.Tensor, adapter
                       T: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Low-rank adapters of many requests beside a shared projection: Y = base + scale_a (drop(X) U_a^T) V_a^T with the adapter
     a = adapter_of[t] of each token t (none outside [0, slots)).  U [slots, max_rank, m], V [slots, n, max_rank]; returns (Y, T =
-    drop(X) U_a^T in fp32, which the backward pass takes).  base and Y have out_dtype and may be one tensor."""
+    drop(X) U_a^T in fp32, which the backward pass takes).  base and Y have out_dtype and may be one tensor; m and n are not 0."""
     r = _native().adapters_fwd(X, U, V, adapter_of, ranks, scale, base, _dt(out_dtype), dropout_p, seed, offset, Y, T, workspace)
     return r if type(r) is tuple else _failed(r, "halo_adapters_fwd")
 

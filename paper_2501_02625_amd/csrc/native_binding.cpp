@@ -388,6 +388,8 @@ struct Adapters {
                     U->size(0) == V->size(0) && U->size(1) == V->size(2),
                 "U [slots, max_rank, m] and V [slots, n, max_rank] are contiguous bf16");
         d.b = rows->size(0); d.m = U->size(2); d.n = V->size(1);
+        // the library does nothing without either, and what it has not written is no result
+        require(d.m > 0 && d.n > 0, "U and V have in- and out-features");
         require(U->size(0) <= INT32_MAX && U->size(1) <= INT32_MAX, "the pool is too large");
         d.slots = (int32_t)U->size(0); d.max_rank = (int32_t)U->size(1);
         require(of->scalar_type() == at::kInt && of->is_contiguous() && of->dim() == 1 && of->size(0) == d.b, "adapter_of is int32 [b]");
