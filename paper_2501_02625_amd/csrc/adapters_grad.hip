@@ -193,7 +193,8 @@ grad_kernel(GradArgs g) {
     if (MASK && second) sum(std::bool_constant<MASK>());
     else sum(std::false_type());
     const int rank = rank_of(p, seg.adapter);
-    const float factor = second ? (masked ? g.factor : 1.0f) : scale_of(p, seg.adapter);
+    // Nothing is summed for an adapter without tokens, and its scale, which may be anything, is not used.
+    const float scale = scale_of(p, seg.adapter), factor = second ? (masked ? g.factor : 1.0f) : seg.begin < seg.end ? scale : 1.0f;
     float* dst = seg.part < 0 ? job.out + (int64_t)seg.adapter * wide * R : job.part + (int64_t)seg.part * wide * R;
     const bool rank_major = job.rank_major != 0;
 #pragma unroll

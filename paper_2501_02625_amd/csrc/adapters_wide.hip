@@ -332,6 +332,11 @@ wide_kernel(WideArgs g) {
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = (e < 4 ? lo[e & 3] : hi[e & 3]) * scale;
+        if (!BWD && !__builtin_isfinite(scale)) {        // beyond the token's own rank there is nothing that it could meet
+            const int own_rank = rank_of(p, id);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = r + e < own_rank ? x[e] : 0.0f;
+        }
         v4u q[3];
         split_eight(x, q);
         if constexpr (STACK) {
