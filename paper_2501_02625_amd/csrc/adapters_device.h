@@ -4,7 +4,7 @@
 //   T = drop(X) U_a^T        Y = base + s_a T V_a^T
 //   S = s_a E V_a            E_X = base + drop'(S U_a)       G_U = sum over a's tokens of S_t drop(X)_t       G_V = s_a sum of E_t T_t
 // All matrices but T, S and the gradients are bf16; bf16 matrix instructions accumulate in fp32.  T and S stay fp32: where they are
-// operands they are split exactly into three bf16 pieces, so the sums are those of fp32 products.
+// operands they are split exactly into three bf16 pieces (or four), so the sums are those of fp32 products.
 //
 // The kernels of T, S, Y and E_X take tiles of tokens as they lie; a tile is worked on once for each different adapter among its tokens, so
 // tokens may come in any order and nothing has to be sorted.  The gradients' kernel takes the tokens adapter by adapter, in an order that is
@@ -48,24 +48,32 @@ __device__ __forceinline__ void columns_of(const uint2 (&x)[8], v4u (&y)[4]) {
     }
 }
 
-// x = hi + mid + lo exactly, each piece an fp32 value whose low 16 bits are zero (a bf16): the mantissa's top 8 bits, the next 8, the
-// last 8.  An infinity is its own top piece.
-__device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
-    hi = __float_as_uint(x) & 0xFFFF0000u;
-    const float h = __uint_as_float(hi), r = h == x ? 0.0f : x - h;
-    mid = __float_as_uint(r) & 0xFFFF0000u;
-    lo = __float_as_uint(r - __uint_as_float(mid));
+// x as the sum of N = 3 or 4 pieces, each an fp32 value whose low 16 bits are zero (a bf16), exactly, but for what lies below 2^-133, the
+// least bf16.  The pieces have x's sign, and none of them is zero unless x is (below 2^-110 the last may be): each but the last is the largest
+// bf16 whose magnitude lies below what is left.  So a factor that is infinite makes an infinity of every piece, and an infinite x is two
+// (three) times the largest bf16 and an infinity.  With pieces cut off at the bits of x, of which all but one may be zero, an infinite factor
+// times zero would be NaN.
+template <int N>
+__device__ __forceinline__ void split(float x, uint32_t (&piece)[N]) {
+    x += 0.0f;                                           // -0 becomes 0: below it there is nothing
+#pragma unroll
+    for (int k = 0; k + 1 < N; ++k) {
+        piece[k] = __builtin_elementwise_sub_sat(__float_as_uint(x), 1u) & 0xFFFF0000u;
+        x -= __uint_as_float(piece[k]);
+    }
+    piece[N - 1] = __float_as_uint(x);
 }
 
-// The three pieces of eight values, as operands.
-__device__ __forceinline__ void split_eight(const float (&x)[8], v4u (&q)[3]) {
-    uint32_t piece[3][8];
+// The pieces of eight values, as operands.
+template <int N>
+__device__ __forceinline__ void split_eight(const float (&x)[8], v4u (&q)[N]) {
+    uint32_t piece[8][N];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) split3(x[e], piece[0][e], piece[1][e], piece[2][e]);
+    for (int e = 0; e < 8; ++e) split(x[e], piece[e]);
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
-        q[k] = v4u{pack_hi(piece[k][0], piece[k][1]), pack_hi(piece[k][2], piece[k][3]), pack_hi(piece[k][4], piece[k][5]),
-                   pack_hi(piece[k][6], piece[k][7])};
+    for (int k = 0; k < N; ++k)
+        q[k] = v4u{pack_hi(piece[0][k], piece[1][k]), pack_hi(piece[2][k], piece[3][k]), pack_hi(piece[4][k], piece[5][k]),
+                   pack_hi(piece[6][k], piece[7][k])};
 }
 
 // Loads at a 32-bit byte offset from an address that is the same for the wavefront: one register of address.

@@ -101,15 +101,15 @@ grad_kernel(GradArgs g) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[e] = token[i] < 0 ? 0.0f : x[e];
                 }
-                uint32_t piece[3][4];
+                uint32_t piece[4][3];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) split3(x[e], piece[0][e], piece[1][e], piece[2][e]);
+                for (int e = 0; e < 4; ++e) split(x[e], piece[e]);
                 const int at = (tid + i * THREADS) / (4 * NT) * SMALL + 8 * c4;
                 if (UNITS % THREADS == 0 || tid < UNITS) {
 #pragma unroll
                     for (int k = 0; k < 3; ++k)
                         *reinterpret_cast<uint2*>(reinterpret_cast<char*>(s_small[j & 1][k]) + at) =
-                            make_uint2(pack_hi(piece[k][0], piece[k][1]), pack_hi(piece[k][2], piece[k][3]));
+                            make_uint2(pack_hi(piece[0][k], piece[1][k]), pack_hi(piece[2][k], piece[3][k]));
                 }
             }
         };

@@ -66,8 +66,8 @@ struct Eight {
 
 // A block of 64 features of an adapter, the first operand of the matrix instructions: 16-byte loads of V, or four neighbouring columns of eight
 // rank rows of U, packed.  Every lane loads, from a place that exists; what is not the adapter's is cleared in finish().
-// RC: rank chunks of 32.  RC == 0 (rank up to 16): the halves of the instruction's 32 products hold the pieces (high, middle) and (low,
-// nothing) of the second operand, two instructions instead of three, and the first operand twice.
+// RC: rank chunks of 32.  RC == 0 (rank up to 16): the second operand's values are split in four pieces, of which the halves of an
+// instruction's 32 products hold two and two, two instructions instead of three, and the first operand twice.
 template <int RC_, bool BWD>
 struct AdapterBlock {
     static constexpr bool STACK = RC_ == 0;
@@ -337,11 +337,11 @@ wide_kernel(WideArgs g) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = r + e < own_rank ? x[e] : 0.0f;
         }
-        v4u q[3];
+        v4u q[STACK ? 4 : 3];
         split_eight(x, q);
         if constexpr (STACK) {
             s_thin[j * NP][lane] = kg < 2 ? q[0] : q[1];
-            s_thin[j * NP + 1][lane] = kg < 2 ? q[2] : v4u{0, 0, 0, 0};
+            s_thin[j * NP + 1][lane] = kg < 2 ? q[2] : q[3];
         } else {
 #pragma unroll
             for (int k = 0; k < NP; ++k) s_thin[j * NP + k][lane] = q[k];
