@@ -391,8 +391,9 @@ halo_status halo_dropout(const void* in, halo_dtype dt, int64_t rows, int64_t co
  *                  (may be NULL where that is 0); nothing in it is carried from call to call.  For a backward call with dropout it
  *                  holds the mask, a bit for every element of X, which is drawn once and used twice.
  * ranks, scale and adapter_of need 4-byte alignment only.  Products of bf16 values accumulate in fp32, T and S are not rounded to
- * fewer bits.  Infinities and NaN go where the formulas take them, to their own tokens and columns.  m == 0, n == 0 or (forward) b == 0 is a no-op: nothing is written, neither T nor GU and GV.  Errors as elsewhere; HALO_EUNSUPPORTED: max_rank > 128, slots > 32768,
- * b, m or n > 2^22, (backward) ld_e or ld_x of 2^31 or more.
+ * fewer bits.  Infinities and NaN go where the formulas take them, to their own tokens and columns.  m == 0, n == 0 or (forward)
+ * b == 0 is a no-op: nothing is written, neither T nor GU and GV.  Errors as elsewhere; HALO_EUNSUPPORTED: max_rank > 128,
+ * slots > 32768, b, m or n > 2^22, (backward) ld_e or ld_x of 2^31 or more.
  */
 typedef struct halo_adapters_desc {
     int64_t b, m, n;

@@ -47,12 +47,13 @@ template <> struct Eight<float> {
 };
 
 // A workgroup takes kThreads * kGroups groups of eight elements, row after row; groups: per row.  Row and group of a thread come from one
-// division of the workgroup's first index (the same for all its threads) and a 32-bit one.
+// division of the workgroup's first index (the same for all its threads) and a 32-bit one.  Workgroups are numbered along x and then y, because
+// a dimension of a launch has at most 2^32 - 1 threads: of more, only what is left modulo 2^32 begins, without an error.
 template <typename E, bool RESIDUAL>
 __global__ void __launch_bounds__(kThreads)
 dropout_kernel(const E* in, int64_t ld_in, const E* residual, int64_t ld_res, E* out, int64_t ld_out, int64_t rows, uint32_t cols,
                uint32_t groups, DropoutMask d) {
-    const int64_t first = (int64_t)blockIdx.x * (kThreads * kGroups);
+    const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kThreads * kGroups);
     const int64_t row0 = first / groups;
     const uint32_t group0 = (uint32_t)(first - row0 * groups);
     Eight<E> x[kGroups], r[kGroups];
@@ -96,14 +97,15 @@ dropout_kernel(const E* in, int64_t ld_in, const E* residual, int64_t ld_res, E*
 template <typename E>
 hipError_t launch_typed(const DropoutArgs& a, hipStream_t s) {
     const int64_t groups = (a.cols + 7) / 8, per = kThreads * kGroups, blocks = (a.rows * groups + per - 1) / per;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+    constexpr int64_t kAlongX = 1 << 20;                 // 2^28 threads; with the most rows and columns, 2^12 of them along y
+    const dim3 grid((unsigned)(blocks < kAlongX ? blocks : kAlongX), (unsigned)((blocks + kAlongX - 1) / kAlongX));
     const E *in = reinterpret_cast<const E*>(a.in), *res = reinterpret_cast<const E*>(a.residual);
     E* out = reinterpret_cast<E*>(a.out);
     if (res)
-        hipLaunchKernelGGL((dropout_kernel<E, true>), dim3((unsigned)blocks), dim3(kThreads), 0, s, in, a.ld_in, res, a.ld_res, out,
+        hipLaunchKernelGGL((dropout_kernel<E, true>), grid, dim3(kThreads), 0, s, in, a.ld_in, res, a.ld_res, out,
                            a.ld_out, a.rows, (uint32_t)a.cols, (uint32_t)groups, a.drop);
     else
-        hipLaunchKernelGGL((dropout_kernel<E, false>), dim3((unsigned)blocks), dim3(kThreads), 0, s, in, a.ld_in, res, a.ld_res, out,
+        hipLaunchKernelGGL((dropout_kernel<E, false>), grid, dim3(kThreads), 0, s, in, a.ld_in, res, a.ld_res, out,
                            a.ld_out, a.rows, (uint32_t)a.cols, (uint32_t)groups, a.drop);
     return hipGetLastError();
 }
