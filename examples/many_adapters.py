@@ -46,22 +46,21 @@ class Layer:
     def forward(self, X, adapter_of, residual=None, train=False):
         """Out, and what backward() takes.  Every training pass draws masks of its own: two offsets a step."""
         U, V = self.adapters()
-        p = self.p if train else 0.0
+        p, offset = (self.p, 2 * self.step) if train else (0.0, 0)
+        self.step += train
         Y, state = self.frozen(X)
-        Y, T = binding.halo_adapters_fwd(X, U, V, adapter_of, scale=self.scale, base=Y, dropout_p=p, seed=self.seed, offset=2 * self.step, Y=Y)
+        Y, T = binding.halo_adapters_fwd(X, U, V, adapter_of, scale=self.scale, base=Y, dropout_p=p, seed=self.seed, offset=offset, Y=Y)
         if residual is not None:
-            Y = binding.halo_dropout(Y, p, self.seed, 2 * self.step + 1, residual=residual)
-        return Y, (X, T, U, V, adapter_of, state)
+            Y = binding.halo_dropout(Y, p, self.seed, offset + 1, residual=residual)
+        return Y, (X, T, U, V, adapter_of, state, p, offset, residual is not None)
 
     def backward(self, E, saved):
-        """Gradients of X and of all adapters, of the training pass that `saved` comes from."""
-        X, T, U, V, adapter_of, state = saved
-        E = binding.halo_dropout(E, self.p, self.seed, 2 * self.step + 1)
+        """Gradients of X and of all adapters, of the pass that `saved` comes from."""
+        X, T, U, V, adapter_of, state, p, offset, dropped = saved
+        if dropped:
+            E = binding.halo_dropout(E, p, self.seed, offset + 1)
         EX = binding.halo_linear_bwd(self.desc(E.shape[0]), E, state, want_g=False)[0]
-        grads = binding.halo_adapters_bwd(E, X, T, U, V, adapter_of, scale=self.scale, base=EX, dropout_p=self.p, seed=self.seed,
-                                          offset=2 * self.step)
-        self.step += 1
-        return grads
+        return binding.halo_adapters_bwd(E, X, T, U, V, adapter_of, scale=self.scale, base=EX, dropout_p=p, seed=self.seed, offset=offset)
 
 
 def run(steps=60, tokens=1024, width=256, slots=4, rank=8, device="cuda", say=lambda *a: None):
