@@ -21,6 +21,7 @@
 #include <stdint.h>
 
 #include "adapters.h"
+#include "adapters_plan.h"
 
 namespace halo {
 namespace adapters {
@@ -257,8 +258,6 @@ int grad_chunk(int64_t b, int64_t places, int64_t m, int64_t n, int max_rank);
 // Sums that have a place of their own among a job's parts.
 inline int64_t grad_parts(int64_t cuts) { return cuts > 1 ? 2 * cuts + 1 : 0; }
 hipError_t launch_grads(const GradArgs& g, hipStream_t s);
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace adapters
 }  // namespace halo

@@ -432,14 +432,14 @@ void launch_as(const WideArgs& g, bool f32, int64_t wanted, hipStream_t s) {
 
 template <int RC, bool BWD>
 void launch_by_size(const WideArgs& g, bool f32, hipStream_t s) {
-    constexpr int TALL = RC == 4 ? 8 : 16;               // 96 KB of pieces at most
-    const int64_t strips = ceil_div(BWD ? g.p.m : g.p.n, 512);
+    constexpr int TALL = RC == 4 ? 8 : 16;
     constexpr int WAVES = RC == 4 && BWD ? 4 : 8;        // registers
-    // Tall once its tiles fill the chip (3417 x 11976, rank 64: 60 us, shorter ones 85); MT 4 down to two strips a compute unit, MT 1 below:
-    // 19.5 us instead of 21.8 at 2048 x 4096, rank 16, which is one strip; but 45.6 instead of 39 at 1547 x 12984, rank 32, with 2.5 of them.
-    if (ceil_div(g.p.b, 16 * TALL) * strips >= kFill) launch_as<RC, TALL, WAVES, BWD>(g, f32, kFill, s);
-    else if (ceil_div(g.p.b, 64) * strips >= 2 * kFill) launch_as<RC, 4, WAVES, BWD>(g, f32, 2 * kFill, s);
-    else launch_as<RC, 1, 4, BWD>(g, f32, 4 * kFill, s);
+    const int tokens = wide_tile_tokens(g.p.b, BWD ? g.p.m : g.p.n, g.p.max_rank);
+    if (tokens == 16 * TALL) return launch_as<RC, TALL, WAVES, BWD>(g, f32, kFill, s);
+    if constexpr (RC < 4) {
+        if (tokens == 64) return launch_as<RC, 4, WAVES, BWD>(g, f32, 2 * kFill, s);
+    }
+    launch_as<RC, 1, 4, BWD>(g, f32, 4 * kFill, s);
 }
 
 template <bool BWD>
