@@ -1,10 +1,12 @@
-"""CPU test of which way the rules in csrc/adapters_plan.h send calls."""
+"""CPU test of which way the rules in csrc/adapters_plan.h send the shapes of the GPU tests: a test that is there for one kernel keeps
+reaching it when a rule changes, or fails here."""
 import shutil
 import subprocess
 
 import pytest
 
 from paper_2501_02625_amd import _build
+from tests import test_gpu_adapters_tall as tall
 
 PROGRAM = r"""
 #include <cstdio>
@@ -29,6 +31,17 @@ def ask(tmp_path_factory):
         return [int(x) for x in subprocess.run([str(d / "plan")], input=text, capture_output=True, text=True, check=True).stdout.split()]
 
     return answers
+
+
+def test_shapes_of_the_tests_of_tall_tiles(ask):
+    assert ask((b, wide, rank) for rank, b, wide, tile in tall.SHAPES) == [tile for *_, tile in tall.SHAPES]
+
+
+def test_every_template_is_reached(ask):
+    """The ranks' four templates, each with every tile that the rule has for it."""
+    template = lambda rank: 0 if rank <= 16 else 1 if rank <= 32 else 2 if rank <= 64 else 4
+    reached = {(template(rank), tile) for rank, _, _, tile in tall.SHAPES}
+    assert reached == {(t, tile) for t in (0, 1, 2) for tile in (64, 256)} | {(4, 128)}
 
 
 def test_tiles_of_any_size(ask):
