@@ -349,7 +349,8 @@ halo_status halo_peft_bwd(const halo_linear_desc* desc, int32_t rank, const void
  *   Philox4x32-10 with the counter words (j / 8, i, offset mod 2^32, offset / 2^32) and the key (seed mod 2^32, seed / 2^32).
  *
  * The mask depends on (seed, offset, i, j) alone, neither on ld nor on the machine, so the gradient of the branch is the same call
- * on the output's gradient, without the residual.  A caller takes another offset for every tensor and step.
+ * on the output's gradient, without the residual.  A caller takes another offset for every tensor and step.  Seed and offset are
+ * arguments of the call: a captured graph draws the same mask at every replay (so do halo_adapters_*'s).
  *
  *   in, residual, out   [rows x cols] of type dt (bf16 or fp32), each with its own leading dimension; residual may be NULL (0).  out
  *                       may be in or residual themselves (same leading dimension), and overlap neither otherwise.
@@ -386,6 +387,7 @@ halo_status halo_dropout(const void* in, halo_dtype dt, int64_t rows, int64_t co
  *   T              fp32 [b x max_rank], dense: written by the forward pass, read by the backward pass (for G_V).  Columns beyond the
  *                  adapter's rank are 0.
  *   GU, GV         fp32, dense, laid out like U and V; 0 beyond an adapter's rank and for adapters without tokens (b == 0 included).
+ *   Outputs and workspace overlap neither one another nor, but for base, what the call reads.
  *   EX, GU, GV     any may be NULL to skip it (not all three).  X is read for G_U only, T for G_V only, U for E_X, V for E_X and G_U.
  *   workspace      halo_adapters_fwd_workspace_bytes(desc) resp. halo_adapters_bwd_workspace_bytes(desc) bytes, 16-byte aligned
  *                  (may be NULL where that is 0); nothing in it is carried from call to call.  For a backward call with dropout it

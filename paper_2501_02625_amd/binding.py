@@ -427,7 +427,7 @@ def halo_peft_bwd(desc: LinearDesc, E: torch.Tensor, X: torch.Tensor, T: torch.T
 def halo_dropout(x: torch.Tensor, p: float, seed: int, offset: int, *, residual: Optional[torch.Tensor] = None,
                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """residual + drop(x), x a bf16 or fp32 matrix.  The mask is a function of (seed, offset, row, column), both 64-bit integers: the
-    same call on the gradient, without the residual, is the backward pass."""
+    same call on the gradient, without the residual, is the backward pass; a captured graph draws the same mask at every replay."""
     r = _native().dropout(x, p, seed, offset, residual, out)
     return r if type(r) is not int else _failed(r, "halo_dropout")
 

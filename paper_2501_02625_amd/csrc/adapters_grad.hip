@@ -247,7 +247,9 @@ grad_join_kernel(AdapterPool p, GroupArgs group, GradJob v, GradJob u) {
     *reinterpret_cast<v4f*>(job.out + (int64_t)a * size + i) = sum;
 }
 
-constexpr int64_t kFill = 512;                           // workgroups that the chip holds at once
+// Workgroups that the segments are cut for, two a compute unit.  Registers leave room for three, but cut for 768 the sums and their joins take
+// as long: 8192 tokens, 14336 + 4096 columns, rank 64 110 us and 113, 2048, 4096 + 4096, rank 16 19 and 20.5, 4096 of them, rank 32 29 and 28.
+constexpr int64_t kFill = 512;
 
 template <int NT>
 void launch_as(const GradArgs& g, hipStream_t s) {
@@ -259,7 +261,7 @@ void launch_as(const GradArgs& g, hipStream_t s) {
 
 }  // namespace
 
-// Segments are cut so that together with the column tiles they fill the chip once: every further one costs a partial sum that is written and
+// Segments are cut so that together with the column tiles they are kFill workgroups: every further one costs a partial sum that is written and
 // read again.  Few tokens have little to be read: a segment of several is at least 64 places, and its partial sum as much as what it reads.
 int grad_chunk(int64_t b, int64_t places, int64_t m, int64_t n, int max_rank) {
     const int64_t tiles = ceil_div(m, kGradCols) + ceil_div(n, kGradCols), wanted = kFill > tiles ? kFill / tiles : 1;

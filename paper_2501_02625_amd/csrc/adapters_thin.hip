@@ -24,7 +24,9 @@ struct TileAdapters {
     }
 };
 
-// One adapter's tokens, written down by a workgroup.  There is a cut at every chunk-th place, and an adapter of several segments, which are
+// One adapter's tokens, written down by a workgroup, which reads all of adapter_of, twice if the adapter has tokens: slots times tokens in
+// all.  (S and this at 8192 tokens, 512 columns, rank 8: 10 us up to 1024 slots, 30 at 8192, 104 at 32768, where writing the gradients, zeros
+// but for those of four adapters, takes another 344.)  There is a cut at every chunk-th place, and an adapter of several segments, which are
 // equally long, has at least as many cuts among its places as segments but the first: these sum into the parts of those cuts k, in order, and
 // the first one into cuts + k of the first of them.
 template <int THREADS>
@@ -469,8 +471,14 @@ thin_rows_kernel(ThinArgs g) {
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-// From here on thin_rows_kernel: at 1021 tokens, K = 960, rank 16 it takes 7.8 us and thin_few_kernel 5.4, at 777, K = 1336, rank 40 11.7 and
-// 10.4; at 2603, K = 4096, rank 24 12.4 and 16.0, at 8192, K = 4096, rank 64 with dropout 38 and 72.
+// From here on thin_rows_kernel.  Where the kernels cross depends on K as well, which this rule does not: us of thin_few_kernel and
+// thin_rows_kernel, forward, four adapters, requests in turn:
+//    tokens       K = 1024, rank 16 and 64       K = 4096, rank 16 and 64
+//       512      3.8  5.5      5.4  6.4          3.9  7.4      6.6  9.2
+//       777      3.8  5.6      5.5  6.6          5.6  7.5     13.1  9.4
+//      1037      3.8  5.5      5.5  6.6          8.0  7.5     18.0  9.4
+//      2048      3.9  5.5      6.5  6.7          8.7  7.6     20.3 10.9
+//      4096      5.0  5.7     12.4  6.9         12.5  8.9     29.0 12.3
 constexpr int64_t kManyTokens = 1024;
 constexpr int64_t kFill = 512, kCompute = 256;           // workgroups that fill the chip, and its compute units
 
@@ -524,7 +532,10 @@ ThinPlan thin_plan(int64_t b, int64_t K, int slots) {
         int64_t lanes = kFill / ((tiles > 0 ? tiles : 1) * splits);
         if (lanes < 4) lanes = tiles * splits <= 4 * kFill ? 4 : 1;      // so many tiles are several rounds of workgroups anyway
         q.lanes = (int)(lanes < most ? lanes : most);
-    } else {                                             // few tokens: one for each adapter that there may be; or for a second one
+    } else {
+        // Few tokens: a workgroup for each adapter that there may be in a tile; more than 256: for a second one only.  K = 4096, rank 16, 64
+        // adapters, tokens of one adapter after the other and in turn, us with a workgroup each and with two: 5.6 and 10.2, 5.6 and 10.2 at
+        // 64 tokens; 5.0 and 6.1, 6.5 and 11.2 at 128; 6.2 and 4.2, 8.8 and 11.2 at 256; 8.8 and 6.0, 12.3 and 12.0 at 272.
         if (b > 256 && most > 2) most = 2;
         q.lanes = (int)(most < 1 ? 1 : most);
         const int64_t busy = b <= 256 ? tiles * q.lanes : tiles;

@@ -140,10 +140,11 @@ struct AdapterBlock {
 // A workgroup owns a tile of 16 MT tokens, the columns of its matrix instructions, whose thin values it keeps in LDS as the operands' lanes
 // hold them, split in pieces; of the different adapters among the tokens it takes every gridDim.z-th.  Its wavefronts go over blocks of 64
 // features, the rows: a step is a block times 16 tokens.  The base of the next steps and the next block of the adapter are on their way
-// meanwhile; nothing is exchanged once the pieces are in LDS.  Tall tiles (MT 16) read the adapter once for 256 tokens, little next to base
-// and result; short ones give few tokens more workgroups.
+// meanwhile; nothing is exchanged once the pieces are in LDS.  Tall tiles (MT 16, above rank 64 MT 8) read the adapter once for 256 (128)
+// tokens, little next to base and result; short ones give few tokens more workgroups.
 // Measured: forward, 8192 tokens, 14336 features, rank 64, bf16: 117 us, 470 MB of base and result, 4.0 TB/s; a copy of as much takes 92.  At 64
-// tokens, 14336 features, 64 adapters of rank 16 it is 14 us for 33 MB: the chain of one workgroup, from the ids to the adapter to the store.
+// tokens, 14336 features, 64 adapters of rank 16 it is 14 us for 33 MB: a wavefront has three or four blocks of features and asks for one ahead, so
+// that it waits for memory at nearly each of them.
 template <int RC_, int MT, int WAVES, bool BWD, bool F32>
 __global__ void __launch_bounds__(64 * WAVES, WAVES == 8 || (RC_ == 4 && BWD) ? 1 : 2)
 wide_kernel(WideArgs g) {
@@ -405,6 +406,9 @@ void launch_as(const WideArgs& g, bool f32, int64_t wanted, hipStream_t s) {
         int64_t most = 16 * MT < 16 ? 16 * MT : 16;
         if (g.p.b < most) most = g.p.b;
         if (g.p.slots < most) most = g.p.slots;
+        // Rank 16, 4096 features, 64 adapters in turn, us with a workgroup for each that there may be in a tile and with as many as fill the chip:
+        // 11.2 and 11.7 at 128 tokens, 13.4 and 15.0 at 256, 17.9 and 17.2 at 272; with tokens of one adapter after the other 7.3 and 8.2, 7.5 and
+        // 7.4, 9.4 and 9.1.
         lanes = g.p.b <= 256 ? most : wanted / (tiles * strips);
         if (MT == 1 && lanes < 2) lanes = 2;             // for the tiles with a request's border: 16.6 us instead of 19.5 at 2048 x 4096
         if (lanes > most) lanes = most;
@@ -413,7 +417,8 @@ void launch_as(const WideArgs& g, bool f32, int64_t wanted, hipStream_t s) {
     int64_t y = ceil_div(wanted, tiles * lanes);
     if (y > strips) y = strips;
     // As many as one round of workgroups holds, one a compute unit, or several rounds, if that is shorter by the steps of each, its start like
-    // four.  (To fill the chip at least: 133 us instead of 67 at 6813 x 7096, rank 64, fp32, where that was 270 workgroups.)
+    // four; steps are counted for the workgroup, not for its busiest wavefront.  (To fill the chip at least: 133 us instead of 67 at 6813 x 7096,
+    // rank 64, fp32, where that was 270 workgroups.)
     if (MT >= 4) {
         int64_t least = INT64_MAX;
         for (int rounds = 1; rounds <= 8; ++rounds) {

@@ -1,5 +1,6 @@
 // Dropout masks from a counter-based generator: Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as
-// 1, 2, 3", 2011).  A mask is a function of (seed, offset, row, column) alone, so it is never stored: whoever needs it draws it again.
+// 1, 2, 3", 2011).  A mask is a function of (seed, offset, row, column) alone, so it need not be kept from the forward pass: the backward
+// pass draws it again (that of the adapters once, for two kernels: a bit an element in its workspace).
 //
 // One call gives the 8 x 16 random bits of eight consecutive elements of a row: the counter is (column / 8, row, offset low, offset
 // high), the key (seed low, seed high), and element j takes half j % 2 (the low one first) of word (j % 8) / 2.  The element is kept
