@@ -418,6 +418,151 @@ halo_status halo_adapters_bwd(const halo_adapters_desc* desc, const void* E, int
                               const void* base, int64_t ld_base, void* EX, int64_t ld_ex, float* GU, float* GV, void* workspace,
                               size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * What stands around a layer's products in a training step: bias, activation and residual behind the forward product, their
+ * gradient, the norm in front of it, and the optimizer that takes the gradients.
+ *
+ * halo_gemm_i8_epilogue: halo_gemm_i8_desc (K-contiguous B) with more in its epilogue, all in fp32:
+ *
+ *   z[i,j] = (float(acc[i,j]) * row_scale[i]) * col_scale[j] + bias[j]
+ *   Z[i,j] = z[i,j] rounded to c_dt;        C[i,j] = act(z[i,j]) + residual[i,j] rounded to c_dt
+ *
+ *   act       none: x; relu: max(x, 0); gelu: x Phi(x), Phi the normal distribution function; gelu_tanh: x / (1 + exp(-2 u)) with
+ *             u = sqrt(2 / pi) (x + 0.044715 x^3); silu: x / (1 + exp(-x)).
+ *   bias      [N], bf16 or fp32 (bias_dt), 16-byte aligned; NULL = 0.
+ *   residual  [M x N] of type c_dt; NULL = 0.  May be C itself, with the same leading dimension.
+ *   Z         [M x N] of type c_dt, for halo_activation_bwd; NULL: not kept.
+ * K == 0: acc is 0, the rest of the formula holds.  C and Z overlap neither each other nor, but for the residual, what the call reads.
+ * An infinity or NaN in bias or residual reaches its own columns (its own element).  HALO_EINVAL: no C, or acc_out; HALO_EUNSUPPORTED:
+ * transB == 0.
+ *
+ * halo_linear_fwd_epilogue: halo_linear_fwd whose product is this one, Y = act(X W^T + bias) + residual in out_dt; residual and Z are
+ * dense unless their leading dimensions say otherwise.  e == NULL: halo_linear_fwd.
+ */
+typedef enum {
+    HALO_ACT_NONE = 0, HALO_ACT_RELU = 1, HALO_ACT_GELU = 2, HALO_ACT_GELU_TANH = 3, HALO_ACT_SILU = 4
+} halo_activation;
+
+typedef struct halo_epilogue {
+    const void* bias; int32_t bias_dt /* halo_dtype */;
+    int32_t activation /* halo_activation */;
+    const void* residual; int64_t ld_res;
+    void* Z; int64_t ld_z;
+} halo_epilogue;
+
+halo_status halo_gemm_i8_epilogue(const halo_gemm_desc* g, const halo_epilogue* e, void* stream);
+
+halo_status halo_linear_fwd_epilogue(const halo_linear_desc* desc, const void* X, const void* W, void* Y, int8_t* Xq, float* s_x,
+                                     int8_t* Wq, float* s_w, const halo_epilogue* e, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/* halo_activation_bwd: the gradient of that epilogue.   E_Z = E act'(Z),   G_bias[j] = sum over the rows i of E[i,j] act'(Z[i,j])
+ *   E, Z, EZ   [rows x cols] of type dt, each with its own leading dimension.  EZ may be E or Z itself (same leading dimension).
+ *              The residual's gradient is E.  act none: Z is not read and may be NULL.  relu' (0) = 0.
+ *   EZ, GB     either may be NULL to skip it (not both).  GB fp32 [cols]: the sum of the products before they are rounded to dt, in
+ *              fp32; 0 where rows == 0.
+ *   workspace  halo_activation_bwd_workspace_bytes(rows, cols) bytes, 16-byte aligned, for GB only; nothing in it is carried over.
+ * cols == 0 is a no-op. */
+size_t halo_activation_bwd_workspace_bytes(int64_t rows, int64_t cols);
+
+halo_status halo_activation_bwd(const void* E, int64_t ld_e, const void* Z, int64_t ld_z, halo_dtype dt, int64_t rows, int64_t cols,
+                                halo_activation act, void* EZ, int64_t ld_ez, float* GB, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Norm of the rows of a matrix and its gradient.
+ *
+ *   forward    mean_i = sum_j X[i,j] / cols  (rms: 0),   rstd_i = 1 / sqrt(sum_j (X[i,j] - mean_i)^2 / cols + eps),
+ *              Y[i,j] = xh[i,j] weight[j] + bias[j]   with   xh[i,j] = (X[i,j] - mean_i) rstd_i
+ *   backward   d = E weight,   E_X[i,j] = base[i,j] + rstd_i (d[i,j] - sum_j d / cols - xh[i,j] sum_j (d xh) / cols)   (rms: without the
+ *              first sum),   G_W[j] = sum_i E[i,j] xh[i,j],   G_B[j] = sum_i E[i,j]
+ *
+ *   X, Y, E, EX, base   [rows x cols] of type dt, each with its own leading dimension; cols at most 32768, rows at most 2^31 - 1.
+ *   weight, bias        [cols], of type weight_dt, 16-byte aligned; NULL: 1, resp. 0.
+ *   mean, rstd          fp32 [rows], 4-byte aligned.  The forward pass writes them where they are not NULL (rms: not the mean); the
+ *                       backward pass reads them (rms: rstd only).
+ *   Y                   may be X itself, with the same leading dimension.
+ *   base                the gradient that goes round the norm; NULL = 0.
+ *   EX                  may be E or base itself, with the same leading dimension.
+ *   EX, GW, GB          any may be NULL to skip it (not all three).  GW, GB fp32 [cols], 16-byte aligned; 0 where rows == 0.
+ *   workspace           halo_layer_norm_bwd_workspace_bytes(desc) bytes, 16-byte aligned, for GW and GB only.
+ * All in fp32, each result rounded once.  The squares are summed about the mean, in a second pass over the row in registers.  cols == 0
+ * is a no-op, and so is rows == 0 but for GW and GB.
+ */
+typedef enum { HALO_NORM_LAYER = 0, HALO_NORM_RMS = 1 } halo_norm_kind;
+
+typedef struct halo_norm_desc {
+    int64_t rows, cols;
+    int32_t kind;           /* halo_norm_kind */
+    int32_t dt, weight_dt;  /* halo_dtype */
+    int32_t reserved;       /* 0 */
+    double eps;             /* not negative, finite */
+} halo_norm_desc;
+
+size_t halo_layer_norm_bwd_workspace_bytes(const halo_norm_desc* desc);
+
+halo_status halo_layer_norm_fwd(const halo_norm_desc* desc, const void* X, int64_t ld_x, const void* weight, const void* bias, void* Y,
+                                int64_t ld_y, float* mean, float* rstd, void* stream);
+
+halo_status halo_layer_norm_bwd(const halo_norm_desc* desc, const void* E, int64_t ld_e, const void* X, int64_t ld_x, const float* mean,
+                                const float* rstd, const void* weight, const void* base, int64_t ld_base, void* EX, int64_t ld_ex,
+                                float* GW, float* GB, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * halo_adamw: one AdamW step over many tensors at once, in place, with states in 32 or in 8 bits.
+ *
+ *   g = grad * grad_scale;   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) (g g);   r = sqrt(v)
+ *   p = p (1 - lr weight_decay) - (lr / (1 - beta1^step)) (m / (r / sqrt(1 - beta2^step) + eps))
+ *
+ * Every operation is one fp32 operation rounded to nearest, in that order from left to right; 1 - beta1, 1 - beta2, 1 - lr weight_decay,
+ * lr / (1 - beta1^step) and 1 / sqrt(1 - beta2^step), by which r is multiplied, are computed in 64 bits and rounded once.  So the results
+ * are the same bit for bit wherever they are computed like that.
+ *
+ * tensors[t], size elements each (dense; a size of 0 is skipped):
+ *   param      of type param_dt.  bf16 with a master: param is the rounded master.  bf16 without: p, computed from the bf16 value, is
+ *              rounded at random, to the upper 16 bits of (its fp32 bits + u); a NaN stays one.  (To nearest, an update below half a
+ *              step of bf16 would be lost every time.)
+ *   grad       of type grad_dt.
+ *   m, v       state_bits 32: fp32.  state_bits 8: e4m3 (OCP) codes, with m_scale and v_scale, fp32 [ceil(size / 256)]: element i of m
+ *              stands for code * m_scale[i / 256], that of v for (code * v_scale[i / 256])^2.  All zeros are states of 0.
+ *   master     fp32, bf16 parameters only: for all tensors or for none (NULL).
+ * What is written, 8 bits: with A the largest |m| (r for v) of the 256, at least 2^-110, the scale is A / 448 and q = min(|m| (448 / A),
+ * 448); q lies between two neighbours lo <= q < hi of e4m3 and becomes hi where 65536 (q - lo) > u (hi - lo), for v where
+ * 65536 ((q - lo) (q + lo)) > u (hi^2 - lo^2), and lo otherwise: on average m and v themselves, not a value that is one rounding off at
+ * every step (v moves by less than half a step of 8 bits from step to step, and to nearest would not move at all).  A v that is not 0
+ * is kept at least at 2^-9 v_scale, so that m is never divided by a 0 that rounding made.  If A is no finite number, all codes of
+ * the 256 become NaN.
+ * u: 16 random bits, as in halo_dropout, of element i % 8 from the Philox counter (i / 8, 4 t + kind, o mod 2^32, o / 2^32) with
+ * o = offset + step, and the key (seed mod 2^32, seed / 2^32); kind 0: param, 1: m, 2: v.  Two calls of one step take different offsets
+ * or seeds (offsets further apart than there are steps).
+ *
+ *   step, lr, grad_scale   step counts from 1.  step_ptr, lr_ptr, grad_scale_ptr, where not NULL, are device memory that holds the
+ *                          value (step below 1: 1) for this call: a captured graph then takes new ones at every replay.
+ *   beta1, beta2           in [0, 1);  lr, eps, weight_decay: finite, not negative;  grad_scale: finite.
+ *   count                  at most 1024 tensors, each of at most 2^34 elements.
+ * Pointers are 16-byte aligned, but for the scales, step_ptr (8), lr_ptr and grad_scale_ptr (4 bytes).  What the call writes overlaps
+ * nothing else that it reads or writes; parameters, states, masters and scales that overlap one another are refused (HALO_EINVAL).  The
+ * array `tensors` is host memory and is not used after the call returns; addresses are copied into a captured graph.  infinities and
+ * NaN: 32 bits, their own elements; 8 bits, their 256 elements' states and own parameters.
+ */
+#define HALO_ADAMW_BLOCK 256
+typedef struct halo_adamw_tensor {
+    int64_t size;
+    void* param; const void* grad; void* m; void* v; float* master; float* m_scale; float* v_scale;
+} halo_adamw_tensor;
+
+typedef struct halo_adamw_desc {
+    int32_t param_dt, grad_dt;  /* halo_dtype */
+    int32_t state_bits;         /* 32 or 8 */
+    int32_t reserved;           /* 0 */
+    int64_t step;
+    double lr, beta1, beta2, eps, weight_decay, grad_scale;
+    uint64_t seed, offset;
+    const int64_t* step_ptr; const float* lr_ptr; const float* grad_scale_ptr;
+} halo_adamw_desc;
+
+halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* tensors, int32_t count, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,7 +18,8 @@ NATIVE_PATH = os.path.join(PKG_DIR, "_halo_native.so")
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 
 SOURCES = ["halo_api.hip", "row_transform.hip", "col_ops.hip", "gemm_i8.hip", "gemm_mx6.hip", "row_kron.hip", "lowrank.hip",
-           "adapters.hip", "adapters_thin.hip", "adapters_wide.hip", "adapters_grad.hip", "dropout.hip"]
+           "adapters.hip", "adapters_thin.hip", "adapters_wide.hip", "adapters_grad.hip", "dropout.hip",
+           "gemm_i8_epilogue.hip", "layer_norm.hip", "activation_grad.hip", "adamw.hip", "around_api.hip"]
 
 # -ffp-contract=off: every fp32 add/mul of the rotation and the quantiser is rounded on its own, which is
 # what makes the INT8 codes reproducible bit for bit.  Packed fp32 instructions are switched off.
@@ -48,7 +49,8 @@ def _run(cmd, cwd=None):
 
 # Kernels whose accumulators are accumulation registers named in the text of inline assembly (csrc/matrix_asm.h), by source.
 ACCUMULATOR_KERNELS = "gemm_i8_kernel"
-ACCUMULATOR_SOURCES = {"gemm_i8.hip": ACCUMULATOR_KERNELS, "gemm_mx6.hip": "gemm_mx6_lines_kernel"}
+ACCUMULATOR_SOURCES = {"gemm_i8.hip": ACCUMULATOR_KERNELS, "gemm_mx6.hip": "gemm_mx6_lines_kernel",
+                       "gemm_i8_epilogue.hip": "gemm_i8_epilogue_kernel"}
 
 
 def accumulator_faults(asm: str, kernel: str = ACCUMULATOR_KERNELS):

@@ -23,6 +23,9 @@ HALO_BF16, HALO_F32 = 0, 1
 HALO_QUANT_ROWS, HALO_QUANT_COLS_T = 0, 1
 HALO_SCALE_PER_ROW, HALO_SCALE_PER_TENSOR = 0, 1
 HALO_GEMM_AUTO = -1
+HALO_ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+HALO_NORM_KINDS = {"layer": 0, "rms": 1}
+HALO_ADAMW_BLOCK = 256
 HALO_GEMM_CONFIGS = {"256x256x64": 0, "256x256x128": 1, "256x128x128": 2, "128x128x64": 3, "staged_128x128x64": 4}
 
 EXPORTED_SYMBOLS = (
@@ -38,6 +41,8 @@ EXPORTED_SYMBOLS = (
     "halo_peft_workspace_bytes", "halo_peft_fwd", "halo_peft_bwd",
     "halo_dropout",
     "halo_adapters_fwd_workspace_bytes", "halo_adapters_bwd_workspace_bytes", "halo_adapters_fwd", "halo_adapters_bwd",
+    "halo_gemm_i8_epilogue", "halo_linear_fwd_epilogue", "halo_activation_bwd_workspace_bytes", "halo_activation_bwd",
+    "halo_layer_norm_bwd_workspace_bytes", "halo_layer_norm_fwd", "halo_layer_norm_bwd", "halo_adamw",
 )
 
 
@@ -65,6 +70,29 @@ class AdaptersDesc(ctypes.Structure):
     _fields_ = [("b", ctypes.c_int64), ("m", ctypes.c_int64), ("n", ctypes.c_int64), ("slots", ctypes.c_int32),
                 ("max_rank", ctypes.c_int32), ("out_dt", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("dropout_p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64)]
+
+
+class Epilogue(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("bias_dt", ctypes.c_int32), ("activation", ctypes.c_int32), ("residual", ctypes.c_void_p),
+                ("ld_res", ctypes.c_int64), ("Z", ctypes.c_void_p), ("ld_z", ctypes.c_int64)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("kind", ctypes.c_int32), ("dt", ctypes.c_int32),
+                ("weight_dt", ctypes.c_int32), ("reserved", ctypes.c_int32), ("eps", ctypes.c_double)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_int64), ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("master", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class AdamwDesc(ctypes.Structure):
+    _fields_ = [("param_dt", ctypes.c_int32), ("grad_dt", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("step", ctypes.c_int64), ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("grad_scale", ctypes.c_double), ("seed", ctypes.c_uint64),
+                ("offset", ctypes.c_uint64), ("step_ptr", ctypes.c_void_p), ("lr_ptr", ctypes.c_void_p),
+                ("grad_scale_ptr", ctypes.c_void_p)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -141,6 +169,22 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.halo_adapters_bwd.restype = c.c_int
     lib.halo_adapters_bwd.argtypes = [c.POINTER(AdaptersDesc), vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp,
                                       sz, vp]
+    lib.halo_gemm_i8_epilogue.restype = c.c_int
+    lib.halo_gemm_i8_epilogue.argtypes = [c.POINTER(GemmDesc), c.POINTER(Epilogue), vp]
+    lib.halo_linear_fwd_epilogue.restype = c.c_int
+    lib.halo_linear_fwd_epilogue.argtypes = [c.POINTER(LinearDesc), vp, vp, vp, vp, vp, vp, vp, c.POINTER(Epilogue), vp, sz, vp]
+    lib.halo_activation_bwd_workspace_bytes.restype = sz
+    lib.halo_activation_bwd_workspace_bytes.argtypes = [i64, i64]
+    lib.halo_activation_bwd.restype = c.c_int
+    lib.halo_activation_bwd.argtypes = [vp, i64, vp, i64, c.c_int, i64, i64, c.c_int, vp, i64, vp, vp, sz, vp]
+    lib.halo_layer_norm_bwd_workspace_bytes.restype = sz
+    lib.halo_layer_norm_bwd_workspace_bytes.argtypes = [c.POINTER(NormDesc)]
+    lib.halo_layer_norm_fwd.restype = c.c_int
+    lib.halo_layer_norm_fwd.argtypes = [c.POINTER(NormDesc), vp, i64, vp, vp, vp, i64, vp, vp, vp]
+    lib.halo_layer_norm_bwd.restype = c.c_int
+    lib.halo_layer_norm_bwd.argtypes = [c.POINTER(NormDesc), vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    lib.halo_adamw.restype = c.c_int
+    lib.halo_adamw.argtypes = [c.POINTER(AdamwDesc), c.POINTER(AdamwTensor), i32, vp]
     if path == _build.LIB_PATH:
         _lib = lib
     return lib
@@ -468,3 +512,81 @@ def halo_adapters_bwd(E: torch.Tensor, X: Optional[torch.Tensor], T: Optional[to
     r = _native().adapters_bwd(E, X, T, U, V, adapter_of, ranks, scale, base, _dt(out_dtype), dropout_p, seed, offset, bool(want_ex),
                                bool(want_gu), bool(want_gv), EX, GU, GV, workspace)
     return r if type(r) is tuple else _failed(r, "halo_adapters_bwd")
+
+
+def _activation(name: str) -> int:
+    if name not in HALO_ACTIVATIONS:
+        raise ValueError("activation is one of %s, got %r" % (", ".join(HALO_ACTIVATIONS), name))
+    return HALO_ACTIVATIONS[name]
+
+
+def _norm_kind(name: str) -> int:
+    if name not in HALO_NORM_KINDS:
+        raise ValueError("kind is one of %s, got %r" % (", ".join(HALO_NORM_KINDS), name))
+    return HALO_NORM_KINDS[name]
+
+
+def halo_gemm_i8_epilogue(a: torch.Tensor, b: torch.Tensor, *, row_scale: Optional[torch.Tensor] = None,
+                          col_scale: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, activation: str = "none",
+                          residual: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32, want_z: bool = False,
+                          out: Optional[torch.Tensor] = None, Z: Optional[torch.Tensor] = None):
+    """z = diag(row_scale) (A B^T) diag(col_scale) + bias on INT8 codes, C = act(z) + residual; returns (C, z in C's type, or None where it
+    is not wanted).  activation: "none", "relu", "gelu", "gelu_tanh" or "silu".  residual has C's type and may be `out` itself."""
+    r = _native().gemm_i8_epilogue(a, b, row_scale, col_scale, bias, _activation(activation), residual,
+                                   HALO_F32 if out is not None else _dt(out_dtype), bool(want_z), out, Z)
+    return r if type(r) is tuple else _failed(r, "halo_gemm_i8_epilogue")
+
+
+def halo_linear_fwd_epilogue(desc: LinearDesc, X: Optional[torch.Tensor], W: Optional[torch.Tensor], *,
+                             bias: Optional[torch.Tensor] = None, activation: str = "none", residual: Optional[torch.Tensor] = None,
+                             want_z: bool = False, Z: Optional[torch.Tensor] = None, state: Optional[LinearState] = None,
+                             Y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """halo_linear_fwd with Y = act(X W^T + bias) + residual; returns (Y, LinearState, Z or None), Z = X W^T + bias for
+    halo_activation_bwd.  residual has Y's type and may be Y itself."""
+    s = state
+    codes = (None,) * 4 if s is None else (s.Xq, s.s_x, s.Wq, s.s_w)
+    r = _native().linear_fwd_epilogue(desc, X, W, *codes, Y, workspace, s is None, bias, _activation(activation), residual, bool(want_z), Z)
+    if type(r) is not tuple:
+        return _failed(r, "halo_linear_fwd_epilogue")
+    return r[0], LinearState(*r[1:5]) if s is None else s, r[5]
+
+
+def halo_activation_bwd(E: torch.Tensor, Z: Optional[torch.Tensor], activation: str = "none", *, want_ez: bool = True, want_gb: bool = True,
+                        EZ: Optional[torch.Tensor] = None, GB: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradient of the epilogue of halo_gemm_i8_epilogue and halo_linear_fwd_epilogue: returns (E_Z = E act'(Z), the bias' gradient in
+    fp32), None where not wanted.  EZ may be E or Z itself; the residual's gradient is E."""
+    r = _native().activation_bwd(E, Z, _activation(activation), bool(want_ez), bool(want_gb), EZ, GB, workspace)
+    return r if type(r) is tuple else _failed(r, "halo_activation_bwd")
+
+
+def halo_layer_norm_fwd(X: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *, eps: float = 1e-5,
+                        kind: str = "layer", want_stats: bool = True, Y: Optional[torch.Tensor] = None,
+                        mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None):
+    """Norm of each row, kind "layer" or "rms" (mean 0); returns (Y, mean, rstd), the statistics in fp32 for the backward pass, None
+    where there are none.  Y may be X itself."""
+    r = _native().layer_norm_fwd(X, weight, bias, eps, _norm_kind(kind), bool(want_stats), Y, mean, rstd)
+    return r if type(r) is tuple else _failed(r, "halo_layer_norm_fwd")
+
+
+def halo_layer_norm_bwd(E: torch.Tensor, X: Optional[torch.Tensor], mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor],
+                        weight: Optional[torch.Tensor] = None, *, kind: str = "layer", base: Optional[torch.Tensor] = None,
+                        want_ex: bool = True, want_gw: bool = True, want_gb: bool = True, EX: Optional[torch.Tensor] = None,
+                        GW: Optional[torch.Tensor] = None, GB: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients of halo_layer_norm_fwd: returns (E_X = base + the norm's part, G_W fp32, G_B fp32), None where not wanted.  base is the
+    gradient that goes round the norm; EX may be E or base itself."""
+    r = _native().layer_norm_bwd(E, X, mean, rstd, weight, _norm_kind(kind), base, bool(want_ex), bool(want_gw), bool(want_gb), EX, GW, GB,
+                                 workspace)
+    return r if type(r) is tuple else _failed(r, "halo_layer_norm_bwd")
+
+
+def halo_adamw(params, grads, m, v, *, step, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, grad_scale=1.0,
+               masters=None, m_scales=None, v_scales=None, seed: int = 0, offset: int = 0) -> None:
+    """One AdamW step, in place, of many tensors at once: lists of tensors with one entry for each parameter.
+
+    params are fp32, or bf16 with fp32 masters, or bf16 alone, which are rounded at random; grads bf16 or fp32; m and v fp32, or
+    float8_e4m3fn with m_scales and v_scales, fp32 [ceil(elements / 256)] (m = code * scale, v = (code * scale)^2; all zeros to begin
+    with).  The random bits of 8-bit states and bf16 parameters follow from (seed, offset + step).  step, lr and grad_scale may be device
+    tensors of one element (int64, fp32, fp32), so that a captured graph takes new values at every replay."""
+    r = _native().adamw(params, grads, m, v, masters, m_scales, v_scales, step, lr, betas[0], betas[1], eps, weight_decay, grad_scale, seed,
+                        offset)
+    return None if r is None else _failed(r, "halo_adamw")

@@ -1,0 +1,271 @@
+// The INT8 GEMM with bias, activation and residual in its epilogue (halo_gemm_i8_epilogue):  z = (float(acc) * row_scale) * col_scale +
+// bias,  C = act(z) + residual, and z itself where it is wanted for the backward pass.  Main loop and tiles: gemm_i8_device.h.
+#pragma clang fp contract(off)
+
+#include "activation.h"
+#include "gemm_i8_device.h"
+
+namespace halo {
+namespace {
+
+// 16 bytes of a row: eight bf16 or four fp32 values.
+template <bool F32>
+struct Piece {
+    static constexpr int W = F32 ? 4 : 8;
+    __device__ __forceinline__ static float get(const v4u& q, int j) {
+        if constexpr (F32) return __uint_as_float(q[j]);
+        else return __uint_as_float((j & 1) ? q[j >> 1] & 0xFFFF0000u : q[j >> 1] << 16);
+    }
+    __device__ __forceinline__ static v4u put(const float* y) {
+        v4u q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (F32) q[i] = __float_as_uint(y[i]);
+            else q[i] = pack_bf16x2(y[2 * i], y[2 * i + 1]);
+        }
+        return q;
+    }
+    // n of the values (n > 0); p: the first one's address
+    __device__ __forceinline__ static void store(void* p, const v4u& q, int n) {
+        if (n >= W) {
+            __builtin_nontemporal_store(q, reinterpret_cast<v4u*>(p));
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            if (j >= n) break;
+            if constexpr (F32) reinterpret_cast<uint32_t*>(p)[j] = q[j];
+            else reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(q[j >> 1] >> (16 * (j & 1)));
+        }
+    }
+};
+template <bool F32>
+__device__ __forceinline__ char* address(const void* p, int64_t ld, int64_t row, int64_t col) {
+    return reinterpret_cast<char*>(const_cast<void*>(p)) + (row * ld + col) * (F32 ? 4 : 2);
+}
+__device__ __forceinline__ float bias_at(const EpilogueArgs& e, int64_t col) {
+    if (!e.bias) return 0.0f;
+    if (e.bias_f32) return reinterpret_cast<const float*>(e.bias)[col];
+    return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(e.bias)[col] << 16);
+}
+template <class F>
+__device__ __forceinline__ void with_activation(int act, const F& f) {
+    switch (act) {
+        case HALO_ACT_RELU: f(Int<HALO_ACT_RELU>()); break;
+        case HALO_ACT_GELU: f(Int<HALO_ACT_GELU>()); break;
+        case HALO_ACT_GELU_TANH: f(Int<HALO_ACT_GELU_TANH>()); break;
+        case HALO_ACT_SILU: f(Int<HALO_ACT_SILU>()); break;
+        default: f(Int<HALO_ACT_NONE>()); break;
+    }
+}
+
+// The accumulators of a wavefront go through LDS, four rows of 16 x 16 tiles at a time, so that a lane has 16 bytes of C, Z and residual
+// that lie together, always of the same columns, and the code that computes them is a loop (over the accumulators, which are named
+// registers, it would be as long as the tile).  The LDS belongs to the wavefront: no barrier but the first.
+template <class Cfg, bool F32, int ACT>
+__device__ __forceinline__ void finish_tile(const GemmArgs& a, const EpilogueArgs& e, int64_t m0, int64_t n0, int wave, int lane,
+                                            unsigned char* smem) {
+    using P = Piece<F32>;
+    constexpr int TM = Cfg::TM, TN = Cfg::TN, WN = Cfg::WN, W = P::W, LANES = WN / W, ROWS = 64 / LANES;      // lanes a row, rows a step
+    constexpr int PITCH = WN + 4, STEPS = 64 / ROWS, AHEAD = 4;
+    static_assert(TM % 4 == 0 && STEPS % AHEAD == 0 && 4 * 64 * PITCH * 4 <= Cfg::LDS_BYTES, "what a wavefront holds in LDS");
+    const int wave_m = wave >> 1, wave_n = wave & 1;
+    int32_t* mine = reinterpret_cast<int32_t*>(smem) + wave * (64 * PITCH);
+    const int at_row = lane / LANES, at_col = lane % LANES * W;
+    const int64_t col = n0 + wave_n * WN + at_col;
+    const int n = a.N - col < W ? (int)(a.N - col) : W;          // columns of this lane inside the matrix; may be negative
+    float cs[W], bias[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+        const int64_t c = col + j < a.N ? col + j : a.N - 1;
+        cs[j] = a.col_scale ? a.col_scale[c] : 1.0f;
+        bias[j] = bias_at(e, c);
+    }
+    __syncthreads();                                             // every wavefront has read its last operands
+#pragma unroll 1
+    for (int part = 0; part < TM / 4; ++part) {
+        auto dump = [&](auto first) {
+            StaticFor<0, 4>::run([&](auto ii) {
+                __builtin_amdgcn_sched_barrier(0);
+                hold_accumulators<TM * TN>();
+                StaticFor<0, TN>::run([&](auto jj) {
+                    constexpr int i = decltype(ii)::value, j = decltype(jj)::value, t = (decltype(first)::value + i) * TN + j;
+                    *reinterpret_cast<v4i*>(mine + (16 * i + row_of_lane(lane & 15)) * PITCH + 16 * j + 4 * (lane >> 4)) = read_acc<t>();
+                });
+            });
+            __builtin_amdgcn_sched_barrier(0);
+            hold_accumulators<TM * TN>();
+        };
+        if constexpr (TM > 4) {
+            if (part) dump(Int<4>());
+            else dump(Int<0>());
+        } else {
+            dump(Int<0>());
+        }
+        const int64_t row0 = m0 + wave_m * Cfg::WM + 64 * part + at_row;
+        v4u res[AHEAD], next_res[AHEAD];
+        float rs[AHEAD], next_rs[AHEAD];
+        auto request = [&](int step) {                           // every address lies inside its matrix
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int64_t row = row0 + (step + k) * ROWS, r = row < a.M ? row : a.M - 1;
+                next_rs[k] = a.row_scale ? a.row_scale[r] : 1.0f;
+                next_res[k] = (v4u){0u, 0u, 0u, 0u};
+                if (e.residual && n > 0) next_res[k] = *reinterpret_cast<const v4u*>(address<F32>(e.residual, e.ld_res, r, col));
+            }
+        };
+        request(0);
+#pragma unroll 1
+        for (int step = 0; step < STEPS; step += AHEAD) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                rs[k] = next_rs[k];
+                res[k] = next_res[k];
+            }
+            if (step + AHEAD < STEPS) request(step + AHEAD);
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int64_t row = row0 + (step + k) * ROWS;
+                const int32_t* from = mine + ((step + k) * ROWS + at_row) * PITCH + at_col;
+                v4i x[W / 4];
+#pragma unroll
+                for (int q = 0; q < W / 4; ++q) x[q] = *reinterpret_cast<const v4i*>(from + 4 * q);
+                float z[W], y[W];
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    z[j] = ((float)x[j / 4][j % 4] * rs[k]) * cs[j] + bias[j];
+                    y[j] = activation<ACT>(z[j]) + P::get(res[k], j);
+                }
+                if (row >= a.M || n <= 0) continue;
+                if (e.Z) P::store(address<F32>(e.Z, e.ld_z, row, col), P::put(z), n);
+                P::store(address<F32>(a.C, a.ldc, row, col), P::put(y), n);
+            }
+        }
+    }
+}
+
+template <int TM, int TN>
+__global__ void __launch_bounds__(256, 1) __attribute__((aligned(8192)))
+gemm_i8_epilogue_kernel(GemmArgs a, EpilogueArgs e, int tiles_m, int tiles_n) {
+    using Cfg = GemmCfg<TM, TN, true>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int tile_m, tile_n;
+    tile_of_block<Cfg::GROUP_M>(blockIdx.x, tiles_m, tiles_n, tile_m, tile_n);
+    // the divisions run in vector registers; what follows from them belongs in scalar ones
+    const int64_t m0 = (int64_t)__builtin_amdgcn_readfirstlane(tile_m) * Cfg::BM, n0 = (int64_t)__builtin_amdgcn_readfirstlane(tile_n) * Cfg::BN;
+    main_loop<Cfg, true, false>(a, m0, n0, wave, lane, smem);
+    with_activation(e.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+        if (a.c_is_f32) finish_tile<Cfg, true, ACT>(a, e, m0, n0, wave, lane, smem);
+        else finish_tile<Cfg, false, ACT>(a, e, m0, n0, wave, lane, smem);
+    });
+}
+
+// One value: z to Z, act(z) + residual to C.
+template <bool F32>
+__device__ __forceinline__ void finish_one(const GemmArgs& a, const EpilogueArgs& e, int64_t row, int64_t col, float z) {
+    auto load = [](const char* p) {
+        return F32 ? *reinterpret_cast<const float*>(p) : __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+    };
+    auto store = [](char* p, float x) {
+        if constexpr (F32) *reinterpret_cast<float*>(p) = x;
+        else *reinterpret_cast<uint16_t*>(p) = bf16_bits(x);
+    };
+    float y = 0.0f;
+    with_activation(e.act, [&](auto act) { y = activation<decltype(act)::value>(z); });
+    if (e.residual) y += load(address<F32>(e.residual, e.ld_res, row, col));
+    if (e.Z) store(address<F32>(e.Z, e.ld_z, row, col), z);
+    store(address<F32>(a.C, a.ldc, row, col), y);
+}
+
+template <int TM, int TN>
+__global__ void __launch_bounds__(256) gemm_i8_epilogue_small_kernel(GemmArgs a, EpilogueArgs e, int tiles_n) {
+    using Sums = SmallSums<SmallCfg<TM, TN, true>>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    Sums s;
+    small_sums<TM, TN, true>(a, blockIdx.x, tiles_n, smem, s);
+    if (s.row >= a.M) return;
+    const float rs = a.row_scale ? a.row_scale[s.row] : 1.0f;
+#pragma unroll
+    for (int j = 0; j < Sums::EPT; ++j) {
+        const int64_t col = s.col + j;
+        if (col >= a.N) break;
+        const float z = ((float)s.v[j / Sums::VW][j % Sums::VW] * rs) * (a.col_scale ? a.col_scale[col] : 1.0f) + bias_at(e, col);
+        if (a.c_is_f32) finish_one<true>(a, e, s.row, col, z);
+        else finish_one<false>(a, e, s.row, col, z);
+    }
+}
+
+// One thread per output, for what the tiles do not take: K = 0, and row pitches so large that the rows of a tile do not fit one
+// buffer's 4 GiB.
+__global__ void __launch_bounds__(256) gemm_i8_epilogue_plain_kernel(GemmArgs a, EpilogueArgs e) {
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < a.M * a.N; at += (int64_t)gridDim.x * 256) {
+        const int64_t row = at / a.N, col = at % a.N;
+        int acc = 0;
+        for (int64_t k = 0; k < a.K; ++k) acc += (int)a.A[row * a.lda + k] * (int)a.B[col * a.ldb + k];
+        const float z = ((float)acc * (a.row_scale ? a.row_scale[row] : 1.0f)) * (a.col_scale ? a.col_scale[col] : 1.0f) + bias_at(e, col);
+        if (a.c_is_f32) finish_one<true>(a, e, row, col, z);
+        else finish_one<false>(a, e, row, col, z);
+    }
+}
+
+inline int64_t tiles(int64_t n, int t) { return (n + t - 1) / t; }
+
+template <int TM, int TN>
+hipError_t launch_tiled(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
+    using Cfg = GemmCfg<TM, TN, true>;
+    static std::once_flag once;
+    static hipError_t attr_result = hipSuccess;
+    auto kern = gemm_i8_epilogue_kernel<TM, TN>;
+    const hipError_t err = raise_lds_limit(kern, Cfg::LDS_BYTES, &once, &attr_result);
+    if (err != hipSuccess) return err;
+    const int tiles_m = (int)tiles(a.M, Cfg::BM), tiles_n = (int)tiles(a.N, Cfg::BN);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(Cfg::NT), Cfg::LDS_BYTES, s, a, e, tiles_m, tiles_n);
+    return hipGetLastError();
+}
+
+template <int TM, int TN>
+hipError_t launch_split(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
+    using Cfg = SmallCfg<TM, TN, true>;
+    static std::once_flag once;
+    static hipError_t attr_result = hipSuccess;
+    auto kern = gemm_i8_epilogue_small_kernel<TM, TN>;
+    const hipError_t err = raise_lds_limit(kern, Cfg::LDS_BYTES, &once, &attr_result);
+    if (err != hipSuccess) return err;
+    const int64_t blocks = tiles(a.M, Cfg::BM) * tiles(a.N, Cfg::BN);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), Cfg::LDS_BYTES, s, a, e, (int)tiles(a.N, Cfg::BN));
+    return hipGetLastError();
+}
+template <int TM>
+hipError_t launch_split_by_columns(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
+    const int columns = small_tile_columns(a);
+    if (columns == 16) return launch_split<TM, 1>(a, e, s);
+    if (columns == 32) return launch_split<TM, 2>(a, e, s);
+    return launch_split<TM, 4>(a, e, s);
+}
+
+}  // namespace
+
+hipError_t launch_gemm_i8_epilogue(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
+    if (a.M == 0 || a.N == 0) return hipSuccess;
+    if (!a.transB || !a.C || a.acc_out || a.left_stages || a.lr_rank) return hipErrorInvalidValue;
+    if (!tiles_can_run(a)) {
+        const int64_t blocks = std::min(tiles(a.M * a.N, 256), int64_t(1) << 20);
+        hipLaunchKernelGGL(gemm_i8_epilogue_plain_kernel, dim3((unsigned)blocks), dim3(256), 0, s, a, e);
+        return hipGetLastError();
+    }
+    switch (a.config < 0 ? choose_config(a, nullptr) : a.config) {
+        case 0:
+        case 1: return launch_tiled<8, 8>(a, e, s);
+        case 2: return launch_tiled<8, 4>(a, e, s);
+        case 3:
+        case 4: return launch_tiled<4, 4>(a, e, s);
+        case kSmall64: return launch_split<4, 4>(a, e, s);
+        case kSmall32: return a.M <= 16 ? launch_split_by_columns<1>(a, e, s) : launch_split_by_columns<2>(a, e, s);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+}  // namespace halo

@@ -494,6 +494,40 @@ halo_status halo_gemm_i8_desc(const halo_gemm_desc* g, void* stream) {
     return from_hip(launch_gemm_i8(a, reinterpret_cast<hipStream_t>(stream)));
 }
 
+// What halo_epilogue says of a product that check_gemm has passed.
+static halo_status check_epilogue(const halo_epilogue* e, const GemmArgs& a, EpilogueArgs* out) {
+    const int dt = a.c_is_f32 ? HALO_F32 : HALO_BF16;
+    if (e->activation < HALO_ACT_NONE || e->activation > HALO_ACT_SILU) return HALO_EINVAL;
+    if (e->bias && e->bias_dt != HALO_BF16 && e->bias_dt != HALO_F32) return HALO_EINVAL;
+    if (!aligned16(e->bias)) return HALO_EALIGN;
+    const int64_t per16 = dt == HALO_BF16 ? 8 : 4;
+    if (e->residual) {
+        if (e->ld_res < a.N || (e->residual == a.C && e->ld_res != a.ldc)) return HALO_ESHAPE;
+        if (!aligned16(e->residual) || e->ld_res % per16) return HALO_EALIGN;
+    }
+    if (e->Z) {
+        if (e->Z == a.C || e->Z == e->residual) return HALO_EINVAL;
+        if (e->ld_z < a.N) return HALO_ESHAPE;
+        if (!aligned16(e->Z) || e->ld_z % per16) return HALO_EALIGN;
+    }
+    *out = EpilogueArgs{e->bias, e->bias_dt == HALO_F32 ? 1 : 0, e->activation, e->residual, e->ld_res, e->Z, e->ld_z};
+    return HALO_OK;
+}
+
+halo_status halo_gemm_i8_epilogue(const halo_gemm_desc* g, const halo_epilogue* e, void* stream) {
+    if (!g || !e) return HALO_EINVAL;
+    GemmArgs a;
+    bool skip;
+    halo_status st = check_gemm(g, &a, &skip);
+    if (st != HALO_OK || skip) return st;
+    if (!g->C || g->acc_out) return HALO_EINVAL;
+    if (!g->transB) return HALO_EUNSUPPORTED;
+    EpilogueArgs x;
+    st = check_epilogue(e, a, &x);
+    if (st != HALO_OK) return st;
+    return from_hip(launch_gemm_i8_epilogue(a, x, reinterpret_cast<hipStream_t>(stream)));
+}
+
 halo_status halo_mfma_i8_probe(const int8_t* operands, int32_t iters, int32_t* sink, void* stream) {
     if (!operands || iters < 0) return HALO_EINVAL;
     if (!aligned16(operands)) return HALO_EALIGN;
@@ -611,9 +645,9 @@ size_t halo_linear_workspace_bytes(const halo_linear_desc* desc) {
     return bwd_layout(desc).total;
 }
 
-halo_status halo_linear_fwd(const halo_linear_desc* desc, const void* X, const void* W, void* Y, int8_t* Xq,
-                            float* s_x, int8_t* Wq, float* s_w, void* workspace, size_t workspace_bytes,
-                            void* stream) {
+halo_status halo_linear_fwd_epilogue(const halo_linear_desc* desc, const void* X, const void* W, void* Y, int8_t* Xq, float* s_x,
+                                     int8_t* Wq, float* s_w, const halo_epilogue* e, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
     int32_t hm, hb;
     halo_status st = resolve_desc(desc, &hm, &hb);
     if (st != HALO_OK) return st;
@@ -623,6 +657,16 @@ halo_status halo_linear_fwd(const halo_linear_desc* desc, const void* X, const v
     if ((X && !aligned16(X)) || (W && !aligned16(W)) || !aligned16(Y) || !aligned16(Xq) || !aligned16(Wq))
         return HALO_EALIGN;
     const halo_dtype odt = (halo_dtype)desc->out_dt;
+    const halo_gemm_desc gemm{Xq, m, Wq, m, 1, b, n, m, s_x, s_w, Y, (int32_t)odt, n, nullptr, 0, HALO_GEMM_AUTO};
+    if (e) {                                                     // before anything is enqueued
+        GemmArgs a;
+        EpilogueArgs x;
+        bool skip;
+        st = check_gemm(&gemm, &a, &skip);
+        if (st == HALO_OK) st = check_epilogue(e, a, &x);
+        if (st != HALO_OK) return st;
+    }
+    auto product = [&]() { return e ? halo_gemm_i8_epilogue(&gemm, e, stream) : halo_gemm_i8_desc(&gemm, stream); };
     const bool tensor = desc->scale_mode == HALO_SCALE_PER_TENSOR;
     if (tensor && (X || W)) {
         // one scale per tensor (the paper's quantiser): two passes per operand, scratch from the workspace
@@ -650,7 +694,7 @@ halo_status halo_linear_fwd(const halo_linear_desc* desc, const void* X, const v
             r.given_amax = max_x; r.given_parts = (int)parts[0]; r.out_scale = s_x;
             r.given_amax2 = max_w; r.given_parts2 = (int)parts[1]; r.out_scale2 = s_w;
             if (launch_row_transform(r, IN_BF16, OUT_Q8, hs) != hipSuccess) return HALO_EHIP;
-            return halo_gemm_i8(Xq, m, Wq, m, 1, b, n, m, s_x, s_w, Y, odt, n, nullptr, 0, stream);
+            return product();
         }
         if (X) {
             st = halo_hadamard_quant_tensor(X, HALO_BF16, b, m, m, HALO_QUANT_ROWS, hm, 0, Xq, m, s_x, tq, tq_bytes, stream);
@@ -660,7 +704,7 @@ halo_status halo_linear_fwd(const halo_linear_desc* desc, const void* X, const v
             st = halo_hadamard_quant_tensor(W, HALO_BF16, n, m, m, HALO_QUANT_ROWS, hm, 0, Wq, m, s_w, tq, tq_bytes, stream);
             if (st != HALO_OK) return st;
         }
-        return halo_gemm_i8(Xq, m, Wq, m, 1, b, n, m, s_x, s_w, Y, odt, n, nullptr, 0, stream);
+        return product();
     }
     if (X && W && !tensor) {
         // X and W get the same treatment: one launch rotates and quantises both
@@ -669,7 +713,7 @@ halo_status halo_linear_fwd(const halo_linear_desc* desc, const void* X, const v
         set_right_block(r, hm);
         r.rows2 = n; r.in2 = W; r.out2 = Wq; r.out_scale2 = s_w;
         if (launch_row_transform(r, IN_BF16, OUT_Q8, reinterpret_cast<hipStream_t>(stream)) != hipSuccess) return HALO_EHIP;
-        return halo_gemm_i8(Xq, m, Wq, m, 1, b, n, m, s_x, s_w, Y, odt, n, nullptr, 0, stream);
+        return product();
     }
     if (X) {
         st = halo_hadamard_quant(X, HALO_BF16, b, m, m, HALO_QUANT_ROWS, hm, 0, nullptr, Xq, m, s_x, nullptr, 0, stream);
@@ -679,7 +723,12 @@ halo_status halo_linear_fwd(const halo_linear_desc* desc, const void* X, const v
         st = halo_hadamard_quant(W, HALO_BF16, n, m, m, HALO_QUANT_ROWS, hm, 0, nullptr, Wq, m, s_w, nullptr, 0, stream);
         if (st != HALO_OK) return st;
     }
-    return halo_gemm_i8(Xq, m, Wq, m, 1, b, n, m, s_x, s_w, Y, odt, n, nullptr, 0, stream);
+    return product();
+}
+
+halo_status halo_linear_fwd(const halo_linear_desc* desc, const void* X, const void* W, void* Y, int8_t* Xq, float* s_x, int8_t* Wq,
+                            float* s_w, void* workspace, size_t workspace_bytes, void* stream) {
+    return halo_linear_fwd_epilogue(desc, X, W, Y, Xq, s_x, Wq, s_w, nullptr, workspace, workspace_bytes, stream);
 }
 
 halo_status halo_linear_bwd(const halo_linear_desc* desc, const void* E, const int8_t* Xq, const float* s_x,

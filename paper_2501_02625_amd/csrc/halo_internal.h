@@ -170,6 +170,17 @@ hipError_t launch_dual_quant_static(DualQuantArgs a, hipStream_t s);
 constexpr int kMaxLowRank = 64;
 hipError_t launch_gemm_i8(const GemmArgs& a, hipStream_t s);
 hipError_t launch_gemm_i8_pair(const GemmArgs& a1, const GemmArgs& a2, hipStream_t s);
+// The same with bias, activation and residual behind it (K-contiguous B, C required, no acc_out).
+struct EpilogueArgs {
+    const void* bias;        // [N], may be null
+    int bias_f32;
+    int act;                 // halo_activation
+    const void* residual;    // [M x N] of C's type, may be null
+    int64_t ld_res;
+    void* Z;                 // the same, may be null
+    int64_t ld_z;
+};
+hipError_t launch_gemm_i8_epilogue(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s);
 // True if `cfg` names a tile configuration that can run a product with reduction length K.
 bool gemm_config_valid(int cfg, int64_t K);
 // 256 workgroups x 8 wavefronts x iters x 32 MFMAs on the 4 KB of operand bytes at `operands`.

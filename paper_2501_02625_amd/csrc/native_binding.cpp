@@ -17,6 +17,9 @@
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
+#include <vector>
+
 #include "halo.h"
 
 namespace {
@@ -450,6 +453,240 @@ PyObject* adapters_bwd(PyObject* const* a) {
     return Py_BuildValue("(NNN)", wrap_or_none(want_ex, EX), wrap_or_none(want_gu, GU), wrap_or_none(want_gv, GV));
 }
 
+// What runs on the current device's stream has its memory there.
+void on_current_device(const Context& c, std::initializer_list<const at::Tensor*> all) {
+    for (const at::Tensor* t : all) {
+        if (!t || t->device().index() == c.device) continue;
+        PyErr_SetString(PyExc_ValueError, "tensors are on the current device");
+        throw Failed();
+    }
+}
+// None, or a dense vector of n elements, of one of the two types.
+bool vector_of(const at::Tensor* t, int64_t n) {
+    return !t || (t->dim() == 1 && t->size(0) == n && t->is_contiguous() &&
+                  (t->scalar_type() == at::kBFloat16 || t->scalar_type() == at::kFloat));
+}
+bool floats(const at::Tensor* t, int64_t n) { return vector_of(t, n) && (!t || t->scalar_type() == at::kFloat); }
+at::Tensor scratch_of(const at::Tensor* given, size_t need, const at::Tensor& like, const Context& c) {
+    return given ? *given : new_tensor({(int64_t)(need > 16 ? need : 16)}, at::kByte, like, c.device);
+}
+
+// bias, activation, residual, want_z, Z of a product [M x N] of the type
+struct Epilogue {
+    const at::Tensor *bias, *residual;
+    at::Tensor Z;
+    halo_epilogue e{};
+    bool want_z;
+    Epilogue(PyObject* b, PyObject* act, PyObject* res, PyObject* want, PyObject* z, int64_t M, int64_t N, at::ScalarType type,
+             const at::Tensor& like, const Context& c, bool padded)
+        : bias(tensor(b)), residual(tensor(res)), want_z(want == Py_True || z != Py_None) {
+        const at::Tensor* given = tensor(z);
+        require(vector_of(bias, N), "bias is a bf16 or fp32 vector, one element for each column");
+        require(matrix(residual, M, N, type) && matrix(given, M, N, type), "residual and Z are matrices like the output, with contiguous rows");
+        if (given) Z = *given;
+        else if (want_z) Z = padded ? new_padded(M, N, type, like, c.device) : new_tensor({M, N}, type, like, c.device);
+        e.bias = data(bias); e.bias_dt = bias ? dtype_code(*bias) : HALO_F32;
+        e.activation = (int32_t)integer(act);
+        e.residual = data(residual); e.ld_res = pitch(residual);
+        e.Z = data(Z); e.ld_z = Z.defined() ? pitch(&Z) : 0;
+        on_current_device(c, {bias, residual, given});
+    }
+};
+
+// a, b, row_scale, col_scale, bias, activation, residual, dtype of a new output, want_z, out, Z
+PyObject* gemm_i8_epilogue(PyObject* const* a) {
+    const at::Tensor *A = tensor(a[0]), *B = tensor(a[1]), *rs = tensor(a[2]), *cs = tensor(a[3]), *out = tensor(a[9]);
+    require(A && B && A->dim() == 2 && B->dim() == 2 && A->size(1) == B->size(1), "operands are int8 matrices that fit together");
+    const int64_t M = A->size(0), K = A->size(1), N = B->size(0);
+    require(matrix(A, M, K, at::kChar) && matrix(B, N, K, at::kChar), "operands are int8 matrices with contiguous rows");
+    require(floats(rs, M) && floats(cs, N), "row_scale is fp32 [M], col_scale fp32 [N]");
+    const at::ScalarType type = out ? out->scalar_type() : out_dtype(integer(a[7]));
+    require(matrix(out, M, N, type), "out is [M, N] with contiguous rows");
+    const Context c;
+    on_current_device(c, {A, B, rs, cs, out});
+    const at::Tensor C = out ? *out : new_padded(M, N, type, *A, c.device);
+    const Epilogue f(a[4], a[5], a[6], a[8], a[10], M, N, type, *A, c, true);
+    // the pitch of a matrix of one row does not matter, but has to be one that int8 rows can have
+    const int64_t lda = M > 1 ? A->stride(0) : (K + 15) / 16 * 16, ldb = N > 1 ? B->stride(0) : (K + 15) / 16 * 16;
+    const halo_gemm_desc g{(int8_t*)data(A), lda, (int8_t*)data(B), ldb, 1, M, N, K, (float*)data(rs), (float*)data(cs), data(C),
+                           (int32_t)dtype_code(C), pitch(&C), nullptr, 0, HALO_GEMM_AUTO};
+    const halo_status st = without_gil(halo_gemm_i8_epilogue, &g, &f.e, c.stream);
+    if (st != HALO_OK) return PyLong_FromLong(st);
+    return Py_BuildValue("(NN)", wrap(C), wrap_or_none(f.want_z, f.Z));
+}
+
+// desc, X, W, Xq, s_x, Wq, s_w, Y, workspace, new_state, bias, activation, residual, want_z, Z
+PyObject* linear_fwd_epilogue(PyObject* const* a) {
+    const Desc desc(a[0]);
+    const halo_linear_desc& d = *desc.d;
+    const at::Tensor *X = tensor(a[1]), *W = tensor(a[2]), *xq = tensor(a[3]), *sx = tensor(a[4]), *wq = tensor(a[5]),
+                     *sw = tensor(a[6]), *y = tensor(a[7]), *ws = tensor(a[8]);
+    const bool make = a[9] == Py_True;
+    const at::Tensor* like = X ? X : xq;
+    require(like != nullptr, "X or a state is needed");
+    require((!X || (matrix(X, d.b, d.m, at::kBFloat16) && X->is_contiguous())) && (!W || (matrix(W, d.n, d.m, at::kBFloat16) && W->is_contiguous())),
+            "X [b, m] and W [n, m] are contiguous bf16");
+    require(!y || (matrix(y, d.b, d.n, desc.out_type()) && y->is_contiguous()), "Y is [b, n] of the output's type, contiguous");
+    const Context c;
+    on_current_device(c, {X, W, xq, sx, wq, sw, y, ws});
+    const at::Tensor Xq = output(xq, make, {d.b, d.m}, at::kChar, *like, c), s_x = output(sx, make, {d.b}, at::kFloat, *like, c),
+                     Wq = output(wq, make, {d.n, d.m}, at::kChar, *like, c), s_w = output(sw, make, {d.n}, at::kFloat, *like, c),
+                     Y = output(y, true, {d.b, d.n}, desc.out_type(), *like, c);
+    const Epilogue f(a[10], a[11], a[12], a[13], a[14], d.b, d.n, desc.out_type(), *like, c, false);
+    at::Tensor scratch;
+    if (!ws && d.scale_mode == HALO_SCALE_PER_TENSOR) {
+        scratch = scratch_of(nullptr, halo_linear_workspace_bytes(&d), *like, c);
+        ws = &scratch;
+    }
+    const halo_status st = without_gil(
+        halo_linear_fwd_epilogue, &d, data(X), data(W), data(Y), (int8_t*)data(Xq), (float*)data(s_x), (int8_t*)data(Wq),
+        (float*)data(s_w), &f.e, data(ws), bytes(ws), c.stream);
+    if (st != HALO_OK) return PyLong_FromLong(st);
+    return Py_BuildValue("(NNNNNN)", wrap(Y), wrap(Xq), wrap(s_x), wrap(Wq), wrap(s_w), wrap_or_none(f.want_z, f.Z));
+}
+
+// E, Z, activation, want_ez, want_gb, EZ, GB, workspace
+PyObject* activation_bwd(PyObject* const* a) {
+    const at::Tensor *E = tensor(a[0]), *Z = tensor(a[1]), *ez = tensor(a[5]), *gb = tensor(a[6]), *ws = tensor(a[7]);
+    const long act = integer(a[2]);
+    const bool want_ez = a[3] == Py_True, want_gb = a[4] == Py_True;
+    require(E && E->dim() == 2, "E is a matrix with contiguous rows");
+    const int64_t rows = E->size(0), cols = E->size(1);
+    const at::ScalarType type = E->scalar_type();
+    const halo_dtype dt = dtype_code(*E);
+    require(matrix(E, rows, cols, type) && matrix(Z, rows, cols, type) && matrix(ez, rows, cols, type),
+            "E, Z and EZ are matrices of one shape and type, with contiguous rows");
+    require(floats(gb, cols), "GB is fp32, one element for each column");
+    const Context c;
+    on_current_device(c, {E, Z, ez, gb, ws});
+    const at::Tensor EZ = want_ez && !ez ? new_padded(rows, cols, type, *E, c.device) : output(want_ez ? ez : nullptr, false, {}, type, *E, c),
+                     GB = output(want_gb ? gb : nullptr, want_gb, {cols}, at::kFloat, *E, c);
+    at::Tensor W;
+    if (want_gb) W = scratch_of(ws, halo_activation_bwd_workspace_bytes(rows, cols), *E, c);
+    const halo_status st = without_gil(halo_activation_bwd, data(E), pitch(E), data(Z), pitch(Z), dt, rows, cols, (halo_activation)act, data(EZ),
+                                       want_ez ? pitch(&EZ) : 0, (float*)data(GB), data(W), W.defined() ? bytes(&W) : 0, c.stream);
+    if (st != HALO_OK) return PyLong_FromLong(st);
+    return Py_BuildValue("(NN)", wrap_or_none(want_ez, EZ), wrap_or_none(want_gb, GB));
+}
+
+halo_norm_desc norm_desc(const at::Tensor& x, const at::Tensor* weight, const at::Tensor* bias, long kind, double eps) {
+    require(vector_of(weight, x.size(1)) && vector_of(bias, x.size(1)) && (!weight || !bias || weight->scalar_type() == bias->scalar_type()),
+            "weight and bias are vectors of one type, bf16 or fp32, one element for each column");
+    const at::Tensor* w = weight ? weight : bias;
+    return halo_norm_desc{x.size(0), x.size(1), (int32_t)kind, (int32_t)dtype_code(x), w ? (int32_t)dtype_code(*w) : (int32_t)HALO_F32, 0, eps};
+}
+
+// X, weight, bias, eps, kind, want_stats, Y, mean, rstd
+PyObject* layer_norm_fwd(PyObject* const* a) {
+    const at::Tensor *X = tensor(a[0]), *w = tensor(a[1]), *b = tensor(a[2]), *y = tensor(a[6]), *m = tensor(a[7]), *r = tensor(a[8]);
+    require(X && X->dim() == 2, "X is a matrix with contiguous rows");
+    const long kind = integer(a[4]);
+    const halo_norm_desc d = norm_desc(*X, w, b, kind, real(a[3]));
+    require(matrix(X, d.rows, d.cols, X->scalar_type()) && matrix(y, d.rows, d.cols, X->scalar_type()), "X and Y are matrices of one shape and type, with contiguous rows");
+    require(floats(m, d.rows) && floats(r, d.rows), "mean and rstd are fp32, one element for each row");
+    const bool stats = a[5] == Py_True, want_mean = (stats || m) && kind == HALO_NORM_LAYER, want_rstd = stats || r;
+    const Context c;
+    on_current_device(c, {X, w, b, y, m, r});
+    const at::Tensor Y = y ? *y : new_padded(d.rows, d.cols, X->scalar_type(), *X, c.device),
+                     mean = output(want_mean ? m : nullptr, want_mean, {d.rows}, at::kFloat, *X, c),
+                     rstd = output(r, want_rstd, {d.rows}, at::kFloat, *X, c);
+    const halo_status st = without_gil(halo_layer_norm_fwd, &d, data(X), pitch(X), data(w), data(b), data(Y), pitch(&Y), (float*)data(mean),
+                                       (float*)data(rstd), c.stream);
+    if (st != HALO_OK) return PyLong_FromLong(st);
+    return Py_BuildValue("(NNN)", wrap(Y), wrap_or_none(want_mean, mean), wrap_or_none(want_rstd, rstd));
+}
+
+// E, X, mean, rstd, weight, kind, base, want_ex, want_gw, want_gb, EX, GW, GB, workspace
+PyObject* layer_norm_bwd(PyObject* const* a) {
+    const at::Tensor *E = tensor(a[0]), *X = tensor(a[1]), *m = tensor(a[2]), *r = tensor(a[3]), *w = tensor(a[4]), *base = tensor(a[6]),
+                     *ex = tensor(a[10]), *gw = tensor(a[11]), *gb = tensor(a[12]), *ws = tensor(a[13]);
+    const bool want_ex = a[7] == Py_True, want_gw = a[8] == Py_True, want_gb = a[9] == Py_True;
+    require(E && E->dim() == 2, "E is a matrix with contiguous rows");
+    const halo_norm_desc d = norm_desc(*E, w, nullptr, integer(a[5]), 0.0);
+    const at::ScalarType type = E->scalar_type();
+    require(matrix(E, d.rows, d.cols, type) && matrix(X, d.rows, d.cols, type) && matrix(base, d.rows, d.cols, type) && matrix(ex, d.rows, d.cols, type),
+            "E, X, base and EX are matrices of one shape and type, with contiguous rows");
+    require(floats(m, d.rows) && floats(r, d.rows), "mean and rstd are fp32, one element for each row");
+    require(floats(gw, d.cols) && floats(gb, d.cols), "GW and GB are fp32, one element for each column");
+    const Context c;
+    on_current_device(c, {E, X, m, r, w, base, ex, gw, gb, ws});
+    const at::Tensor EX = want_ex && !ex ? new_padded(d.rows, d.cols, type, *E, c.device) : output(want_ex ? ex : nullptr, false, {}, type, *E, c),
+                     GW = output(want_gw ? gw : nullptr, want_gw, {d.cols}, at::kFloat, *E, c),
+                     GB = output(want_gb ? gb : nullptr, want_gb, {d.cols}, at::kFloat, *E, c);
+    at::Tensor W;
+    if (want_gw || want_gb) W = scratch_of(ws, halo_layer_norm_bwd_workspace_bytes(&d), *E, c);
+    const halo_status st = without_gil(
+        halo_layer_norm_bwd, &d, data(E), pitch(E), data(X), pitch(X), (float*)data(m), (float*)data(r), data(w), data(base), pitch(base), data(EX),
+        want_ex ? pitch(&EX) : 0, (float*)data(GW), (float*)data(GB), data(W), W.defined() ? bytes(&W) : 0, c.stream);
+    if (st != HALO_OK) return PyLong_FromLong(st);
+    return Py_BuildValue("(NNN)", wrap_or_none(want_ex, EX), wrap_or_none(want_gw, GW), wrap_or_none(want_gb, GB));
+}
+
+// A list or tuple of tensors, or None (an empty one).
+struct Tensors {
+    PyObject* fast = nullptr;
+    Py_ssize_t n = 0;
+    explicit Tensors(PyObject* o) {
+        if (o == Py_None) return;
+        fast = PySequence_Fast(o, "expected a list of tensors");
+        if (!fast) throw Failed();
+        n = PySequence_Fast_GET_SIZE(fast);
+    }
+    ~Tensors() { Py_XDECREF(fast); }
+    Tensors(const Tensors&) = delete;
+    const at::Tensor* at(Py_ssize_t i) const { return fast ? tensor(PySequence_Fast_GET_ITEM(fast, i)) : nullptr; }
+};
+// A number, or a tensor of one element of the type: its address, and `none` for the number.
+template <class T, class F>
+const T* number_or_address(PyObject* o, at::ScalarType type, const Context& c, const F& number) {
+    if (!THPVariable_Check(o)) {
+        number();
+        return nullptr;
+    }
+    const at::Tensor* t = tensor(o);
+    require(t->numel() == 1 && t->scalar_type() == type, "step is int64, lr and grad_scale are fp32, of one element");
+    on_current_device(c, {t});
+    return (const T*)t->data_ptr();
+}
+
+// params, grads, m, v, masters, m_scales, v_scales, step, lr, beta1, beta2, eps, weight_decay, grad_scale, seed, offset
+PyObject* adamw(PyObject* const* a) {
+    const Tensors p(a[0]), g(a[1]), m(a[2]), v(a[3]), master(a[4]), ms(a[5]), vs(a[6]);
+    require(g.n == p.n && m.n == p.n && v.n == p.n && (!master.fast || master.n == p.n) && (!ms.fast || ms.n == p.n) &&
+                (!vs.fast || vs.n == p.n),
+            "the lists have one entry for each parameter");
+    const Context c;
+    halo_adamw_desc d{};
+    d.state_bits = 32;
+    d.step = 1;
+    d.step_ptr = number_or_address<int64_t>(a[7], at::kLong, c, [&] { d.step = integer(a[7]); });
+    d.lr_ptr = number_or_address<float>(a[8], at::kFloat, c, [&] { d.lr = real(a[8]); });
+    d.beta1 = real(a[9]); d.beta2 = real(a[10]); d.eps = real(a[11]); d.weight_decay = real(a[12]);
+    d.grad_scale_ptr = number_or_address<float>(a[13], at::kFloat, c, [&] { d.grad_scale = real(a[13]); });
+    d.seed = word64(a[14]); d.offset = word64(a[15]);
+    std::vector<halo_adamw_tensor> list((size_t)p.n);
+    for (Py_ssize_t i = 0; i < p.n; ++i) {
+        const at::Tensor *P = p.at(i), *G = g.at(i), *M = m.at(i), *V = v.at(i), *R = master.at(i), *SM = ms.at(i), *SV = vs.at(i);
+        require(P && G && M && V, "every parameter has a gradient, m and v");
+        const int64_t n = P->numel(), blocks = (n + HALO_ADAMW_BLOCK - 1) / HALO_ADAMW_BLOCK;
+        const bool eight = M->scalar_type() == at::kFloat8_e4m3fn;
+        for (const at::Tensor* t : {P, G, M, V, R})
+            require(!t || (t->numel() == n && t->is_contiguous()), "what belongs to a parameter has its number of elements and is contiguous");
+        require(M->scalar_type() == V->scalar_type() && (eight || M->scalar_type() == at::kFloat), "m and v are fp32, or both float8_e4m3fn");
+        require(!eight || (SM && SV && floats(SM, blocks) && floats(SV, blocks)), "states in 8 bits have fp32 scales, one for 256 elements");
+        require(!R || R->scalar_type() == at::kFloat, "masters are fp32");
+        const int32_t pd = dtype_code(*P), gd = dtype_code(*G), bits = eight ? 8 : 32;
+        require(i == 0 || (pd == d.param_dt && gd == d.grad_dt && bits == d.state_bits), "all parameters, all gradients and all states have one type");
+        d.param_dt = pd; d.grad_dt = gd; d.state_bits = bits;
+        on_current_device(c, {P, G, M, V, R, eight ? SM : nullptr, eight ? SV : nullptr});
+        list[(size_t)i] = halo_adamw_tensor{n, data(P), data(G), data(M), data(V), (float*)data(R), eight ? (float*)data(SM) : nullptr,
+                                            eight ? (float*)data(SV) : nullptr};
+    }
+    const halo_status st = without_gil(halo_adamw, (const halo_adamw_desc*)&d, (const halo_adamw_tensor*)list.data(), (int32_t)p.n, c.stream);
+    if (st != HALO_OK) return PyLong_FromLong(st);
+    Py_RETURN_NONE;
+}
+
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t count) {
     if (count != N) {
@@ -473,7 +710,9 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t count) {
 PyMethodDef methods[] = {HALO_ENTRY(linear_fwd, 10), HALO_ENTRY(linear_bwd, 11), HALO_ENTRY(peft_fwd, 9), HALO_ENTRY(peft_bwd, 15),
                          HALO_ENTRY(mx6_quant, 4),  HALO_ENTRY(gemm_mx6, 6),    HALO_ENTRY(hadamard_quant, 8),
                          HALO_ENTRY(gemm_i8, 9),    HALO_ENTRY(dropout, 6),     HALO_ENTRY(adapters_fwd, 14),
-                         HALO_ENTRY(adapters_bwd, 20), {nullptr, nullptr, 0, nullptr}};
+                         HALO_ENTRY(adapters_bwd, 20), HALO_ENTRY(gemm_i8_epilogue, 11), HALO_ENTRY(linear_fwd_epilogue, 15),
+                         HALO_ENTRY(activation_bwd, 8), HALO_ENTRY(layer_norm_fwd, 9), HALO_ENTRY(layer_norm_bwd, 14),
+                         HALO_ENTRY(adamw, 16), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_halo_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
