@@ -9,7 +9,7 @@
 #include <cmath>
 
 #include "around.h"
-#include "eight.h"
+#include "halo_internal.h"
 #include "philox.h"
 
 namespace halo {
@@ -17,7 +17,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBlock = 256;                  // elements that share a scale: 32 lanes of eight
-constexpr int kPerGroup = kThreads * 8;      // elements of a workgroup
+constexpr int kRounds = 2;                   // groups of eight elements per thread, all loads issued before the first is used
+constexpr int kPerRound = kThreads * 8, kPerGroup = kPerRound * kRounds;      // elements of a workgroup
 constexpr int kTensors = 48;                 // of a launch; they come as arguments, of which a kernel has 4 KB
 
 struct Batch {
@@ -30,36 +31,152 @@ static_assert(sizeof(Batch) <= 4096, "kernel arguments");
 
 enum { PARAM_F32, PARAM_BF16, PARAM_MASTER };
 
-// The code of the e4m3 number next to q, 0 <= q <= 448, up or down by the random u.  SQUARE: by q's square.
-template <bool SQUARE>
-__device__ __forceinline__ uint32_t code_of(float q, uint32_t u) {
-    const uint32_t bits = __float_as_uint(q);
-    float lo, step;
-    uint32_t code;
-    if (bits >= 0x3C800000u) {               // 2^-6: three bits of fraction
-        code = (bits >> 20) - (120u << 3);
-        lo = __uint_as_float(bits & 0xFFF00000u);
-        step = __uint_as_float((bits & 0x7F800000u) - (3u << 23));
-    } else {                                 // steps of 2^-9
-        code = (uint32_t)(q * 512.0f);
-        lo = (float)code * 0.001953125f;
-        step = 0.001953125f;
-    }
-    const float r = (float)u;
-    bool up;
-    if constexpr (SQUARE) up = ((q - lo) * (q + lo)) * 65536.0f > r * (step * (lo + step + lo));
-    else up = (q - lo) * 65536.0f > r * step;
-    return code + (up ? 1u : 0u);
+// The upper half of a word of random bits as the upper half of a number, and the lower one: u * 65536.
+__device__ __forceinline__ uint32_t upper_half_of(const uint4& u, int j) {
+    const uint32_t w = j < 2 ? u.x : j < 4 ? u.y : j < 6 ? u.z : u.w;
+    return (j & 1) ? w & 0xFFFF0000u : w << 16;
+}
+__device__ __forceinline__ uint32_t half_of(const uint4& u, int j) {
+    const uint32_t w = j < 2 ? u.x : j < 4 ? u.y : j < 6 ? u.z : u.w;
+    return (j & 1) ? w >> 16 : w & 0xFFFFu;
 }
 
-__device__ __forceinline__ float value_of(uint32_t code) {
-    return __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
+// The code of the e4m3 number next to q, 0 <= q <= 448, up or down by the random bits.  SQUARE: by q's square.  From 2^-6 on a number has
+// three bits of fraction, and whether it goes up is a question about its fraction alone: about the bits behind those three, or, of the square,
+// about f = q over the step, 8 <= f < 16, and k, f rounded down: (f - k)(f + k) against u (2 k + 1).  (All of it but for powers of two, which
+// change no rounding, what the definition says in terms of q, lo and hi.)
+template <bool SQUARE>
+__device__ __forceinline__ uint32_t code_of_normal(float q, const uint4& u, int j) {
+    const uint32_t bits = __float_as_uint(q);
+    bool up;
+    if constexpr (SQUARE) {
+        const uint32_t fb = (bits & 0x007FFFFFu) | 0x41000000u;
+        const float f = __uint_as_float(fb), k = __uint_as_float(fb & 0xFFF00000u);
+        up = (f - k) * (f + k) > (float)half_of(u, j) * __builtin_fmaf(k, 2.0f / 65536.0f, 1.0f / 65536.0f);
+    } else {
+        up = bits << 12 > upper_half_of(u, j);
+    }
+    return (bits >> 20) - (120u << 3) + (up ? 1u : 0u);
 }
+// Below 2^-6 the steps are 2^-9.  A square that is not 0 does not become 0.
+template <bool SQUARE>
+__device__ __forceinline__ uint32_t code_of_small(float q, float x, const uint4& u, int j) {
+    const float t = q * 512.0f, k = __builtin_truncf(t), r = (float)half_of(u, j);
+    bool up;
+    if constexpr (SQUARE) up = (t - k) * (t + k) > r * __builtin_fmaf(k, 2.0f / 65536.0f, 1.0f / 65536.0f);
+    else up = (t - k) * 65536.0f > r;
+    const uint32_t code = (uint32_t)k + (up ? 1u : 0u);
+    return SQUARE && x > 0.0f && code == 0 ? 1u : code;
+}
+// Codes of eight values, signs included (of m).  Small ones are rare, and a wavefront that has none does not look at each.
+template <bool SQUARE>
+__device__ __forceinline__ void codes_of(const float* x, float inverse, const uint4& u, uint32_t* out) {
+    float q[8], least = 448.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        q[j] = __builtin_fminf(__builtin_fabsf(x[j]) * inverse, 448.0f);
+        least = __builtin_fminf(least, q[j]);
+    }
+    uint32_t c[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[j] = code_of_normal<SQUARE>(q[j], u, j);
+    if (__builtin_amdgcn_ballot_w64(least < 0.015625f)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t small = code_of_small<SQUARE>(q[j], x[j], u, j);
+            c[j] = q[j] < 0.015625f ? small : c[j];
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int j = 4 * h + e;
+            w |= c[j] << (8 * e);
+            if constexpr (!SQUARE) w |= (__float_as_uint(x[j]) & 0x80000000u) >> (24 - 8 * e);
+        }
+        out[h] = w;
+    }
+}
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+
+// Eight consecutive elements as they are in memory: fp32, bf16 or e4m3 codes.  n: how many there are (8, but at a tensor's end).
+template <int BYTES>
+struct Run {
+    static constexpr int WORDS = 2 * BYTES;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const void* base, int64_t i, int n) {
+        const char* p = reinterpret_cast<const char*>(base) + i * BYTES;
+        if (n == 8) {
+            if constexpr (BYTES == 1) {
+                const v2u q = __builtin_nontemporal_load(reinterpret_cast<const v2u*>(p));
+                w[0] = q[0]; w[1] = q[1];
+            } else {
+#pragma unroll
+                for (int k = 0; k < WORDS / 4; ++k) {
+                    const v4u q = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p) + k);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[4 * k + e] = q[e];
+                }
+            }
+            return;
+        }
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) w[k] = 0;
+#pragma unroll
+        for (int j = 0; j < 7; ++j) {
+            if (j >= n) break;
+            if constexpr (BYTES == 4) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+            else if constexpr (BYTES == 2) w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
+            else w[j >> 2] |= (uint32_t)reinterpret_cast<const uint8_t*>(p)[j] << (8 * (j & 3));
+        }
+    }
+    __device__ __forceinline__ void store(void* base, int64_t i, int n) const {
+        char* p = reinterpret_cast<char*>(base) + i * BYTES;
+        if (n == 8) {
+            if constexpr (BYTES == 1) {
+                __builtin_nontemporal_store((v2u){w[0], w[1]}, reinterpret_cast<v2u*>(p));
+            } else {
+#pragma unroll
+                for (int k = 0; k < WORDS / 4; ++k)
+                    __builtin_nontemporal_store((v4u){w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]}, reinterpret_cast<v4u*>(p) + k);
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 7; ++j) {
+            if (j >= n) break;
+            if constexpr (BYTES == 4) reinterpret_cast<uint32_t*>(p)[j] = w[j];
+            else if constexpr (BYTES == 2) reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            else reinterpret_cast<uint8_t*>(p)[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+        }
+    }
+    __device__ __forceinline__ void get(float* x) const {
+        if constexpr (BYTES == 4) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+        } else if constexpr (BYTES == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float((j & 1) ? w[j >> 1] & 0xFFFF0000u : w[j >> 1] << 16);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[k], true);
+                x[4 * k] = lo[0]; x[4 * k + 1] = lo[1]; x[4 * k + 2] = hi[0]; x[4 * k + 3] = hi[1];
+            }
+        }
+    }
+};
 
 template <int PARAM, bool GRAD32, bool STATE8>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(Batch b) {
-    int t = 0;
-    while (t + 1 < b.count && blockIdx.x >= b.end[t]) ++t;
+    // the tensor: of a wavefront's lanes, those whose tensor ends before this workgroup
+    const int lane = threadIdx.x & 63;
+    const bool behind = lane < kTensors && blockIdx.x >= b.end[lane < kTensors ? lane : 0];
+    const int t = __builtin_amdgcn_readfirstlane(__builtin_popcountll(__builtin_amdgcn_ballot_w64(behind)));
     const AdamwTensor& x = b.tensor[t];
     const uint32_t first = t ? b.end[t - 1] : 0;
     AdamwStep c = b.step;
@@ -73,105 +190,118 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(Batch b) {
         c.rate = (float)(lr / (1.0 - pow(c.beta1_64, (double)c.step)));
         c.root = (float)(1.0 / sqrt(1.0 - pow(c.beta2_64, (double)c.step)));
     }
-    const int64_t i0 = (int64_t)(blockIdx.x - first) * kPerGroup + threadIdx.x * 8;
-    const int n = x.size - i0 >= 8 ? 8 : x.size > i0 ? (int)(x.size - i0) : 0;         // elements of this thread
     DropoutMask d{};
     d.key0 = c.key0; d.key1 = c.key1; d.offset0 = (uint32_t)c.offset; d.offset1 = (uint32_t)(c.offset >> 32);
-    const uint32_t group = (uint32_t)(i0 >> 3), kind0 = 4u * (uint32_t)x.number;
-    float m[8], v[8], p[8], g[8];
+    const uint32_t kind0 = 4u * (uint32_t)x.number;
+    constexpr int PB = PARAM == PARAM_BF16 ? 2 : 4, SB = STATE8 ? 1 : 4;
+    const int64_t start = (int64_t)(blockIdx.x - first) * kPerGroup + threadIdx.x * 8;
+    Run<PB> rp[kRounds];
+    Run<GRAD32 ? 4 : 2> rg[kRounds];
+    Run<SB> rm[kRounds], rv[kRounds];
+    float sm[kRounds], sv[kRounds];
+    int left[kRounds];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        m[j] = v[j] = p[j] = g[j] = 0.0f;
-        if (j >= n) continue;
-        const int64_t i = i0 + j;
-        if constexpr (GRAD32) g[j] = reinterpret_cast<const float*>(x.grad)[i];
-        else g[j] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(x.grad)[i] << 16);
-        if constexpr (PARAM == PARAM_F32) p[j] = reinterpret_cast<const float*>(x.param)[i];
-        else if constexpr (PARAM == PARAM_MASTER) p[j] = x.master[i];
-        else p[j] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(x.param)[i] << 16);
+    for (int k = 0; k < kRounds; ++k) {
+        const int64_t i = start + k * kPerRound;
+        const int n = left[k] = x.size - i >= 8 ? 8 : x.size > i ? (int)(x.size - i) : 0;
+        rp[k].load(PARAM == PARAM_MASTER ? x.master : x.param, i, n);
+        rg[k].load(x.grad, i, n);
+        rm[k].load(x.m, i, n);
+        rv[k].load(x.v, i, n);
+        sm[k] = sv[k] = 0.0f;
         if constexpr (STATE8) {
-            m[j] = value_of(reinterpret_cast<const uint8_t*>(x.m)[i]) * x.m_scale[i / kBlock];
-            v[j] = value_of(reinterpret_cast<const uint8_t*>(x.v)[i]) * x.v_scale[i / kBlock];
-            v[j] = v[j] * v[j];
-        } else {
-            m[j] = reinterpret_cast<const float*>(x.m)[i];
-            v[j] = reinterpret_cast<const float*>(x.v)[i];
-        }
-    }
-    float root[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        g[j] = g[j] * c.grad_scale;
-        m[j] = c.beta1 * m[j] + c.rest1 * g[j];
-        v[j] = c.beta2 * v[j] + c.rest2 * (g[j] * g[j]);
-        root[j] = __builtin_sqrtf(v[j]);
-        p[j] = p[j] * c.decay - c.rate * (m[j] / (root[j] * c.root + c.eps));
-    }
-    if constexpr (PARAM == PARAM_BF16) {
-        const uint4 u = dropout_bits(d, kind0, group);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t bits = __float_as_uint(p[j]), r = bits + ((w[j >> 1] >> (16 * (j & 1))) & 0xFFFFu);
-            if (j < n) reinterpret_cast<uint16_t*>(x.param)[i0 + j] = p[j] != p[j] ? 0x7FC0 : (uint16_t)(r >> 16);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (j >= n) continue;
-            if constexpr (PARAM == PARAM_F32) reinterpret_cast<float*>(x.param)[i0 + j] = p[j];
-            else {
-                x.master[i0 + j] = p[j];
-                Eight<uint16_t>::store_one(reinterpret_cast<uint16_t*>(x.param) + i0 + j, p[j]);
+            if (n) {
+                sm[k] = x.m_scale[i / kBlock];
+                sv[k] = x.v_scale[i / kBlock];
             }
         }
     }
-    if constexpr (!STATE8) {
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+        const int64_t i = start + k * kPerRound;
+        const int n = left[k];
+        const uint32_t group = (uint32_t)(i >> 3);
+        float p[8], g[8], m[8], v[8], root[8];
+        rp[k].get(p);
+        rg[k].get(g);
+        rm[k].get(m);
+        rv[k].get(v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (j >= n) continue;
-            reinterpret_cast<float*>(x.m)[i0 + j] = m[j];
-            reinterpret_cast<float*>(x.v)[i0 + j] = v[j];
+            if constexpr (STATE8) {
+                m[j] = m[j] * sm[k];
+                v[j] = v[j] * sv[k];
+                v[j] = v[j] * v[j];
+            }
+            g[j] = g[j] * c.grad_scale;
+            m[j] = c.beta1 * m[j] + c.rest1 * g[j];
+            v[j] = c.beta2 * v[j] + c.rest2 * (g[j] * g[j]);
+            root[j] = __builtin_sqrtf(v[j]);
+            p[j] = p[j] * c.decay - c.rate * (m[j] / (root[j] * c.root + c.eps));
         }
-    } else {
-        // the largest of 32 lanes, as bit patterns: a NaN is above an infinity, and that above all numbers
-        uint32_t am = 0, av = 0;
+        if constexpr (PARAM == PARAM_BF16) {
+            const uint4 u = dropout_bits(d, kind0, group);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t bm = __float_as_uint(m[j]) & 0x7FFFFFFFu, bv = __float_as_uint(root[j]) & 0x7FFFFFFFu;
-            am = bm > am && j < n ? bm : am;
-            av = bv > av && j < n ? bv : av;
-        }
+            for (int h = 0; h < 4; ++h) {
+                uint32_t r[2];
 #pragma unroll
-        for (int l = 1; l < 32; l <<= 1) {
-            const uint32_t om = (uint32_t)__shfl_xor((int)am, l), ov = (uint32_t)__shfl_xor((int)av, l);
-            am = om > am ? om : am;
-            av = ov > av ? ov : av;
-        }
-        constexpr uint32_t kLeast = (127u - 110u) << 23;
-        am = am > kLeast ? am : kLeast;
-        av = av > kLeast ? av : kLeast;
-        const float fm = __uint_as_float(am), fv = __uint_as_float(av);
-        if (n && (threadIdx.x & 31) == 0) {
-            x.m_scale[i0 / kBlock] = fm / 448.0f;
-            x.v_scale[i0 / kBlock] = fv / 448.0f;
-        }
-        const float im = 448.0f / fm, iv = 448.0f / fv;
-        const uint4 um = dropout_bits(d, kind0 + 1, group), uv = dropout_bits(d, kind0 + 2, group);
-        const uint32_t wm[4] = {um.x, um.y, um.z, um.w}, wv[4] = {uv.x, uv.y, uv.z, uv.w};
+                for (int e = 0; e < 2; ++e) {
+                    const int j = 2 * h + e;
+                    r[e] = p[j] != p[j] ? 0x7FC00000u : __float_as_uint(p[j]) + half_of(u, j);
+                }
+                rp[k].w[h] = __builtin_amdgcn_perm(r[1], r[0], 0x07060302u);
+            }
+            rp[k].store(x.param, i, n);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (j >= n) continue;
-            const float qm = __builtin_fminf(__builtin_fabsf(m[j]) * im, 448.0f), qv = __builtin_fminf(root[j] * iv, 448.0f);
-            uint32_t cm = code_of<false>(qm, (wm[j >> 1] >> (16 * (j & 1))) & 0xFFFFu);
-            uint32_t cv = code_of<true>(qv, (wv[j >> 1] >> (16 * (j & 1))) & 0xFFFFu);
-            cm |= m[j] < 0.0f ? 0x80u : 0u;
-            if (cv == 0 && root[j] > 0.0f) cv = 1;
-            if (am >= 0x7F800000u) cm = 0x7F;
-            if (av >= 0x7F800000u) cv = 0x7F;
-            reinterpret_cast<uint8_t*>(x.m)[i0 + j] = (uint8_t)cm;
-            reinterpret_cast<uint8_t*>(x.v)[i0 + j] = (uint8_t)cv;
+            for (int j = 0; j < 8; ++j) rp[k].w[j] = __float_as_uint(p[j]);
+            rp[k].store(PARAM == PARAM_MASTER ? x.master : x.param, i, n);
+            if constexpr (PARAM == PARAM_MASTER) {
+                Run<2> r;
+#pragma unroll
+                for (int h = 0; h < 4; ++h) r.w[h] = pack_bf16x2(p[2 * h], p[2 * h + 1]);
+                r.store(x.param, i, n);
+            }
         }
+        if constexpr (!STATE8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                rm[k].w[j] = __float_as_uint(m[j]);
+                rv[k].w[j] = __float_as_uint(v[j]);
+            }
+        } else {
+            // the largest of 32 lanes, as bit patterns: a NaN is above an infinity, and that above all numbers.  (What lies behind the
+            // tensor's end is 0.)
+            uint32_t am = (127u - 110u) << 23, av = am;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t bm = __float_as_uint(m[j]) & 0x7FFFFFFFu, bv = __float_as_uint(root[j]) & 0x7FFFFFFFu;
+                am = bm > am ? bm : am;
+                av = bv > av ? bv : av;
+            }
+#pragma unroll
+            for (int l = 1; l < 32; l <<= 1) {
+                const uint32_t om = (uint32_t)__shfl_xor((int)am, l), ov = (uint32_t)__shfl_xor((int)av, l);
+                am = om > am ? om : am;
+                av = ov > av ? ov : av;
+            }
+            const float fm = __uint_as_float(am), fv = __uint_as_float(av);
+            if (n && (threadIdx.x & 31) == 0) {
+                x.m_scale[i / kBlock] = fm / 448.0f;
+                x.v_scale[i / kBlock] = fv / 448.0f;
+            }
+            const float im = 448.0f / fm, iv = 448.0f / fv;
+            const uint4 um = dropout_bits(d, kind0 + 1, group), uv = dropout_bits(d, kind0 + 2, group);
+            codes_of<false>(m, im, um, rm[k].w);
+            codes_of<true>(root, iv, uv, rv[k].w);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (am >= 0x7F800000u) rm[k].w[h] = 0x7F7F7F7Fu;
+                if (av >= 0x7F800000u) rv[k].w[h] = 0x7F7F7F7Fu;
+            }
+        }
+        rm[k].store(x.m, i, n);
+        rv[k].store(x.v, i, n);
     }
 }
 
