@@ -1,6 +1,8 @@
 // The gradient of the epilogue of a product (halo_activation_bwd): E_Z = E act'(Z), and the bias' gradient, its column sums.
 #pragma clang fp contract(off)
 
+#include <type_traits>
+
 #include "activation.h"
 #include "around.h"
 #include "eight.h"
@@ -8,40 +10,79 @@
 namespace halo {
 namespace {
 
-constexpr int kThreads = 256;
-
-template <typename E>
-__device__ __forceinline__ float widen(E x) {
-    if constexpr (sizeof(E) == 2) return __uint_as_float((uint32_t)x << 16);
-    else return x;
-}
-
-// One thread a column of one part of the rows.
-template <typename E, int ACT>
-__global__ void __launch_bounds__(kThreads) act_grad_kernel(ActGrad a, int64_t rows_per_part) {
-    const int64_t c = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (c >= a.cols) return;
+// A wavefront has 512 columns, eight a lane, or fewer of narrow matrices and then several rows at once; the four of a workgroup have the
+// same columns and take turns at the rows of its part.  Their sums meet in LDS and go to `part`, a row for each part.
+template <typename E, int ACT, int LANES>
+__global__ void __launch_bounds__(256) act_grad_kernel(ActGrad a, int64_t rows_per_part) {
+    constexpr int ROWS = 256 / LANES;        // at once
+    __shared__ float meet[ROWS][LANES * 8];
+    const int lane = threadIdx.x % LANES, at = threadIdx.x / LANES;
+    const int64_t c = ((int64_t)blockIdx.x * LANES + lane) * 8, left = a.cols - c;
     const int64_t r0 = blockIdx.y * rows_per_part, r1 = r0 + rows_per_part < a.rows ? r0 + rows_per_part : a.rows;
-    float sum = 0.0f;
-    for (int64_t r = r0; r < r1; ++r) {
-        const float e = widen(reinterpret_cast<const E*>(a.E)[r * a.ld_e + c]);
-        const float z = ACT == HALO_ACT_NONE ? 0.0f : widen(reinterpret_cast<const E*>(a.Z)[r * a.ld_z + c]);
-        const float d = activation_slope<ACT>(e, z);
-        if (a.EZ) Eight<E>::store_one(reinterpret_cast<E*>(a.EZ) + r * a.ld_ez + c, d);
-        sum += d;
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    auto rows = [&](auto whole) {
+#pragma unroll 4
+        for (int64_t r = r0 + at; r < r1; r += ROWS) {
+            Eight<E> e, z;
+            e.load(reinterpret_cast<const E*>(a.E) + r * a.ld_e + c, left > 4);
+            z = e;
+            if constexpr (ACT != HALO_ACT_NONE) z.load(reinterpret_cast<const E*>(a.Z) + r * a.ld_z + c, left > 4);
+            float d[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                d[j] = activation_slope<ACT>(e.get(j), z.get(j));
+                sum[j] += d[j];
+            }
+            if (!a.EZ) continue;
+            E* p = reinterpret_cast<E*>(a.EZ) + r * a.ld_ez + c;
+            if constexpr (decltype(whole)::value) {
+                Eight<E>::store(p, d);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 7; ++j)
+                    if (j < left) Eight<E>::store_one(p + j, d[j]);
+            }
+        }
+    };
+    if (left >= 8) rows(std::true_type());
+    else if (left > 0) rows(std::false_type());
+    if (!a.GB) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) meet[at][lane * 8 + j] = sum[j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < LANES * 8; i += 256) {
+        const int64_t col = (int64_t)blockIdx.x * LANES * 8 + i;
+        if (col >= a.cols) break;
+        float t = 0.0f;
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) t += meet[k][i];
+        a.part[blockIdx.y * a.cols + col] = t;
     }
-    if (a.GB) a.part[blockIdx.y * a.cols + c] = sum;
 }
 
-int64_t parts_of(int64_t rows) { return rows < 64 ? rows : 64; }
+// Parts of the rows: as many as make some two thousand workgroups, with at least two rows for each of their threads.
+int lanes_of(int64_t cols) { return cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64; }
+int64_t parts_of(int64_t rows, int64_t cols) {
+    const int lanes = lanes_of(cols);
+    const int64_t tiles = (cols + lanes * 8 - 1) / (lanes * 8), at_once = 2 * (256 / lanes);
+    const int64_t most = tiles < 2048 ? 2048 / tiles : 1, parts = (rows + at_once - 1) / at_once;
+    return parts < most ? parts : most;
+}
 
 template <typename E, int ACT>
 hipError_t launch_typed(const ActGrad& a, hipStream_t s) {
-    const int64_t most = parts_of(a.rows), per = most ? (a.rows + most - 1) / most : 1, parts = (a.rows + per - 1) / per;
-    if (parts)
-        hipLaunchKernelGGL((act_grad_kernel<E, ACT>), dim3((unsigned)((a.cols + kThreads - 1) / kThreads), (unsigned)parts), dim3(kThreads), 0,
-                           s, a, per);
-    if (a.GB) return launch_sum_parts(a.part, a.GB, nullptr, nullptr, parts, a.cols, s);
+    const int lanes = lanes_of(a.cols);
+    const int64_t most = parts_of(a.rows, a.cols), per = most ? (a.rows + most - 1) / most : 1, parts = (a.rows + per - 1) / per;
+    if (parts) {
+        const dim3 grid((unsigned)((a.cols + lanes * 8 - 1) / (lanes * 8)), (unsigned)parts);
+        if (lanes == 8) hipLaunchKernelGGL((act_grad_kernel<E, ACT, 8>), grid, dim3(256), 0, s, a, per);
+        else if (lanes == 16) hipLaunchKernelGGL((act_grad_kernel<E, ACT, 16>), grid, dim3(256), 0, s, a, per);
+        else if (lanes == 32) hipLaunchKernelGGL((act_grad_kernel<E, ACT, 32>), grid, dim3(256), 0, s, a, per);
+        else hipLaunchKernelGGL((act_grad_kernel<E, ACT, 64>), grid, dim3(256), 0, s, a, per);
+    }
+    if (a.GB) return launch_sum_parts(a.part, a.GB, nullptr, nullptr, parts, a.cols, a.cols, s);
     return hipGetLastError();
 }
 template <typename E>
@@ -55,43 +96,45 @@ hipError_t launch_act(const ActGrad& a, hipStream_t s) {
     }
 }
 
-// 64 columns a workgroup, 16 threads a column, each every 16th part; the sixteen sums meet in LDS.
+// 32 columns a workgroup, 32 threads a column, each every 32nd part; the sums meet in LDS.
 __global__ void __launch_bounds__(1024) sum_parts_kernel(const float* part, float* out, const float* part2, float* out2, int64_t parts,
-                                                         int64_t cols) {
-    __shared__ float s[16][64];
+                                                         int64_t cols, int64_t pitch) {
+    __shared__ float s[32][33];
     if (blockIdx.y) {
         part = part2;
         out = out2;
     }
-    const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-    const int at = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
+    const int at = threadIdx.x >> 5;
     float t = 0.0f;
     if (c < cols) {
-#pragma unroll 8
-        for (int64_t p = at; p < parts; p += 16) t += part[p * cols + c];
+#pragma unroll 4
+        for (int64_t p = at; p < parts; p += 32) t += part[p * pitch + c];
     }
-    s[at][threadIdx.x & 63] = t;
+    s[at][threadIdx.x & 31] = t;
     __syncthreads();
     if (at || c >= cols) return;
     t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += s[i][threadIdx.x];
+    for (int i = 0; i < 32; ++i) t += s[i][threadIdx.x];
     out[c] = t;
 }
 
 }  // namespace
 
-size_t act_grad_workspace_floats(int64_t rows, int64_t cols) { return (size_t)parts_of(rows) * (size_t)cols; }
+size_t act_grad_workspace_floats(int64_t rows, int64_t cols) { return (size_t)parts_of(rows, cols) * (size_t)cols; }
 
 hipError_t launch_act_grad(const ActGrad& a, hipStream_t s) { return a.f32 ? launch_act<float>(a, s) : launch_act<uint16_t>(a, s); }
 
-hipError_t launch_sum_parts(const float* part, float* out, const float* part2, float* out2, int64_t parts, int64_t cols, hipStream_t s) {
+hipError_t launch_sum_parts(const float* part, float* out, const float* part2, float* out2, int64_t parts, int64_t cols, int64_t pitch,
+                            hipStream_t s) {
     if (!out) {
         out = out2;
         part = part2;
         out2 = nullptr;
     }
-    hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)((cols + 63) / 64), out2 ? 2 : 1), dim3(1024), 0, s, part, out, part2, out2, parts, cols);
+    hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)((cols + 31) / 32), out2 ? 2 : 1), dim3(1024), 0, s, part, out, part2, out2, parts,
+                       cols, pitch);
     return hipGetLastError();
 }
 

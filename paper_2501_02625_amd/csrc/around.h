@@ -35,7 +35,7 @@ struct NormBwd {
     int rms, f32, weight_f32;
 };
 constexpr int64_t kMaxNormCols = 32768;
-size_t norm_bwd_workspace_floats(int64_t rows, int64_t cols);
+size_t norm_bwd_workspace_floats(int64_t rows, int64_t cols, int f32);
 hipError_t launch_norm_fwd(const NormFwd& a, hipStream_t s);
 hipError_t launch_norm_bwd(const NormBwd& a, hipStream_t s);
 
@@ -52,9 +52,10 @@ struct ActGrad {
 size_t act_grad_workspace_floats(int64_t rows, int64_t cols);
 hipError_t launch_act_grad(const ActGrad& a, hipStream_t s);
 
-// out[c] = the sum of part[p][c] over the parts p, in order; part [parts x cols], dense.  A second vector in the same launch: out2 (may be
-// null) from part2.
-hipError_t launch_sum_parts(const float* part, float* out, const float* part2, float* out2, int64_t parts, int64_t cols, hipStream_t s);
+// out[c] = the sum of part[p * pitch + c] over the parts p, always in the same order.  A second vector in the same launch: out2 from part2.
+// Either of the two may be null.
+hipError_t launch_sum_parts(const float* part, float* out, const float* part2, float* out2, int64_t parts, int64_t cols, int64_t pitch,
+                            hipStream_t s);
 
 // ---- AdamW ----
 struct AdamwTensor {

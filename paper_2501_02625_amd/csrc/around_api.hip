@@ -81,7 +81,7 @@ halo_status halo_activation_bwd(const void* E, int64_t ld_e, const void* Z, int6
 // ------------------------------------------------------------------------------------------------
 size_t halo_layer_norm_bwd_workspace_bytes(const halo_norm_desc* desc) {
     if (check_norm(desc) != HALO_OK || desc->rows == 0 || desc->cols == 0) return 0;
-    return norm_bwd_workspace_floats(desc->rows, desc->cols) * 4;
+    return norm_bwd_workspace_floats(desc->rows, desc->cols, desc->dt == HALO_F32 ? 1 : 0) * 4;
 }
 
 halo_status halo_layer_norm_fwd(const halo_norm_desc* desc, const void* X, int64_t ld_x, const void* weight, const void* bias, void* Y,
