@@ -437,8 +437,13 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBwd a, int64_t ro
     }
 }
 
-// Workgroups of a launch: enough for every compute unit to hold several at once; each goes through its rows.
+// Workgroups of a launch: enough for every compute unit to hold several at once; each goes through its rows.  The gradient's hold 1024
+// threads of a compute unit's, or 512 where a thread has four groups: every one more writes a part of the sums and has fewer rows to
+// have on their way.  EX, G_W and G_B in bf16, 256 / 512 / 768 workgroups: 8192 x 4096 (512 lanes) 53.8 us / 47.4 / 53.6, 2048 x 8192 with
+// 1024 lanes 27.1 / 36 / 42, 1024 x 14336 (512 lanes, four groups) 38.4 / 46.4 / 53.6, 8192 x 512 12.1 / 10.4 / 9.8.
 constexpr int64_t kMostFwd = 2048, kMostBwd = 512;
+template <int LANES, int GROUPS>
+constexpr int64_t most_bwd() { return LANES >= 1024 || GROUPS >= 4 ? kMostBwd / 2 : kMostBwd; }
 inline unsigned groups_of(int64_t rows, int teams, int64_t most) {
     const int64_t n = (rows + teams - 1) / teams;
     return (unsigned)(n < most ? n : most);
@@ -467,7 +472,7 @@ hipError_t fwd_by_shape(const NormFwd& a, hipStream_t s) {
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
 hipError_t bwd(const NormBwd& a, hipStream_t s) {
     const bool sums = a.GW || a.GB;
-    const unsigned groups = groups_of(a.rows, TEAMS, kMostBwd);
+    const unsigned groups = groups_of(a.rows, TEAMS, most_bwd<LANES, GROUPS>());
     if (groups && sums) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, true>), dim3(groups), dim3(LANES * TEAMS), 0, s, a);
     else if (groups) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, false>), dim3(groups), dim3(LANES * TEAMS), 0, s, a);
     if (sums) return launch_sum_parts(a.part, a.GW, a.part + groups * ((a.cols + 3) / 4 * 4), a.GB, groups, a.cols, (a.cols + 3) / 4 * 4, s);
@@ -500,9 +505,9 @@ hipError_t bwd_by_shape(const NormBwd& a, hipStream_t s) {
     if (c <= 256) return bwd<E, W32, 32, 1, 8>(a, s);
     if (c <= 512) return bwd<E, W32, 64, 1, 4>(a, s);
     if (c <= 1024) return bwd<E, W32, 64, 2, 4>(a, s);
-    if (c <= 2048) return bwd<E, W32, 256, 1, 2>(a, s);
-    if (c <= 4096) return bwd<E, W32, 256, 2, 2>(a, s);
-    if (c <= 8192) return bwd<E, W32, 512, 2, 1>(a, s);
+    if (c <= 2048) return bwd<E, W32, 256, 1, 1>(a, s);
+    if (c <= 4096) return bwd<E, W32, 512, 1, 1>(a, s);
+    if (c <= 8192) return bwd<E, W32, 1024, 1, 1>(a, s);
     if constexpr (!apart(16384, sizeof(E) == 4)) {
         if (c <= 16384) return bwd<E, W32, 512, 4, 1>(a, s);
     }
