@@ -424,7 +424,7 @@ halo_status halo_adapters_bwd(const halo_adapters_desc* desc, const void* E, int
  *
  * halo_gemm_i8_epilogue: halo_gemm_i8_desc (K-contiguous B) with more in its epilogue, all in fp32:
  *
- *   z[i,j] = (float(acc[i,j]) * row_scale[i]) * col_scale[j] + bias[j]
+ *   z[i,j] = (float(acc[i,j]) * row_scale[i]) * col_scale[j] + bias[j]      (the last product and the sum in one rounding)
  *   Z[i,j] = z[i,j] rounded to c_dt;        C[i,j] = act(z[i,j]) + residual[i,j] rounded to c_dt
  *
  *   act       none: x; relu: max(x, 0); gelu: x Phi(x), Phi the normal distribution function; gelu_tanh: x / (1 + exp(-2 u)) with

@@ -1,5 +1,5 @@
 // The INT8 GEMM with bias, activation and residual in its epilogue (halo_gemm_i8_epilogue):  z = (float(acc) * row_scale) * col_scale +
-// bias,  C = act(z) + residual, and z itself where it is wanted for the backward pass.  Main loop and tiles: gemm_i8_device.h.
+// bias (rounded once with the product),  C = act(z) + residual, and z itself where it is wanted for the backward pass.  Main loop and tiles: gemm_i8_device.h.
 #pragma clang fp contract(off)
 
 #include "activation.h"
@@ -25,10 +25,12 @@ struct Piece {
         }
         return q;
     }
-    // n of the values (n > 0); p: the first one's address
+    // n of the values (n > 0); p: the first one's address.  PAST: past the caches, for whole lines of large matrices.
+    template <bool PAST>
     __device__ __forceinline__ static void store(void* p, const v4u& q, int n) {
         if (n >= W) {
-            __builtin_nontemporal_store(q, reinterpret_cast<v4u*>(p));
+            if constexpr (PAST) __builtin_nontemporal_store(q, reinterpret_cast<v4u*>(p));
+            else *reinterpret_cast<v4u*>(p) = q;
             return;
         }
 #pragma unroll
@@ -61,90 +63,108 @@ __device__ __forceinline__ void with_activation(int act, const F& f) {
 
 // The accumulators of a wavefront go through LDS, four rows of 16 x 16 tiles at a time, so that a lane has 16 bytes of C, Z and residual
 // that lie together, always of the same columns, and the code that computes them is a loop (over the accumulators, which are named
-// registers, it would be as long as the tile).  The LDS belongs to the wavefront: no barrier but the first.
-template <class Cfg, bool F32, int ACT>
-__device__ __forceinline__ void finish_tile(const GemmArgs& a, const EpilogueArgs& e, int64_t m0, int64_t n0, int wave, int lane,
-                                            unsigned char* smem) {
+// registers, it would be as long as the tile).  The LDS belongs to the wavefront: no barrier but the first.  One wavefront per SIMD has
+// nothing to hide a load behind but its own work: scales and bias are requested in front of the main loop, residuals a group of
+// steps ahead.
+template <class Cfg, bool F32>
+struct Finish {
     using P = Piece<F32>;
-    constexpr int TM = Cfg::TM, TN = Cfg::TN, WN = Cfg::WN, W = P::W, LANES = WN / W, ROWS = 64 / LANES;      // lanes a row, rows a step
-    constexpr int PITCH = WN + 4, STEPS = 64 / ROWS, AHEAD = 4;
+    static constexpr int TM = Cfg::TM, TN = Cfg::TN, WN = Cfg::WN, W = P::W, LANES = WN / W, ROWS = 64 / LANES;      // lanes a row, rows a step
+    static constexpr int PITCH = WN + 4, PARTS = TM / 4, STEPS = 64 / ROWS, AHEAD = 4;
     static_assert(TM % 4 == 0 && STEPS % AHEAD == 0 && 4 * 64 * PITCH * 4 <= Cfg::LDS_BYTES, "what a wavefront holds in LDS");
-    const int wave_m = wave >> 1, wave_n = wave & 1;
-    int32_t* mine = reinterpret_cast<int32_t*>(smem) + wave * (64 * PITCH);
-    const int at_row = lane / LANES, at_col = lane % LANES * W;
-    const int64_t col = n0 + wave_n * WN + at_col;
-    const int n = a.N - col < W ? (int)(a.N - col) : W;          // columns of this lane inside the matrix; may be negative
-    float cs[W], bias[W];
+    float rs[TM], cs[W], bias[W];
+    int64_t row0, col;                       // of the wavefront's rows, the lane's columns
+    int at_row, at_col, n;                   // n: columns of the lane inside the matrix; may be negative
+
+    __device__ __forceinline__ Finish(const GemmArgs& a, const EpilogueArgs& e, int64_t m0, int64_t n0, int wave, int lane) {
+        at_row = lane / LANES;
+        at_col = lane % LANES * W;
+        row0 = m0 + (wave >> 1) * Cfg::WM;
+        col = n0 + (wave & 1) * WN + at_col;
+        n = a.N - col < W ? (int)(a.N - col) : W;
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-        const int64_t c = col + j < a.N ? col + j : a.N - 1;
-        cs[j] = a.col_scale ? a.col_scale[c] : 1.0f;
-        bias[j] = bias_at(e, c);
-    }
-    __syncthreads();                                             // every wavefront has read its last operands
-#pragma unroll 1
-    for (int part = 0; part < TM / 4; ++part) {
-        auto dump = [&](auto first) {
-            StaticFor<0, 4>::run([&](auto ii) {
-                __builtin_amdgcn_sched_barrier(0);
-                hold_accumulators<TM * TN>();
-                StaticFor<0, TN>::run([&](auto jj) {
-                    constexpr int i = decltype(ii)::value, j = decltype(jj)::value, t = (decltype(first)::value + i) * TN + j;
-                    *reinterpret_cast<v4i*>(mine + (16 * i + row_of_lane(lane & 15)) * PITCH + 16 * j + 4 * (lane >> 4)) = read_acc<t>();
-                });
-            });
-            __builtin_amdgcn_sched_barrier(0);
-            hold_accumulators<TM * TN>();
-        };
-        if constexpr (TM > 4) {
-            if (part) dump(Int<4>());
-            else dump(Int<0>());
-        } else {
-            dump(Int<0>());
+        for (int i = 0; i < TM; ++i) {
+            const int64_t row = row0 + 16 * i + row_of_lane(lane & 15);
+            rs[i] = a.row_scale ? a.row_scale[row < a.M ? row : a.M - 1] : 1.0f;
         }
-        const int64_t row0 = m0 + wave_m * Cfg::WM + 64 * part + at_row;
-        v4u res[AHEAD], next_res[AHEAD];
-        float rs[AHEAD], next_rs[AHEAD];
-        auto request = [&](int step) {                           // every address lies inside its matrix
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const int64_t c = col + j < a.N ? col + j : a.N - 1;
+            cs[j] = a.col_scale ? a.col_scale[c] : 1.0f;
+            bias[j] = bias_at(e, c);
+        }
+    }
+
+    template <int ACT>
+    __device__ __forceinline__ void run(const GemmArgs& a, const EpilogueArgs& e, int wave, int lane, unsigned char* smem) const {
+        float* mine = reinterpret_cast<float*>(smem) + wave * (64 * PITCH);
+        v4u res[AHEAD], next[AHEAD];
+        auto request = [&](int step) {                           // counted over all parts; every address lies inside its matrix
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k) {
-                const int64_t row = row0 + (step + k) * ROWS, r = row < a.M ? row : a.M - 1;
-                next_rs[k] = a.row_scale ? a.row_scale[r] : 1.0f;
-                next_res[k] = (v4u){0u, 0u, 0u, 0u};
-                if (e.residual && n > 0) next_res[k] = *reinterpret_cast<const v4u*>(address<F32>(e.residual, e.ld_res, r, col));
+                const int64_t row = row0 + (step + k) * ROWS + at_row, r = row < a.M ? row : a.M - 1;
+                next[k] = (v4u){0u, 0u, 0u, 0u};
+                if (e.residual && n > 0) next[k] = *reinterpret_cast<const v4u*>(address<F32>(e.residual, e.ld_res, r, col));
             }
         };
         request(0);
+        __syncthreads();                                         // every wavefront has read its last operands
 #pragma unroll 1
-        for (int step = 0; step < STEPS; step += AHEAD) {
+        for (int part = 0; part < PARTS; ++part) {
+            auto dump = [&](auto first) {
+                StaticFor<0, 4>::run([&](auto ii) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    hold_accumulators<TM * TN>();
+                    StaticFor<0, TN>::run([&](auto jj) {
+                        constexpr int i = decltype(ii)::value, j = decltype(jj)::value, row = decltype(first)::value + i;
+                        const v4i x = read_acc<row * TN + j>();
+                        v4f v;
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                rs[k] = next_rs[k];
-                res[k] = next_res[k];
+                        for (int k = 0; k < 4; ++k) v[k] = (float)x[k] * rs[row];
+                        *reinterpret_cast<v4f*>(mine + (16 * i + row_of_lane(lane & 15)) * PITCH + 16 * j + 4 * (lane >> 4)) = v;
+                    });
+                });
+                __builtin_amdgcn_sched_barrier(0);
+                hold_accumulators<TM * TN>();
+            };
+            if constexpr (PARTS > 1) {
+                if (part) dump(Int<4>());
+                else dump(Int<0>());
+            } else {
+                dump(Int<0>());
             }
-            if (step + AHEAD < STEPS) request(step + AHEAD);
+#pragma unroll 1
+            for (int step = 0; step < STEPS; step += AHEAD) {
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int64_t row = row0 + (step + k) * ROWS;
-                const int32_t* from = mine + ((step + k) * ROWS + at_row) * PITCH + at_col;
-                v4i x[W / 4];
+                for (int k = 0; k < AHEAD; ++k) res[k] = next[k];
+                if (part * STEPS + step + AHEAD < PARTS * STEPS) request(part * STEPS + step + AHEAD);
 #pragma unroll
-                for (int q = 0; q < W / 4; ++q) x[q] = *reinterpret_cast<const v4i*>(from + 4 * q);
-                float z[W], y[W];
+                for (int k = 0; k < AHEAD; ++k) {
+                    const int64_t row = row0 + (part * STEPS + step + k) * ROWS + at_row;
+                    const float* from = mine + ((step + k) * ROWS + at_row) * PITCH + at_col;
+                    v4f x[W / 4];
 #pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    z[j] = ((float)x[j / 4][j % 4] * rs[k]) * cs[j] + bias[j];
-                    y[j] = activation<ACT>(z[j]) + P::get(res[k], j);
+                    for (int q = 0; q < W / 4; ++q) x[q] = *reinterpret_cast<const v4f*>(from + 4 * q);
+                    float z[W], y[W];
+#pragma unroll
+                    for (int j = 0; j < W; ++j) {
+                        z[j] = __builtin_fmaf(x[j / 4][j % 4], cs[j], bias[j]);
+                        y[j] = activation<ACT>(z[j]);
+                    }
+                    if (e.residual) {
+#pragma unroll
+                        for (int j = 0; j < W; ++j) y[j] += P::get(res[k], j);
+                    }
+                    if (row >= a.M || n <= 0) continue;
+                    if (e.Z) P::template store<true>(address<F32>(e.Z, e.ld_z, row, col), P::put(z), n);
+                    P::template store<true>(address<F32>(a.C, a.ldc, row, col), P::put(y), n);
                 }
-                if (row >= a.M || n <= 0) continue;
-                if (e.Z) P::store(address<F32>(e.Z, e.ld_z, row, col), P::put(z), n);
-                P::store(address<F32>(a.C, a.ldc, row, col), P::put(y), n);
             }
         }
     }
-}
+};
 
-template <int TM, int TN>
+template <int TM, int TN, bool F32>
 __global__ void __launch_bounds__(256, 1) __attribute__((aligned(8192)))
 gemm_i8_epilogue_kernel(GemmArgs a, EpilogueArgs e, int tiles_m, int tiles_n) {
     using Cfg = GemmCfg<TM, TN, true>;
@@ -155,47 +175,94 @@ gemm_i8_epilogue_kernel(GemmArgs a, EpilogueArgs e, int tiles_m, int tiles_n) {
     tile_of_block<Cfg::GROUP_M>(blockIdx.x, tiles_m, tiles_n, tile_m, tile_n);
     // the divisions run in vector registers; what follows from them belongs in scalar ones
     const int64_t m0 = (int64_t)__builtin_amdgcn_readfirstlane(tile_m) * Cfg::BM, n0 = (int64_t)__builtin_amdgcn_readfirstlane(tile_n) * Cfg::BN;
+    const Finish<Cfg, F32> finish(a, e, m0, n0, wave, lane);
     main_loop<Cfg, true, false>(a, m0, n0, wave, lane, smem);
-    with_activation(e.act, [&](auto act) {
-        constexpr int ACT = decltype(act)::value;
-        if (a.c_is_f32) finish_tile<Cfg, true, ACT>(a, e, m0, n0, wave, lane, smem);
-        else finish_tile<Cfg, false, ACT>(a, e, m0, n0, wave, lane, smem);
-    });
+    with_activation(e.act, [&](auto act) { finish.template run<decltype(act)::value>(a, e, wave, lane, smem); });
 }
 
+template <bool F32>
+__device__ __forceinline__ float load_one(const char* p) {
+    if constexpr (F32) return *reinterpret_cast<const float*>(p);
+    else return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+}
+template <bool F32>
+__device__ __forceinline__ void store_one(char* p, float x) {
+    if constexpr (F32) *reinterpret_cast<float*>(p) = x;
+    else *reinterpret_cast<uint16_t*>(p) = bf16_bits(x);
+}
 // One value: z to Z, act(z) + residual to C.
 template <bool F32>
 __device__ __forceinline__ void finish_one(const GemmArgs& a, const EpilogueArgs& e, int64_t row, int64_t col, float z) {
-    auto load = [](const char* p) {
-        return F32 ? *reinterpret_cast<const float*>(p) : __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
-    };
-    auto store = [](char* p, float x) {
-        if constexpr (F32) *reinterpret_cast<float*>(p) = x;
-        else *reinterpret_cast<uint16_t*>(p) = bf16_bits(x);
-    };
     float y = 0.0f;
     with_activation(e.act, [&](auto act) { y = activation<decltype(act)::value>(z); });
-    if (e.residual) y += load(address<F32>(e.residual, e.ld_res, row, col));
-    if (e.Z) store(address<F32>(e.Z, e.ld_z, row, col), z);
-    store(address<F32>(a.C, a.ldc, row, col), y);
+    if (e.residual) y += load_one<F32>(address<F32>(e.residual, e.ld_res, row, col));
+    if (e.Z) store_one<F32>(address<F32>(e.Z, e.ld_z, row, col), z);
+    store_one<F32>(address<F32>(a.C, a.ldc, row, col), y);
 }
 
-template <int TM, int TN>
+// What a thread of the small kernel needs beside its sums is requested before them, and arrives while they are formed.
+template <int TM, int TN, bool F32>
 __global__ void __launch_bounds__(256) gemm_i8_epilogue_small_kernel(GemmArgs a, EpilogueArgs e, int tiles_n) {
-    using Sums = SmallSums<SmallCfg<TM, TN, true>>;
+    using Cfg = SmallCfg<TM, TN, true>;
+    using Sums = SmallSums<Cfg>;
+    using P = Piece<F32>;
+    constexpr int EPT = Sums::EPT, PIECES = EPT / P::W;          // 16 bytes at a time, where there are as many
     extern __shared__ __align__(16) unsigned char smem[];
+    const int64_t row = (int64_t)(blockIdx.x / tiles_n) * Cfg::BM + threadIdx.x / Sums::TPR;
+    const int64_t col = (int64_t)(blockIdx.x % tiles_n) * Cfg::BN + threadIdx.x % Sums::TPR * EPT;
+    const int n = row >= a.M || col >= a.N ? 0 : a.N - col < EPT ? (int)(a.N - col) : EPT;
+    float cs[EPT], bias[EPT], res[EPT], rs = 1.0f;
+    v4u pieces[PIECES > 0 ? PIECES : 1];
+#pragma unroll
+    for (int j = 0; j < EPT; ++j) {
+        const int64_t c = col + j < a.N ? col + j : a.N - 1;
+        cs[j] = a.col_scale ? a.col_scale[c] : 1.0f;
+        bias[j] = bias_at(e, c);
+        res[j] = 0.0f;
+    }
+    if (n > 0) {
+        if (a.row_scale) rs = a.row_scale[row];
+        if (e.residual) {
+            if constexpr (PIECES > 0) {
+#pragma unroll
+                for (int q = 0; q < PIECES; ++q)
+                    if (q * P::W < n) pieces[q] = *reinterpret_cast<const v4u*>(address<F32>(e.residual, e.ld_res, row, col + q * P::W));
+            } else {
+#pragma unroll
+                for (int j = 0; j < EPT; ++j)
+                    if (j < n) res[j] = load_one<F32>(address<F32>(e.residual, e.ld_res, row, col + j));
+            }
+        }
+    }
     Sums s;
     small_sums<TM, TN, true>(a, blockIdx.x, tiles_n, smem, s);
-    if (s.row >= a.M) return;
-    const float rs = a.row_scale ? a.row_scale[s.row] : 1.0f;
+    if (n <= 0) return;
+    if constexpr (PIECES > 0) {
+        if (e.residual) {
 #pragma unroll
-    for (int j = 0; j < Sums::EPT; ++j) {
-        const int64_t col = s.col + j;
-        if (col >= a.N) break;
-        const float z = ((float)s.v[j / Sums::VW][j % Sums::VW] * rs) * (a.col_scale ? a.col_scale[col] : 1.0f) + bias_at(e, col);
-        if (a.c_is_f32) finish_one<true>(a, e, s.row, col, z);
-        else finish_one<false>(a, e, s.row, col, z);
+            for (int j = 0; j < EPT; ++j) res[j] = P::get(pieces[j / P::W], j % P::W);
+        }
     }
+    float z[EPT], y[EPT];
+#pragma unroll
+    for (int j = 0; j < EPT; ++j) z[j] = __builtin_fmaf((float)s.v[j / Sums::VW][j % Sums::VW] * rs, cs[j], bias[j]);
+    with_activation(e.act, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < EPT; ++j) y[j] = activation<decltype(act)::value>(z[j]) + res[j];
+    });
+    auto store = [&](const void* base, int64_t ld, const float* v) {
+        if constexpr (PIECES > 0) {
+#pragma unroll
+            for (int q = 0; q < PIECES; ++q)
+                if (q * P::W < n) P::template store<false>(address<F32>(base, ld, row, col + q * P::W), P::put(v + q * P::W), n - q * P::W);
+        } else {
+#pragma unroll
+            for (int j = 0; j < EPT; ++j)
+                if (j < n) store_one<F32>(address<F32>(base, ld, row, col + j), v[j]);
+        }
+    };
+    if (e.Z) store(e.Z, e.ld_z, z);
+    store(a.C, a.ldc, y);
 }
 
 // One thread per output, for what the tiles do not take: K = 0, and row pitches so large that the rows of a tile do not fit one
@@ -205,7 +272,7 @@ __global__ void __launch_bounds__(256) gemm_i8_epilogue_plain_kernel(GemmArgs a,
         const int64_t row = at / a.N, col = at % a.N;
         int acc = 0;
         for (int64_t k = 0; k < a.K; ++k) acc += (int)a.A[row * a.lda + k] * (int)a.B[col * a.ldb + k];
-        const float z = ((float)acc * (a.row_scale ? a.row_scale[row] : 1.0f)) * (a.col_scale ? a.col_scale[col] : 1.0f) + bias_at(e, col);
+        const float z = __builtin_fmaf((float)acc * (a.row_scale ? a.row_scale[row] : 1.0f), a.col_scale ? a.col_scale[col] : 1.0f, bias_at(e, col));
         if (a.c_is_f32) finish_one<true>(a, e, row, col, z);
         else finish_one<false>(a, e, row, col, z);
     }
@@ -213,12 +280,12 @@ __global__ void __launch_bounds__(256) gemm_i8_epilogue_plain_kernel(GemmArgs a,
 
 inline int64_t tiles(int64_t n, int t) { return (n + t - 1) / t; }
 
-template <int TM, int TN>
+template <int TM, int TN, bool F32>
 hipError_t launch_tiled(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
     using Cfg = GemmCfg<TM, TN, true>;
     static std::once_flag once;
     static hipError_t attr_result = hipSuccess;
-    auto kern = gemm_i8_epilogue_kernel<TM, TN>;
+    auto kern = gemm_i8_epilogue_kernel<TM, TN, F32>;
     const hipError_t err = raise_lds_limit(kern, Cfg::LDS_BYTES, &once, &attr_result);
     if (err != hipSuccess) return err;
     const int tiles_m = (int)tiles(a.M, Cfg::BM), tiles_n = (int)tiles(a.N, Cfg::BN);
@@ -226,24 +293,37 @@ hipError_t launch_tiled(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s)
     return hipGetLastError();
 }
 
-template <int TM, int TN>
+template <int TM, int TN, bool F32>
 hipError_t launch_split(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
     using Cfg = SmallCfg<TM, TN, true>;
     static std::once_flag once;
     static hipError_t attr_result = hipSuccess;
-    auto kern = gemm_i8_epilogue_small_kernel<TM, TN>;
+    auto kern = gemm_i8_epilogue_small_kernel<TM, TN, F32>;
     const hipError_t err = raise_lds_limit(kern, Cfg::LDS_BYTES, &once, &attr_result);
     if (err != hipSuccess) return err;
     const int64_t blocks = tiles(a.M, Cfg::BM) * tiles(a.N, Cfg::BN);
     hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), Cfg::LDS_BYTES, s, a, e, (int)tiles(a.N, Cfg::BN));
     return hipGetLastError();
 }
-template <int TM>
+template <int TM, bool F32>
 hipError_t launch_split_by_columns(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
     const int columns = small_tile_columns(a);
-    if (columns == 16) return launch_split<TM, 1>(a, e, s);
-    if (columns == 32) return launch_split<TM, 2>(a, e, s);
-    return launch_split<TM, 4>(a, e, s);
+    if (columns == 16) return launch_split<TM, 1, F32>(a, e, s);
+    if (columns == 32) return launch_split<TM, 2, F32>(a, e, s);
+    return launch_split<TM, 4, F32>(a, e, s);
+}
+template <bool F32>
+hipError_t launch_by_shape(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
+    switch (a.config < 0 ? choose_config(a, nullptr) : a.config) {
+        case 0:
+        case 1: return launch_tiled<8, 8, F32>(a, e, s);
+        case 2: return launch_tiled<8, 4, F32>(a, e, s);
+        case 3:
+        case 4: return launch_tiled<4, 4, F32>(a, e, s);
+        case kSmall64: return launch_split<4, 4, F32>(a, e, s);
+        case kSmall32: return a.M <= 16 ? launch_split_by_columns<1, F32>(a, e, s) : launch_split_by_columns<2, F32>(a, e, s);
+        default: return hipErrorInvalidValue;
+    }
 }
 
 }  // namespace
@@ -256,16 +336,7 @@ hipError_t launch_gemm_i8_epilogue(const GemmArgs& a, const EpilogueArgs& e, hip
         hipLaunchKernelGGL(gemm_i8_epilogue_plain_kernel, dim3((unsigned)blocks), dim3(256), 0, s, a, e);
         return hipGetLastError();
     }
-    switch (a.config < 0 ? choose_config(a, nullptr) : a.config) {
-        case 0:
-        case 1: return launch_tiled<8, 8>(a, e, s);
-        case 2: return launch_tiled<8, 4>(a, e, s);
-        case 3:
-        case 4: return launch_tiled<4, 4>(a, e, s);
-        case kSmall64: return launch_split<4, 4>(a, e, s);
-        case kSmall32: return a.M <= 16 ? launch_split_by_columns<1>(a, e, s) : launch_split_by_columns<2>(a, e, s);
-        default: return hipErrorInvalidValue;
-    }
+    return a.c_is_f32 ? launch_by_shape<true>(a, e, s) : launch_by_shape<false>(a, e, s);
 }
 
 }  // namespace halo
