@@ -62,11 +62,12 @@ __global__ void __launch_bounds__(256) act_grad_kernel(ActGrad a, int64_t rows_p
     }
 }
 
-// Parts of the rows: as many as make some two thousand workgroups, with at least two rows for each of their threads.
+// Parts of the rows: as many as make some two thousand workgroups, with a row for each of their threads at least.  1031 x 1003 in fp32, at
+// least one / two / four rows: 5.3 us / 7.2 / 10.6 (and 4.2 for the sum over the parts, whichever).
 int lanes_of(int64_t cols) { return cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : 64; }
 int64_t parts_of(int64_t rows, int64_t cols) {
     const int lanes = lanes_of(cols);
-    const int64_t tiles = (cols + lanes * 8 - 1) / (lanes * 8), at_once = 2 * (256 / lanes);
+    const int64_t tiles = (cols + lanes * 8 - 1) / (lanes * 8), at_once = 256 / lanes;
     const int64_t most = tiles < 2048 ? 2048 / tiles : 1, parts = (rows + at_once - 1) / at_once;
     return parts < most ? parts : most;
 }

@@ -252,7 +252,8 @@ __global__ void __launch_bounds__(LANES* TEAMS) norm_bwd_kernel(NormBwd a) {
     using S = Shape<LANES, GROUPS, SUMS>;
     using Sum = TeamSum<LANES, TEAMS, 2>;
     __shared__ float s[2][2][TEAMS][Sum::WAVES];
-    __shared__ float meet[SUMS && TEAMS > 1 ? LANES * GROUPS * 8 : 1];
+    constexpr int WIDE = LANES * GROUPS * 8;
+    __shared__ __align__(16) float meet[SUMS && TEAMS > 1 ? 2 * TEAMS * WIDE : 1];
     Sum sum{s};
     const int team = TEAMS > 1 ? threadIdx.x / LANES : 0, lane = threadIdx.x % LANES;
     const int64_t stride = (int64_t)gridDim.x * TEAMS;
@@ -366,30 +367,32 @@ __global__ void __launch_bounds__(LANES* TEAMS) norm_bwd_kernel(NormBwd a) {
         }
     }
     if constexpr (SUMS) {
-        auto finish = [&](float (&v)[GROUPS][8], float* out) {
-            if constexpr (TEAMS > 1) {
-                for (int k = 0; k < TEAMS; ++k) {
-                    __syncthreads();
-                    if (team != k) continue;
-#pragma unroll
-                    for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            float* m = meet + (g * 8 + j) * LANES + lane;
-                            if (k) v[g][j] += *m;
-                            *m = v[g][j];
-                        }
-                }
-            }
-            if (team != TEAMS - 1) return;
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g)
-                if (g < S::FULL || left[g] > 0) store_part(out + S::column(g), v[g], left[g]);
-        };
         // rows of parts begin at multiples of four floats
         const int64_t pitch = (a.cols + 3) / 4 * 4;
-        if (a.GW) finish(gw, a.part + (int64_t)blockIdx.x * pitch);
-        if (a.GB) finish(gb, a.part + ((int64_t)gridDim.x + blockIdx.x) * pitch);
+        float *part_w = a.part + (int64_t)blockIdx.x * pitch, *part_b = a.part + ((int64_t)gridDim.x + blockIdx.x) * pitch;
+        if constexpr (TEAMS > 1) {
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                Eight<float>::store(meet + team * WIDE + S::column(g), gw[g]);
+                Eight<float>::store(meet + (TEAMS + team) * WIDE + S::column(g), gb[g]);
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < 2 * WIDE; i += LANES * TEAMS) {
+                const int which = i / WIDE, c = i % WIDE;
+                if (c >= a.cols || !(which ? a.GB : a.GW)) continue;
+                float v = 0.0f;
+#pragma unroll
+                for (int k = 0; k < TEAMS; ++k) v += meet[(which * TEAMS + k) * WIDE + c];
+                (which ? part_b : part_w)[c] = v;
+            }
+        } else {
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                if (g >= S::FULL && left[g] <= 0) continue;
+                if (a.GW) store_part(part_w + S::column(g), gw[g], left[g]);
+                if (a.GB) store_part(part_b + S::column(g), gb[g], left[g]);
+            }
+        }
     }
 }
 
@@ -504,7 +507,7 @@ hipError_t bwd_by_shape(const NormBwd& a, hipStream_t s) {
     if (c <= 128) return bwd<E, W32, 16, 1, 16>(a, s);
     if (c <= 256) return bwd<E, W32, 32, 1, 8>(a, s);
     if (c <= 512) return bwd<E, W32, 64, 1, 4>(a, s);
-    if (c <= 1024) return bwd<E, W32, 64, 2, 4>(a, s);
+    if (c <= 1024) return bwd<E, W32, 128, 1, 4>(a, s);
     if (c <= 2048) return bwd<E, W32, 256, 1, 1>(a, s);
     if (c <= 4096) return bwd<E, W32, 512, 1, 1>(a, s);
     if (c <= 8192) return bwd<E, W32, 1024, 1, 1>(a, s);
