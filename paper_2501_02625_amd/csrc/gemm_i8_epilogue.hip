@@ -70,7 +70,8 @@ template <class Cfg, bool F32>
 struct Finish {
     using P = Piece<F32>;
     static constexpr int TM = Cfg::TM, TN = Cfg::TN, WN = Cfg::WN, W = P::W, LANES = WN / W, ROWS = 64 / LANES;      // lanes a row, rows a step
-    static constexpr int PITCH = WN + 4, PARTS = TM / 4, STEPS = 64 / ROWS, AHEAD = 4;
+    static constexpr int PITCH = WN + 4, PARTS = TM / 4, STEPS = 64 / ROWS, AHEAD = 4, SIZE = F32 ? 4 : 2;
+    using Buffer = __amdgpu_buffer_rsrc_t;
     static_assert(TM % 4 == 0 && STEPS % AHEAD == 0 && 4 * 64 * PITCH * 4 <= Cfg::LDS_BYTES, "what a wavefront holds in LDS");
     float rs[TM], cs[W], bias[W];
     int64_t row0, col;                       // of the wavefront's rows, the lane's columns
@@ -95,19 +96,37 @@ struct Finish {
         }
     }
 
-    template <int ACT>
+    // A matrix of C's type from the wavefront's first row and column on, as a buffer that ends behind the matrix' last row: loads from rows
+    // behind it give zeros, stores to them nothing, and neither needs a branch.  (With branches around them the compiler cannot count
+    // what is on its way, and every residual waited for all stores in front of it.)
+    __device__ __forceinline__ Buffer buffer(const void* p, int64_t ld, const GemmArgs& a) const {
+        const int64_t rows = a.M - row0 < Cfg::WM ? a.M - row0 : Cfg::WM;
+        return __builtin_amdgcn_make_buffer_rsrc(address<F32>(p, ld, row0, col - at_col), 0, rows > 0 ? (int)(uint32_t)(rows * ld * SIZE) : 0, 0x00020000);
+    }
+
+    template <int ACT, bool RES>
     __device__ __forceinline__ void run(const GemmArgs& a, const EpilogueArgs& e, int wave, int lane, unsigned char* smem) const {
         float* mine = reinterpret_cast<float*>(smem) + wave * (64 * PITCH);
+        constexpr int PAST = 2;                                  // past the caches
+        const bool partly = n > 0 && n < W, ragged = a.N % W != 0;
+        const Buffer to_c = buffer(a.C, a.ldc, a), to_z = buffer(e.Z, e.ld_z, a), from_r = buffer(e.residual, e.ld_res, a);
+        const uint32_t up_c = (uint32_t)(ROWS * a.ldc * SIZE), up_z = (uint32_t)(ROWS * e.ld_z * SIZE), up_r = (uint32_t)(ROWS * e.ld_res * SIZE);
+        // where the lane's 16 bytes of the next row are; those of columns outside the matrix are outside the buffers
+        uint32_t at_c = n > 0 ? (uint32_t)((at_row * a.ldc + at_col) * SIZE) : kOutside;
+        uint32_t at_z = n > 0 ? (uint32_t)((at_row * e.ld_z + at_col) * SIZE) : kOutside;
+        uint32_t at_r = n > 0 ? (uint32_t)((at_row * e.ld_res + at_col) * SIZE) : kOutside;
+        const uint32_t more_c = n > 0 ? up_c : 0, more_z = n > 0 ? up_z : 0, more_r = n > 0 ? up_r : 0;
         v4u res[AHEAD], next[AHEAD];
-        auto request = [&](int step) {                           // counted over all parts; every address lies inside its matrix
+        auto request = [&]() {
+            if constexpr (RES) {
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int64_t row = row0 + (step + k) * ROWS + at_row, r = row < a.M ? row : a.M - 1;
-                next[k] = (v4u){0u, 0u, 0u, 0u};
-                if (e.residual && n > 0) next[k] = *reinterpret_cast<const v4u*>(address<F32>(e.residual, e.ld_res, r, col));
+                for (int k = 0; k < AHEAD; ++k) {
+                    next[k] = __builtin_amdgcn_raw_buffer_load_b128(from_r, (int)at_r, 0, 0);
+                    at_r += more_r;
+                }
             }
         };
-        request(0);
+        request();
         __syncthreads();                                         // every wavefront has read its last operands
 #pragma unroll 1
         for (int part = 0; part < PARTS; ++part) {
@@ -137,10 +156,9 @@ struct Finish {
             for (int step = 0; step < STEPS; step += AHEAD) {
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) res[k] = next[k];
-                if (part * STEPS + step + AHEAD < PARTS * STEPS) request(part * STEPS + step + AHEAD);
+                request();                                       // behind the last rows: outside the buffer, or rows that nobody uses
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) {
-                    const int64_t row = row0 + (part * STEPS + step + k) * ROWS + at_row;
                     const float* from = mine + ((step + k) * ROWS + at_row) * PITCH + at_col;
                     v4f x[W / 4];
 #pragma unroll
@@ -149,15 +167,20 @@ struct Finish {
 #pragma unroll
                     for (int j = 0; j < W; ++j) {
                         z[j] = __builtin_fmaf(x[j / 4][j % 4], cs[j], bias[j]);
-                        y[j] = activation<ACT>(z[j]);
+                        y[j] = activation<ACT, !F32>(z[j]);
+                        if constexpr (RES) y[j] += P::get(res[k], j);
                     }
-                    if (e.residual) {
-#pragma unroll
-                        for (int j = 0; j < W; ++j) y[j] += P::get(res[k], j);
+                    if (e.Z) __builtin_amdgcn_raw_buffer_store_b128(P::put(z), to_z, (int)(partly ? kOutside : at_z), 0, PAST);
+                    __builtin_amdgcn_raw_buffer_store_b128(P::put(y), to_c, (int)(partly ? kOutside : at_c), 0, PAST);
+                    if (ragged) {                                // uniform: some tile's columns end inside a lane's 16 bytes
+                        const int64_t row = row0 + (part * STEPS + step + k) * ROWS + at_row;
+                        if (partly && row < a.M) {
+                            if (e.Z) P::template store<false>(address<F32>(e.Z, e.ld_z, row, col), P::put(z), n);
+                            P::template store<false>(address<F32>(a.C, a.ldc, row, col), P::put(y), n);
+                        }
                     }
-                    if (row >= a.M || n <= 0) continue;
-                    if (e.Z) P::template store<true>(address<F32>(e.Z, e.ld_z, row, col), P::put(z), n);
-                    P::template store<true>(address<F32>(a.C, a.ldc, row, col), P::put(y), n);
+                    at_c += more_c;
+                    at_z += more_z;
                 }
             }
         }
@@ -177,7 +200,10 @@ gemm_i8_epilogue_kernel(GemmArgs a, EpilogueArgs e, int tiles_m, int tiles_n) {
     const int64_t m0 = (int64_t)__builtin_amdgcn_readfirstlane(tile_m) * Cfg::BM, n0 = (int64_t)__builtin_amdgcn_readfirstlane(tile_n) * Cfg::BN;
     const Finish<Cfg, F32> finish(a, e, m0, n0, wave, lane);
     main_loop<Cfg, true, false>(a, m0, n0, wave, lane, smem);
-    with_activation(e.act, [&](auto act) { finish.template run<decltype(act)::value>(a, e, wave, lane, smem); });
+    with_activation(e.act, [&](auto act) {
+        if (e.residual) finish.template run<decltype(act)::value, true>(a, e, wave, lane, smem);
+        else finish.template run<decltype(act)::value, false>(a, e, wave, lane, smem);
+    });
 }
 
 template <bool F32>
@@ -194,7 +220,7 @@ __device__ __forceinline__ void store_one(char* p, float x) {
 template <bool F32>
 __device__ __forceinline__ void finish_one(const GemmArgs& a, const EpilogueArgs& e, int64_t row, int64_t col, float z) {
     float y = 0.0f;
-    with_activation(e.act, [&](auto act) { y = activation<decltype(act)::value>(z); });
+    with_activation(e.act, [&](auto act) { y = activation<decltype(act)::value, !F32>(z); });
     if (e.residual) y += load_one<F32>(address<F32>(e.residual, e.ld_res, row, col));
     if (e.Z) store_one<F32>(address<F32>(e.Z, e.ld_z, row, col), z);
     store_one<F32>(address<F32>(a.C, a.ldc, row, col), y);
@@ -248,7 +274,7 @@ __global__ void __launch_bounds__(256) gemm_i8_epilogue_small_kernel(GemmArgs a,
     for (int j = 0; j < EPT; ++j) z[j] = __builtin_fmaf((float)s.v[j / Sums::VW][j % Sums::VW] * rs, cs[j], bias[j]);
     with_activation(e.act, [&](auto act) {
 #pragma unroll
-        for (int j = 0; j < EPT; ++j) y[j] = activation<decltype(act)::value>(z[j]) + res[j];
+        for (int j = 0; j < EPT; ++j) y[j] = activation<decltype(act)::value, !F32>(z[j]) + res[j];
     });
     auto store = [&](const void* base, int64_t ld, const float* v) {
         if constexpr (PIECES > 0) {
@@ -266,7 +292,7 @@ __global__ void __launch_bounds__(256) gemm_i8_epilogue_small_kernel(GemmArgs a,
 }
 
 // One thread per output, for what the tiles do not take: K = 0, and row pitches so large that the rows of a tile do not fit one
-// buffer's 4 GiB.
+// buffer.
 __global__ void __launch_bounds__(256) gemm_i8_epilogue_plain_kernel(GemmArgs a, EpilogueArgs e) {
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < a.M * a.N; at += (int64_t)gridDim.x * 256) {
         const int64_t row = at / a.N, col = at % a.N;
@@ -331,7 +357,9 @@ hipError_t launch_by_shape(const GemmArgs& a, const EpilogueArgs& e, hipStream_t
 hipError_t launch_gemm_i8_epilogue(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
     if (a.M == 0 || a.N == 0) return hipSuccess;
     if (!a.transB || !a.C || a.acc_out || a.left_stages || a.lr_rank) return hipErrorInvalidValue;
-    if (!tiles_can_run(a)) {
+    // offsets from a wavefront's first row are 32-bit numbers
+    const int64_t most = int64_t(1) << 22;
+    if (!tiles_can_run(a) || a.ldc > most || (e.residual && e.ld_res > most) || (e.Z && e.ld_z > most)) {
         const int64_t blocks = std::min(tiles(a.M * a.N, 256), int64_t(1) << 20);
         hipLaunchKernelGGL(gemm_i8_epilogue_plain_kernel, dim3((unsigned)blocks), dim3(256), 0, s, a, e);
         return hipGetLastError();

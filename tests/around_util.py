@@ -61,9 +61,11 @@ def within(got, want, bound, what):
                              % (what, bad.sum(), bad.size, i, g[i], want[i], np.broadcast_to(bound, g.shape)[i]))
 
 
-def act_bound(z, y, name):
+def act_bound(z, y, name, dtype=torch.float32):
     """How far act(z) may be from its value y: the exponential's argument is off by a few roundings, which counts where it is large and
-    negative; the reciprocal, the exponential and the products by one rounding each (1.5 for the polynomial of gelu)."""
+    negative; the reciprocal, the exponential and the products by one rounding each (1.5 for the polynomial of gelu).  For bf16 results
+    gelu's polynomial is a shorter one, 3.2e-5 of the tail Phi(-|z|) off at most: z times the tail is all of y for z < 0, and at most y for
+    z > 0, where y = z (1 - tail) and tail <= 1/2."""
     z, y = np.asarray(z), np.abs(y)
     below = z < 0
     if name in ("none", "relu"):
@@ -71,7 +73,7 @@ def act_bound(z, y, name):
     if name == "silu":
         return (np.abs(z) * below + 10) * U * y + 1e-30
     if name == "gelu":
-        return (z * z * below + 20) * U * y + 1e-30
+        return ((z * z * below + 20) * U + (3.2e-5 if dtype == torch.bfloat16 else 0.0)) * y + 1e-30
     return (5 * np.abs(1.6 * (z + 0.044715 * z ** 3)) * below + 14) * U * y + 1e-30
 
 

@@ -81,7 +81,7 @@ def test_forward_and_backward_are_those_of_the_parts():
     for s, bias, act, res, got, z in ((k.s1, b1, "gelu", None, k.a, k.z), (k.s2, b2, "none", k.x, y, None)):
         want, wz = orc.product(*codes(s), host(bias), act, None if res is None else host(res))
         off = 6 * U * (np.abs(wz) + np.abs(wz - host(bias)))
-        within(got, want, 1.2 * off + act_bound(wz, want, act) + U * np.abs(want) + HALF[BF] * (np.abs(want) + 1e-6), act)
+        within(got, want, 1.2 * off + act_bound(wz, want, act, BF) + U * np.abs(want) + HALF[BF] * (np.abs(want) + 1e-6), act)
         if z is not None:
             within(z, wz, off + HALF[BF] * (np.abs(wz) + 1e-6), "Z")
     e = ((y - k.target) * 0.01).to(BF)

@@ -30,7 +30,7 @@ def check(A, B, rs, cs, bias, act, res, C, Z, dtype, what):
         within(Z, z, off_z + HALF[dtype] * np.abs(z) * (1 + 1e-6), what + " Z")
     a = orc.act(z, act)
     # act's slope is at most 1.13
-    bound = 1.2 * off_z + act_bound(z, a, act) + U * np.abs(y) + HALF[dtype] * (np.abs(y) + 1e-6)
+    bound = 1.2 * off_z + act_bound(z, a, act, dtype) + U * np.abs(y) + HALF[dtype] * (np.abs(y) + 1e-6)
     within(C, y, bound, what + " C")
 
 
