@@ -69,20 +69,23 @@ __device__ __forceinline__ void with_activation(int act, const F& f) {
 template <class Cfg, bool F32>
 struct Finish {
     using P = Piece<F32>;
-    static constexpr int TM = Cfg::TM, TN = Cfg::TN, WN = Cfg::WN, W = P::W, LANES = WN / W, ROWS = 64 / LANES;      // lanes a row, rows a step
+    static constexpr int TM = Cfg::TM, TN = Cfg::TN, WN = Cfg::WN, W = P::W;
+    static constexpr int LANES = (WN > 64 ? 128 : 64) / W, ROWS = 64 / LANES;             // lanes a row (of 96 columns, a quarter idle), rows a step
     static constexpr int PITCH = WN + 4, PARTS = TM / 4, STEPS = 64 / ROWS, AHEAD = 4, SIZE = F32 ? 4 : 2;
     using Buffer = __amdgpu_buffer_rsrc_t;
     static_assert(TM % 4 == 0 && STEPS % AHEAD == 0 && 4 * 64 * PITCH * 4 <= Cfg::LDS_BYTES, "what a wavefront holds in LDS");
     float rs[TM], cs[W], bias[W];
-    int64_t row0, col;                       // of the wavefront's rows, the lane's columns
+    int64_t row0, col, col0;                 // of the wavefront's rows, the lane's columns, the tile's
     int at_row, at_col, n;                   // n: columns of the lane inside the matrix; may be negative
 
     __device__ __forceinline__ Finish(const GemmArgs& a, const EpilogueArgs& e, int64_t m0, int64_t n0, int wave, int lane) {
         at_row = lane / LANES;
         at_col = lane % LANES * W;
         row0 = m0 + (wave >> 1) * Cfg::WM;
-        col = n0 + (wave & 1) * WN + at_col;
-        n = a.N - col < W ? (int)(a.N - col) : W;
+        col0 = n0;
+        col = n0 + (wave & 1) * 16 * Cfg::LOW_STEP + at_col;
+        if (TN % 4 != 0 && at_col >= 16 * Cfg::LOW_STEP) col = n0 + Cfg::high_column(wave & 1) + at_col - 16 * Cfg::LOW_STEP;
+        n = at_col >= WN ? 0 : a.N - col < W ? (int)(a.N - col) : W;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int64_t row = row0 + 16 * i + row_of_lane(lane & 15);
@@ -94,14 +97,15 @@ struct Finish {
             cs[j] = a.col_scale ? a.col_scale[c] : 1.0f;
             bias[j] = bias_at(e, c);
         }
+        if (at_col >= WN) at_col = 0;                            // an idle lane reads LDS where another does
     }
 
-    // A matrix of C's type from the wavefront's first row and column on, as a buffer that ends behind the matrix' last row: loads from rows
+    // A matrix of C's type from the wavefront's first row and the tile's first column on, as a buffer that ends behind the matrix' last row: loads from rows
     // behind it give zeros, stores to them nothing, and neither needs a branch.  (With branches around them the compiler cannot count
     // what is on its way, and every residual waited for all stores in front of it.)
     __device__ __forceinline__ Buffer buffer(const void* p, int64_t ld, const GemmArgs& a) const {
         const int64_t rows = a.M - row0 < Cfg::WM ? a.M - row0 : Cfg::WM;
-        return __builtin_amdgcn_make_buffer_rsrc(address<F32>(p, ld, row0, col - at_col), 0, rows > 0 ? (int)(uint32_t)(rows * ld * SIZE) : 0, 0x00020000);
+        return __builtin_amdgcn_make_buffer_rsrc(address<F32>(p, ld, row0, col0), 0, rows > 0 ? (int)(uint32_t)(rows * ld * SIZE) : 0, 0x00020000);
     }
 
     template <int ACT, bool RES>
@@ -112,9 +116,9 @@ struct Finish {
         const Buffer to_c = buffer(a.C, a.ldc, a), to_z = buffer(e.Z, e.ld_z, a), from_r = buffer(e.residual, e.ld_res, a);
         const uint32_t up_c = (uint32_t)(ROWS * a.ldc * SIZE), up_z = (uint32_t)(ROWS * e.ld_z * SIZE), up_r = (uint32_t)(ROWS * e.ld_res * SIZE);
         // where the lane's 16 bytes of the next row are; those of columns outside the matrix are outside the buffers
-        uint32_t at_c = n > 0 ? (uint32_t)((at_row * a.ldc + at_col) * SIZE) : kOutside;
-        uint32_t at_z = n > 0 ? (uint32_t)((at_row * e.ld_z + at_col) * SIZE) : kOutside;
-        uint32_t at_r = n > 0 ? (uint32_t)((at_row * e.ld_res + at_col) * SIZE) : kOutside;
+        uint32_t at_c = n > 0 ? (uint32_t)((at_row * a.ldc + col - col0) * SIZE) : kOutside;
+        uint32_t at_z = n > 0 ? (uint32_t)((at_row * e.ld_z + col - col0) * SIZE) : kOutside;
+        uint32_t at_r = n > 0 ? (uint32_t)((at_row * e.ld_res + col - col0) * SIZE) : kOutside;
         const uint32_t more_c = n > 0 ? up_c : 0, more_z = n > 0 ? up_z : 0, more_r = n > 0 ? up_r : 0;
         v4u res[AHEAD], next[AHEAD];
         auto request = [&]() {
@@ -187,15 +191,12 @@ struct Finish {
     }
 };
 
-template <int TM, int TN, bool F32>
-__global__ void __launch_bounds__(256, 1) __attribute__((aligned(8192)))
-gemm_i8_epilogue_kernel(GemmArgs a, EpilogueArgs e, int tiles_m, int tiles_n) {
-    using Cfg = GemmCfg<TM, TN, true>;
-    extern __shared__ __align__(16) unsigned char smem[];
+template <class Cfg, bool F32>
+__device__ __forceinline__ void one_tile(const GemmArgs& a, const EpilogueArgs& e, int bid, int tiles_m, int tiles_n, unsigned char* smem) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int tile_m, tile_n;
-    tile_of_block<Cfg::GROUP_M>(blockIdx.x, tiles_m, tiles_n, tile_m, tile_n);
+    tile_of_block<Cfg::GROUP_M>(bid, tiles_m, tiles_n, tile_m, tile_n);
     // the divisions run in vector registers; what follows from them belongs in scalar ones
     const int64_t m0 = (int64_t)__builtin_amdgcn_readfirstlane(tile_m) * Cfg::BM, n0 = (int64_t)__builtin_amdgcn_readfirstlane(tile_n) * Cfg::BN;
     const Finish<Cfg, F32> finish(a, e, m0, n0, wave, lane);
@@ -204,6 +205,22 @@ gemm_i8_epilogue_kernel(GemmArgs a, EpilogueArgs e, int tiles_m, int tiles_n) {
         if (e.residual) finish.template run<decltype(act)::value, true>(a, e, wave, lane, smem);
         else finish.template run<decltype(act)::value, false>(a, e, wave, lane, smem);
     });
+}
+
+template <int TM, int TN, bool F32>
+__global__ void __launch_bounds__(256, 1) __attribute__((aligned(8192)))
+gemm_i8_epilogue_kernel(GemmArgs a, EpilogueArgs e, int tiles_m, int tiles_n) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    one_tile<GemmCfg<TM, TN, true>, F32>(a, e, blockIdx.x, tiles_m, tiles_n, smem);
+}
+
+// The first columns in tiles of 256 x 256, the others (a2, e2) in 256 x 192: two_widths.
+template <bool F32>
+__global__ void __launch_bounds__(256, 1) __attribute__((aligned(8192)))
+two_widths_gemm_i8_epilogue_kernel(GemmArgs a, EpilogueArgs e, int tiles_n, GemmArgs a2, EpilogueArgs e2, int tiles_n2, int tiles_m, unsigned blocks1) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    if (blockIdx.x >= blocks1) one_tile<GemmCfg<8, 6, true>, F32>(a2, e2, blockIdx.x - blocks1, tiles_m, tiles_n2, smem);
+    else one_tile<GemmCfg<8, 8, true>, F32>(a, e, blockIdx.x, tiles_m, tiles_n, smem);
 }
 
 template <bool F32>
@@ -319,6 +336,30 @@ hipError_t launch_tiled(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s)
     return hipGetLastError();
 }
 
+template <bool F32>
+hipError_t launch_two_widths(const GemmArgs& a, const EpilogueArgs& e, int64_t wide, hipStream_t s) {
+    static std::once_flag once;
+    static hipError_t attr_result = hipSuccess;
+    constexpr int lds = GemmCfg<8, 8, true>::LDS_BYTES;
+    auto kern = two_widths_gemm_i8_epilogue_kernel<F32>;
+    const hipError_t err = raise_lds_limit(kern, lds, &once, &attr_result);
+    if (err != hipSuccess) return err;
+    auto from = [&](const void* p, int bytes) { return p ? const_cast<char*>(static_cast<const char*>(p)) + wide * bytes : nullptr; };
+    GemmArgs g = a, g2 = a;
+    EpilogueArgs e2 = e;
+    g.N = wide;
+    g2.N -= wide;
+    g2.B += wide * a.ldb;
+    if (a.col_scale) g2.col_scale += wide;
+    g2.C = from(a.C, F32 ? 4 : 2);
+    e2.bias = from(e.bias, e.bias_f32 ? 4 : 2);
+    e2.residual = from(e.residual, F32 ? 4 : 2);
+    e2.Z = from(e.Z, F32 ? 4 : 2);
+    const int tiles_m = (int)tiles(a.M, 256), n1 = (int)(wide / 256), n2 = (int)tiles(g2.N, 192);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * (n1 + n2))), dim3(256), lds, s, g, e, n1, g2, e2, n2, tiles_m, (unsigned)(tiles_m * n1));
+    return hipGetLastError();
+}
+
 template <int TM, int TN, bool F32>
 hipError_t launch_split(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
     using Cfg = SmallCfg<TM, TN, true>;
@@ -340,6 +381,8 @@ hipError_t launch_split_by_columns(const GemmArgs& a, const EpilogueArgs& e, hip
 }
 template <bool F32>
 hipError_t launch_by_shape(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
+    const int64_t wide = two_widths(a);      // -1 where N is no multiple of 16 or one width is faster
+    if (wide >= 0) return launch_two_widths<F32>(a, e, wide, s);
     switch (a.config < 0 ? choose_config(a, nullptr) : a.config) {
         case 0:
         case 1: return launch_tiled<8, 8, F32>(a, e, s);

@@ -38,11 +38,13 @@ def check(A, B, rs, cs, bias, act, res, C, Z, dtype, what):
 # end inside a tile in rows, columns and K
 SHAPES = [(1, 16, 16), (1, 1000, 4096), (1, 4096, 4096), (3, 8192, 512), (16, 14336, 256), (17, 1024, 1008), (32, 4096, 1024), (32, 16384, 128),
           (64, 2048, 2064), (512, 2048, 512), (1000, 1003, 1008), (2048, 2048, 256), (1024, 4096, 4096), (4096, 4096, 400), (2999, 4093, 144),
-          (4100, 8200, 128), (33, 1, 64), (300, 7, 96)]
+          (4100, 8200, 128), (33, 1, 64), (300, 7, 96), (30, 8192, 128)]
+# tiles of 256 x 192, alone and behind tiles of 256 x 256; rows that end inside one
+TWO_WIDTHS = [(2199, 5312, 1024, torch.bfloat16), (4531, 5520, 256, torch.bfloat16), (1411, 7760, 2048, torch.float32),
+              (4231, 6688, 1024, torch.float32)]
 
 
-@pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("M,N,K", SHAPES)
+@pytest.mark.parametrize("M,N,K,dtype", [s + (d,) for s in SHAPES for d in DTYPES] + TWO_WIDTHS)
 def test_product(M, N, K, dtype):
     A, B, rs, cs, rng = operands(M, N, K, M + N + K)
     act = ACTS[(M + N + K) % 5]
