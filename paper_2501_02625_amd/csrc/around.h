@@ -80,7 +80,7 @@ struct AdamwStep {
     const float* lr_ptr;
     const float* grad_scale_ptr;
     int64_t step;
-    double lr, beta1_64, beta2_64, weight_decay;
+    double lr, log_beta1, log_beta2, weight_decay;      // logarithms to base 2
 };
 // param: 0 fp32, 1 bf16, 2 bf16 with a master copy.
 hipError_t launch_adamw(const AdamwStep& step, const AdamwTensor* tensors, int count, int param, int grad_f32, int state8, hipStream_t s);

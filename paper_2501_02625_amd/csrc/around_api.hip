@@ -182,7 +182,7 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
     s.key0 = (uint32_t)d.seed; s.key1 = (uint32_t)(d.seed >> 32);
     s.step = d.step_ptr ? 1 : d.step;
     s.offset = d.offset + (d.step_ptr ? 0 : (uint64_t)d.step);
-    s.lr = d.lr_ptr ? 0.0 : d.lr; s.beta1_64 = d.beta1; s.beta2_64 = d.beta2; s.weight_decay = d.weight_decay;
+    s.lr = d.lr_ptr ? 0.0 : d.lr; s.log_beta1 = std::log2(d.beta1); s.log_beta2 = std::log2(d.beta2); s.weight_decay = d.weight_decay;
     s.step_ptr = d.step_ptr; s.lr_ptr = d.lr_ptr; s.grad_scale_ptr = d.grad_scale_ptr;
     adamw_numbers((double)s.step, s.lr, d.beta1, d.beta2, d.weight_decay, &s.decay, &s.rate, &s.root);
     const int param = d.param_dt == HALO_F32 ? 0 : masters ? 2 : 1;

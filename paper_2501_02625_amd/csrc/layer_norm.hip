@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(LANES* TEAMS) norm_bwd_kernel(NormBwd a) {
     const bool need_x = a.EX || a.GW;
     Weights<W32> w[GROUPS];
     Eight<E> x[GROUPS], e[GROUPS], next_x[GROUPS], next_e[GROUPS];
-    float mean, rstd, next_mean = 0.0f, next_rstd = 0.0f;
+    float mean = 0.0f, rstd = 0.0f, next_mean = 0.0f, next_rstd = 0.0f;
     float gw[GROUPS][8], gb[GROUPS][8];
     int left[GROUPS];
     int64_t row = (int64_t)blockIdx.x * TEAMS + team;
