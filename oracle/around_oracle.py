@@ -100,8 +100,9 @@ def philox(counter, key):
     return x
 
 
-def random16(n, tensor, kind, seed, offset):
-    g = np.arange((n + 7) // 8, dtype=np.uint64)
+def random16(n, tensor, kind, seed, offset, first=0):
+    """Of the elements from `first` on, a multiple of 8."""
+    g = np.arange((n + 7) // 8, dtype=np.uint64) + np.uint64(first // 8)
     full = lambda v: np.full(g.shape, v & 0xFFFFFFFF, np.uint64)
     w = philox([g & np.uint64(0xFFFFFFFF), full(4 * tensor + kind), full(offset), full((offset >> 32) & 0xFFFFFFFF)], seed)
     halves = [(w[j // 2] >> np.uint64(16 * (j % 2))) & np.uint64(0xFFFF) for j in range(8)]
@@ -151,9 +152,9 @@ def codes_of(x, u, square):
 
 
 def adamw(p, g, m, v, *, step, lr, betas, eps, weight_decay, grad_scale, tensor=0, seed=0, offset=0, m_scale=None, v_scale=None,
-          bf16=False):
+          bf16=False, first=0):
     """One tensor (flat).  p, g fp32 values; m, v fp32, or uint8 codes with their scales; bf16: p comes back as bf16 bits, rounded at
-    random.  Returns (p, m, v, m_scale, v_scale)."""
+    random; first: the first element's place in the tensor.  Returns (p, m, v, m_scale, v_scale)."""
     b1, b2 = betas
     n, o = len(p), (offset + step) % 2 ** 64
     r1, r2 = F(1 - b1), F(1 - b2)
@@ -171,10 +172,10 @@ def adamw(p, g, m, v, *, step, lr, betas, eps, weight_decay, grad_scale, tensor=
         p = p * decay - rate * (m / (root * root_by + F(eps)))
         assert p.dtype == F and m.dtype == F and v.dtype == F
         if bf16:
-            bits = (p.view(np.uint32).astype(np.uint64) + random16(n, tensor, 0, seed, o).astype(np.uint64)) >> np.uint64(16)
+            bits = (p.view(np.uint32).astype(np.uint64) + random16(n, tensor, 0, seed, o, first).astype(np.uint64)) >> np.uint64(16)
             p = np.where(np.isnan(p), 0x7FC0, bits & np.uint64(0xFFFF)).astype(np.uint16)
         if eight:
-            mc, ms = codes_of(m, random16(n, tensor, 1, seed, o), False)
-            vc, vs = codes_of(root, random16(n, tensor, 2, seed, o), True)
+            mc, ms = codes_of(m, random16(n, tensor, 1, seed, o, first), False)
+            vc, vs = codes_of(root, random16(n, tensor, 2, seed, o, first), True)
             return p, mc, vc, ms, vs
     return p, m, v, None, None
