@@ -161,30 +161,42 @@ struct Finish {
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) res[k] = next[k];
                 request();                                       // behind the last rows: outside the buffer, or rows that nobody uses
+                // a group of steps without a branch, so that they cover one another's latencies, and then its stores
+                v4f x[AHEAD][W / 4];
+                v4u zs[AHEAD], ys[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                    for (int q = 0; q < W / 4; ++q)
+                        x[k][q] = *reinterpret_cast<const v4f*>(mine + ((step + k) * ROWS + at_row) * PITCH + at_col + 4 * q);
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) {
-                    const float* from = mine + ((step + k) * ROWS + at_row) * PITCH + at_col;
-                    v4f x[W / 4];
-#pragma unroll
-                    for (int q = 0; q < W / 4; ++q) x[q] = *reinterpret_cast<const v4f*>(from + 4 * q);
                     float z[W], y[W];
 #pragma unroll
                     for (int j = 0; j < W; ++j) {
-                        z[j] = __builtin_fmaf(x[j / 4][j % 4], cs[j], bias[j]);
+                        z[j] = __builtin_fmaf(x[k][j / 4][j % 4], cs[j], bias[j]);
                         y[j] = activation<ACT, !F32>(z[j]);
                         if constexpr (RES) y[j] += P::get(res[k], j);
                     }
-                    if (e.Z) __builtin_amdgcn_raw_buffer_store_b128(P::put(z), to_z, (int)(partly ? kOutside : at_z), 0, PAST);
-                    __builtin_amdgcn_raw_buffer_store_b128(P::put(y), to_c, (int)(partly ? kOutside : at_c), 0, PAST);
-                    if (ragged) {                                // uniform: some tile's columns end inside a lane's 16 bytes
+                    zs[k] = P::put(z);
+                    ys[k] = P::put(y);
+                }
+                if (e.Z) {
+#pragma unroll
+                    for (int k = 0; k < AHEAD; ++k) __builtin_amdgcn_raw_buffer_store_b128(zs[k], to_z, (int)(partly ? kOutside : at_z + k * more_z), 0, PAST);
+                    at_z += AHEAD * more_z;
+                }
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) __builtin_amdgcn_raw_buffer_store_b128(ys[k], to_c, (int)(partly ? kOutside : at_c + k * more_c), 0, PAST);
+                at_c += AHEAD * more_c;
+                if (ragged) {                                    // uniform: some tile's columns end inside a lane's 16 bytes
+#pragma unroll
+                    for (int k = 0; k < AHEAD; ++k) {
                         const int64_t row = row0 + (part * STEPS + step + k) * ROWS + at_row;
-                        if (partly && row < a.M) {
-                            if (e.Z) P::template store<false>(address<F32>(e.Z, e.ld_z, row, col), P::put(z), n);
-                            P::template store<false>(address<F32>(a.C, a.ldc, row, col), P::put(y), n);
-                        }
+                        if (!partly || row >= a.M) continue;
+                        if (e.Z) P::template store<false>(address<F32>(e.Z, e.ld_z, row, col), zs[k], n);
+                        P::template store<false>(address<F32>(a.C, a.ldc, row, col), ys[k], n);
                     }
-                    at_c += more_c;
-                    at_z += more_z;
                 }
             }
         }
