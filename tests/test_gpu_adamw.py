@@ -154,6 +154,21 @@ def test_extremes(state):
         m.compare("step %d:" % step)
 
 
+@pytest.mark.parametrize("state", [32, 8])
+def test_nan_parameters_stay_nan(state):
+    """bf16 parameters of their own: a NaN in the parameter, in the gradient and, with any payload, in a 32-bit state."""
+    m = Model([1024], "bf16", "bf16", state, 9)
+    m.dp[0][3], m.dg[0][500] = float("nan"), float("nan")
+    m.dp[0][700:702].view(torch.int16).fill_(0x7FFF)
+    gone = {3, 500, 700, 701}
+    if state == 32:
+        m.dm[0][800:801].view(torch.int32).fill_(0x7FFFFFFF)
+        m.dv[0][801:802].view(torch.int32).fill_(-1)
+        gone |= {800, 801}
+    m.call(**dict(HYPER, step=1, seed=1, offset=0))
+    assert set(torch.isnan(m.dp[0].float()).nonzero()[:, 0].tolist()) == gone
+
+
 def test_no_state_of_0_is_divided_by():
     """8 bits: where v is far below its block's largest, it is kept above 0, and the update stays bounded when the gradient ends."""
     n = 1024
