@@ -542,9 +542,9 @@ halo_status halo_layer_norm_bwd(const halo_norm_desc* desc, const void* E, int64
  *   beta1, beta2           in [0, 1);  lr, eps, weight_decay: finite, not negative;  grad_scale: finite.
  *   count                  at most 1024 tensors, each of at most 2^34 elements.
  * Pointers are 16-byte aligned, but for the scales, step_ptr (8), lr_ptr and grad_scale_ptr (4 bytes).  What the call writes overlaps
- * nothing else that it reads or writes; parameters, states, masters and scales that overlap one another are refused (HALO_EINVAL).  The
- * array `tensors` is host memory and is not used after the call returns; addresses are copied into a captured graph.  infinities and
- * NaN: 32 bits, their own elements; 8 bits, their 256 elements' states and own parameters.
+ * nothing else that it reads or writes, or it is refused (HALO_EINVAL; a gradient may belong to several tensors).  The array `tensors`
+ * is host memory and is not used after the call returns; addresses are copied into a captured graph.  Infinities and NaN: 32 bits, their
+ * own elements; 8 bits, their 256 elements' states and own parameters.
  */
 #define HALO_ADAMW_BLOCK 256
 typedef struct halo_adamw_tensor {

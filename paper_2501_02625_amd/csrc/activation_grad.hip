@@ -1,4 +1,6 @@
-// The gradient of the epilogue of a product (halo_activation_bwd): E_Z = E act'(Z), and the bias' gradient, its column sums.
+// The gradient of the epilogue of a product (halo_activation_bwd): E_Z = E act'(Z), and the bias' gradient, its column sums, in one pass.
+// What bounds it is memory, and of small matrices the two launches.  8192 x 14336 in bf16 with gelu: 145 us, 4.9 TB/s (a large copy reaches
+// 5.1), and 4.5 for the sum over 73 parts of the rows; with two rows of a thread's on their way instead of four 165.
 #pragma clang fp contract(off)
 
 #include <type_traits>

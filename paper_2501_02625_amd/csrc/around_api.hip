@@ -43,6 +43,7 @@ halo_status check_norm(const halo_norm_desc* d) {
 
 struct Range {
     uintptr_t from, to;
+    bool written;
 };
 
 }  // namespace
@@ -143,7 +144,7 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
     const bool eight = d.state_bits == 8;
     const size_t pe = d.param_dt == HALO_BF16 ? 2 : 4, se = eight ? 1 : 4;
     AdamwTensor list[kMost];
-    Range written[kMost * 6];
+    Range used[kMost * 7];
     int n = 0, ranges = 0;
     bool masters = false, plain = false;
     for (int32_t t = 0; t < count; ++t) {
@@ -156,11 +157,12 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
         if (x.size > (int64_t(1) << 34)) return HALO_EUNSUPPORTED;
         if (!aligned(x.param, 16) || !aligned(x.grad, 16) || !aligned(x.m, 16) || !aligned(x.v, 16) || !aligned(x.master, 16)) return HALO_EALIGN;
         if (eight && (!aligned(x.m_scale, 4) || !aligned(x.v_scale, 4))) return HALO_EALIGN;
-        auto add = [&](const void* p, size_t bytes) {
-            if (p) written[ranges++] = Range{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes};
+        auto add = [&](const void* p, size_t bytes, bool written = true) {
+            if (p) used[ranges++] = Range{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written};
         };
         const size_t size = (size_t)x.size, blocks = (size + HALO_ADAMW_BLOCK - 1) / HALO_ADAMW_BLOCK;
         add(x.param, size * pe);
+        add(x.grad, size * (d.grad_dt == HALO_BF16 ? 2 : 4), false);
         add(x.m, size * se);
         add(x.v, size * se);
         add(x.master, size * 4);
@@ -171,10 +173,14 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
         list[n++] = AdamwTensor{x.param, x.grad, x.m, x.v, x.master, x.m_scale, x.v_scale, x.size, t};
     }
     if (masters && plain) return HALO_EINVAL;
-    // a tensor given twice would be updated by two workgroups at once
-    std::sort(written, written + ranges, [](const Range& a, const Range& b) { return a.from < b.from; });
-    for (int i = 1; i < ranges; ++i)
-        if (written[i].from < written[i - 1].to) return HALO_EINVAL;
+    // A tensor given twice would be updated by two workgroups at once.  Gradients may be shared.
+    std::sort(used, used + ranges, [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t end = 0, written_end = 0;      // of what lies in front
+    for (int i = 0; i < ranges; ++i) {
+        if (used[i].from < (used[i].written ? end : written_end)) return HALO_EINVAL;
+        end = std::max(end, used[i].to);
+        if (used[i].written) written_end = std::max(written_end, used[i].to);
+    }
     if (n == 0) return HALO_OK;
     AdamwStep s{};
     s.beta1 = (float)d.beta1; s.rest1 = (float)(1.0 - d.beta1); s.beta2 = (float)d.beta2; s.rest2 = (float)(1.0 - d.beta2);

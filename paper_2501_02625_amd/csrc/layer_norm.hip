@@ -2,7 +2,9 @@
 //
 // What bounds both is memory.  A row is held in registers by a team of LANES lanes, eight elements at a time and GROUPS times, so that it is
 // read once: the mean, then the squares about it, then the result.  Teams go from row to row, with the next row's loads on their way
-// while this one is worked on; weight and bias stay in registers.
+// while this one is worked on; weight and bias stay in registers.  bf16, 8192 x 4096 with a bias: 25 us, 5.4 TB/s (a large copy reaches 5.1),
+// one row of 4096 2.1 us; the gradient with a base and G_W, 2048 x 4096: 14.5 us, 4.6 TB/s, and 4.0 for the sum over 512 parts of
+// the rows.
 #pragma clang fp contract(off)
 
 #include <type_traits>
@@ -440,11 +442,18 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBwd a, int64_t ro
     }
 }
 
-// Workgroups of a launch: enough for every compute unit to hold several at once; each goes through its rows.  The gradient's hold 1024
+// Lanes and groups of a row.  As many lanes as the row has pieces of eight, up to 64, so that no wavefront meets another; beyond 512
+// columns two groups or more lanes, whichever was faster.  Forward, bf16, columns and rows: two groups of 64 lanes / one of 128, 1000 x
+// 16384 15.0 us / 16.0, but backward, where sums take registers, four teams of 128 lanes, 1003 x 1031 in fp32 6.3 us, and of 64 7.6; one
+// group of 256 / four of 64, 2048 x 4096 9.7 / 12.5; one of 512 / two of 256, 4096 x 8192 25.0 / 24.1, 4096 x 64 3.4 / 3.9; one of 1024 / two of
+// 512, 8192 x 2048 15.5 / 18.4; backward one of 512 / two of 256, 4096 x 2048 14.5 / 15.4.
+//
+// Workgroups of a launch: enough for every compute unit to hold several at once; each goes through its rows.  Forward 2^19 threads: 2^18 /
+// 2^19 / 2^20, 4096 x 8192 28.4 us / 25.0 / 24.4, 14336 x 1024 14.8 / 16.2 / 19.4, 1000 x 16384 14.5 / 14.9 / 16.3.  The gradient's hold 1024
 // threads of a compute unit's, or 512 where a thread has four groups: every one more writes a part of the sums and has fewer rows to
 // have on their way.  EX, G_W and G_B in bf16, 256 / 512 / 768 workgroups: 8192 x 4096 (512 lanes) 53.8 us / 47.4 / 53.6, 2048 x 8192 with
 // 1024 lanes 27.1 / 36 / 42, 1024 x 14336 (512 lanes, four groups) 38.4 / 46.4 / 53.6, 8192 x 512 12.1 / 10.4 / 9.8.
-constexpr int64_t kMostFwd = 2048, kMostBwd = 512;
+constexpr int64_t kThreadsFwd = 1 << 19, kMostBwd = 512;
 template <int LANES, int GROUPS>
 constexpr int64_t most_bwd() { return LANES >= 1024 || GROUPS >= 4 ? kMostBwd / 2 : kMostBwd; }
 inline unsigned groups_of(int64_t rows, int teams, int64_t most) {
@@ -454,7 +463,8 @@ inline unsigned groups_of(int64_t rows, int teams, int64_t most) {
 
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
 hipError_t fwd(const NormFwd& a, hipStream_t s) {
-    hipLaunchKernelGGL((norm_fwd_kernel<E, W32, LANES, GROUPS, TEAMS>), dim3(groups_of(a.rows, TEAMS, kMostFwd)), dim3(LANES * TEAMS), 0, s, a);
+    const unsigned groups = groups_of(a.rows, TEAMS, kThreadsFwd / (LANES * TEAMS));
+    hipLaunchKernelGGL((norm_fwd_kernel<E, W32, LANES, GROUPS, TEAMS>), dim3(groups), dim3(LANES * TEAMS), 0, s, a);
     return hipGetLastError();
 }
 template <typename E, bool W32>
@@ -466,8 +476,8 @@ hipError_t fwd_by_shape(const NormFwd& a, hipStream_t s) {
     if (c <= 512) return fwd<E, W32, 64, 1, 4>(a, s);
     if (c <= 1024) return fwd<E, W32, 64, 2, 4>(a, s);
     if (c <= 2048) return fwd<E, W32, 256, 1, 1>(a, s);
-    if (c <= 4096) return fwd<E, W32, 256, 2, 1>(a, s);
-    if (c <= 8192) return fwd<E, W32, 512, 2, 1>(a, s);
+    if (c <= 4096) return fwd<E, W32, 512, 1, 1>(a, s);
+    if (c <= 8192) return fwd<E, W32, 1024, 1, 1>(a, s);
     if (c <= 16384) return fwd<E, W32, 1024, 2, 1>(a, s);
     return fwd<E, W32, 512, 8, 1>(a, s);
 }
@@ -493,7 +503,8 @@ hipError_t bwd_apart(const NormBwd& a, hipStream_t s) {
         const int64_t tiles = (a.cols + 511) / 512, most = apart_parts(a.rows, a.cols);
         const int64_t per = most ? (a.rows + most - 1) / most : 1, parts = (a.rows + per - 1) / per;
         if (parts) hipLaunchKernelGGL((norm_columns_kernel<E>), dim3((unsigned)tiles, (unsigned)parts), dim3(256), 0, s, a, per);
-        const hipError_t e = launch_sum_parts(a.part, a.GW, a.part + parts * ((a.cols + 3) / 4 * 4), a.GB, parts, a.cols, (a.cols + 3) / 4 * 4, s);
+        const hipError_t e = launch_sum_parts(a.part, a.GW, a.part + parts * ((a.cols + 3) / 4 * 4), a.GB, parts, a.cols,
+                                              (a.cols + 3) / 4 * 4, s);
         if (e != hipSuccess) return e;
     }
     if (a.EX && a.rows)

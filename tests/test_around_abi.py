@@ -186,6 +186,7 @@ def test_adamw(lib, change, status):
     (dict(grad=0x20000002), EALIGN), (dict(m=0x20000004), EALIGN), (dict(v=0x20000008), EALIGN), (dict(master=0x20600004), EALIGN),
     (dict(m_scale=0x20400002), EALIGN), (dict(v_scale=0x20500001), EALIGN), (dict(m=0x20000000), EINVAL), (dict(m_scale=0x20300000), EINVAL),
     (dict(param=0x10000000), EINVAL), (dict(param=0x10000000 + 1984), EINVAL), (dict(v=0x10300000 + 992), EINVAL), (dict(master=0x20600000), EINVAL),
+    (dict(grad=0x10000000), EINVAL), (dict(grad=0x20200000), EINVAL), (dict(m=0x10100000), EINVAL), (dict(param=0x10100000 + 1984), EINVAL),
 ])
 def test_adamw_tensors(lib, change, status):
     """The second of two tensors: missing, misaligned, or overlapping the first or itself; one master for two."""

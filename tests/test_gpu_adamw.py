@@ -218,6 +218,16 @@ def test_numbers_from_the_device_and_graphs():
         m.compare("replay %d:" % k)
 
 
+def test_a_gradient_of_two_parameters():
+    m = Model([700, 700], "bf16", "fp32", 8, 10)
+    m.g[1] = m.g[0]
+    m.dg[1] = m.dg[0]
+    more = dict(HYPER, step=1, seed=1, offset=0)
+    m.call(**more)
+    m.expect(**more)
+    m.compare()
+
+
 def test_two_streams():
     """Calls on two streams, each with its own tensors, at once."""
     a, b = Model([50_000], "bf16", "fp32", 8, 7), Model([60_000], "bf16", "fp32", 8, 8)
