@@ -6,9 +6,9 @@
 // above v by the variance of the rounding, every step again), they follow.
 //
 // What bounds it: memory with states in 32 bits (12.6M elements in fp32 71 us, 5.0 TB/s; a large copy reaches 5.1), with 8 bits
-// instructions as much, some hundred an element, a seventh of them the random numbers: 219M elements in bf16 497 to 520 us, 4.3 TB/s; 470
-// with the random numbers left out, 500 with approximate roots and quotients and the rest as it was then (566).  One round instead of two
-// 545, four as two; loads that stay in the caches as these.
+// instructions as much, some hundred an element: 219M elements in bf16 500 to 530 us on different cards, 4.1 to 4.4 TB/s; 467 without the
+// random numbers where it takes 530.  There one round instead of two 545, and loads that stay in the caches 537; before the roots were what
+// they are, four rounds as two.
 #pragma clang fp contract(off)
 
 #include <cmath>
