@@ -4,7 +4,7 @@
 // read once: the mean, then the squares about it, then the result.  Teams go from row to row, with the next row's loads on their way
 // while this one is worked on; weight and bias stay in registers.  bf16, 8192 x 4096 with a bias: 25 us, 5.4 TB/s (a large copy reaches 5.1),
 // one row of 4096 2.1 us; the gradient with a base and G_W, 2048 x 4096: 14.5 us, 4.6 TB/s, and 4.0 for the sum over 512 parts of
-// the rows.
+// the rows; 128 x 4096, in one launch, 4.4.
 #pragma clang fp contract(off)
 
 #include <type_traits>
@@ -248,9 +248,64 @@ __global__ void __launch_bounds__(LANES* TEAMS) norm_fwd_kernel(NormFwd a) {
     }
 }
 
+// G_W and G_B of 64 columns over all rows, by a workgroup of THREADS: eight lanes have a row's part.
+template <typename E, int THREADS>
+__device__ __forceinline__ void few_rows_columns(const NormBwd& a, int block, float (&meet)[THREADS / 64][2][64]) {
+    const int lane = threadIdx.x & 7, c = block * 64 + lane * 8, left = a.cols - c;
+    float sum[2][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[0][j] = sum[1][j] = 0.0f;
+    if (left > 0) {
+#pragma unroll 4
+        for (int64_t r = threadIdx.x >> 3; r < a.rows; r += THREADS / 8) {
+            Eight<E> e, x;
+            e.load(reinterpret_cast<const E*>(a.E) + r * a.ld_e + c, left > 4);
+            float mean = 0.0f, rstd = 0.0f;
+            cut(x, 0);
+            if (a.GW) {
+                x.load(reinterpret_cast<const E*>(a.X) + r * a.ld_x + c, left > 4);
+                mean = a.mean ? a.mean[r] : 0.0f;
+                rstd = a.rstd[r];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sum[0][j] = __builtin_fmaf(e.get(j), (x.get(j) - mean) * rstd, sum[0][j]);
+                sum[1][j] += e.get(j);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+#pragma unroll
+            for (int d = 8; d < 64; d *= 2) sum[i][j] += __shfl_xor(sum[i][j], d);
+            if ((threadIdx.x & 63) < 8) meet[threadIdx.x >> 6][i][lane * 8 + j] = sum[i][j];
+        }
+    __syncthreads();
+    if (threadIdx.x >= 128) return;
+    const int which = threadIdx.x >> 6, col = block * 64 + (threadIdx.x & 63);
+    float* out = which ? a.GB : a.GW;
+    if (!out || col >= a.cols) return;
+    float t = 0.0f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) t += meet[w][which][threadIdx.x & 63];
+    out[col] = t;
+}
+
 // EX, and with SUMS the sums of the columns over the workgroup's rows, which go to part: the teams add theirs to one another in LDS.
+// Without SUMS the first row_groups workgroups have the rows, and those behind them, of few rows, the sums.
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS, bool SUMS>
-__global__ void __launch_bounds__(LANES* TEAMS) norm_bwd_kernel(NormBwd a) {
+__global__ void __launch_bounds__(LANES* TEAMS) norm_bwd_kernel(NormBwd a, unsigned row_groups) {
+    if constexpr (!SUMS) {
+        __shared__ float columns[LANES * TEAMS / 64][2][64];
+        if (blockIdx.x >= row_groups) {
+            few_rows_columns<E, LANES * TEAMS>(a, blockIdx.x - row_groups, columns);
+            return;
+        }
+    } else {
+        row_groups = gridDim.x;
+    }
     using S = Shape<LANES, GROUPS, SUMS>;
     using Sum = TeamSum<LANES, TEAMS, 2>;
     __shared__ float s[2][2][TEAMS][Sum::WAVES];
@@ -258,7 +313,7 @@ __global__ void __launch_bounds__(LANES* TEAMS) norm_bwd_kernel(NormBwd a) {
     __shared__ __align__(16) float meet[SUMS && TEAMS > 1 ? 2 * TEAMS * WIDE : 1];
     Sum sum{s};
     const int team = TEAMS > 1 ? threadIdx.x / LANES : 0, lane = threadIdx.x % LANES;
-    const int64_t stride = (int64_t)gridDim.x * TEAMS;
+    const int64_t stride = (int64_t)row_groups * TEAMS;
     const E *X = reinterpret_cast<const E*>(a.X), *Er = reinterpret_cast<const E*>(a.E), *base = reinterpret_cast<const E*>(a.base);
     const bool need_x = a.EX || a.GW;
     Weights<W32> w[GROUPS];
@@ -482,12 +537,33 @@ hipError_t fwd_by_shape(const NormFwd& a, hipStream_t s) {
     return fwd<E, W32, 512, 8, 1>(a, s);
 }
 
+// Few rows, eight for each thread of the sums at most: E_X and the sums of the columns in one launch, by workgroups of their own, which read E
+// and X once more.  Layer norm with a base in a graph, one launch / parts and their sum: bf16, 64 x 512 4.1 us / 5.6, 128 x 14336 7.6 / 19.8,
+// 256 x 512 4.9 / 6.1, 512 x 512 6.3 / 5.9 (not taken), 512 x 4096 7.0 / 15.9, 512 x 14336 21.1 / 29.1, 1024 x 4096 12.0 / 16.1 (not
+// taken), 1024 x 8192 the same; fp32, 256 x 4096 6.7 / 11.8, 512 x 8192 22.0 / 20.4, 1024 x 8192 36.5 / 29.1 (not taken).
+inline bool few_rows(const NormBwd& a, int threads) { return (a.GW || a.GB) && a.rows > 0 && a.rows <= (threads < 512 ? threads : 512); }
+template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
+hipError_t bwd_few_rows(const NormBwd& a, hipStream_t s) {
+    const unsigned groups = a.EX ? groups_of(a.rows, TEAMS, kMostBwd) : 0, columns = (unsigned)(a.cols + 63) / 64;
+    auto launch = [&](unsigned rows, unsigned behind) {
+        hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, false>), dim3(rows + behind), dim3(LANES * TEAMS), 0, s, a, rows);
+    };
+    if (a.EX == a.E || a.EX == a.X) {        // it would be overwritten while columns are read
+        launch(0, columns);
+        launch(groups, 0);
+    } else {
+        launch(groups, columns);
+    }
+    return hipGetLastError();
+}
+
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
 hipError_t bwd(const NormBwd& a, hipStream_t s) {
+    if (few_rows(a, LANES * TEAMS)) return bwd_few_rows<E, W32, LANES, GROUPS, TEAMS>(a, s);
     const bool sums = a.GW || a.GB;
     const unsigned groups = groups_of(a.rows, TEAMS, most_bwd<LANES, GROUPS>());
-    if (groups && sums) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, true>), dim3(groups), dim3(LANES * TEAMS), 0, s, a);
-    else if (groups) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, false>), dim3(groups), dim3(LANES * TEAMS), 0, s, a);
+    if (groups && sums) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, true>), dim3(groups), dim3(LANES * TEAMS), 0, s, a, groups);
+    else if (groups) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, false>), dim3(groups), dim3(LANES * TEAMS), 0, s, a, groups);
     if (sums) return launch_sum_parts(a.part, a.GW, a.part + groups * ((a.cols + 3) / 4 * 4), a.GB, groups, a.cols, (a.cols + 3) / 4 * 4, s);
     return hipGetLastError();
 }
@@ -499,6 +575,7 @@ inline int64_t apart_parts(int64_t rows, int64_t cols) {
 }
 template <typename E, bool W32, int GROUPS>
 hipError_t bwd_apart(const NormBwd& a, hipStream_t s) {
+    if (few_rows(a, 512)) return bwd_few_rows<E, W32, 512, GROUPS, 1>(a, s);
     if (a.GW || a.GB) {
         const int64_t tiles = (a.cols + 511) / 512, most = apart_parts(a.rows, a.cols);
         const int64_t per = most ? (a.rows + most - 1) / most : 1, parts = (a.rows + per - 1) / per;
@@ -507,8 +584,10 @@ hipError_t bwd_apart(const NormBwd& a, hipStream_t s) {
                                               (a.cols + 3) / 4 * 4, s);
         if (e != hipSuccess) return e;
     }
-    if (a.EX && a.rows)
-        hipLaunchKernelGGL((norm_bwd_kernel<E, W32, 512, GROUPS, 1, false>), dim3(groups_of(a.rows, 1, kMostBwd)), dim3(512), 0, s, a);
+    if (a.EX && a.rows) {
+        const unsigned groups = groups_of(a.rows, 1, kMostBwd);
+        hipLaunchKernelGGL((norm_bwd_kernel<E, W32, 512, GROUPS, 1, false>), dim3(groups), dim3(512), 0, s, a, groups);
+    }
     return hipGetLastError();
 }
 template <typename E, bool W32>
