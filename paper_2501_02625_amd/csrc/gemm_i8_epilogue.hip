@@ -70,14 +70,17 @@ __device__ __forceinline__ void with_activation(int act, const F& f) {
 // The accumulators of a wavefront go through LDS, four rows of 16 x 16 tiles at a time, so that a lane has 16 bytes of C, Z and residual
 // that lie together, always of the same columns, and the code that computes them is a loop (over the accumulators, which are named
 // registers, it would be as long as the tile).  The LDS belongs to the wavefront: no barrier but the first.  One wavefront per SIMD has
-// nothing to hide a load behind but its own work: scales and bias are requested in front of the main loop, residuals a group of
-// steps ahead.
+// nothing to hide a load behind but its own work: scales and bias are requested in front of the main loop, residuals groups of steps
+// ahead.
 template <class Cfg, bool F32>
 struct Finish {
     using P = Piece<F32>;
     static constexpr int TM = Cfg::TM, TN = Cfg::TN, WN = Cfg::WN, W = P::W;
     static constexpr int LANES = (WN > 64 ? 128 : 64) / W, ROWS = 64 / LANES;             // lanes a row (of 96 columns, a quarter idle), rows a step
     static constexpr int PITCH = WN + 4, PARTS = TM / 4, STEPS = 64 / ROWS, AHEAD = 4, SIZE = F32 ? 4 : 2;
+    // groups of steps whose residual is on its way: fp32, one / two / three, 4747 x 4096 x 512 36.2 us / 34.0 / 33.6, 8192 x 14336 x 512 with Z
+    // 344 / 329 / 327; bf16, with half the bytes, 28.3 / 29.1 / 29.6 and 180 each way
+    static constexpr int GROUPS = F32 ? 2 : 1;
     using Buffer = __amdgpu_buffer_rsrc_t;
     static_assert(TM % 4 == 0 && STEPS % AHEAD == 0 && 4 * 64 * PITCH * 4 <= Cfg::LDS_BYTES, "what a wavefront holds in LDS");
     float rs[TM], cs[W], bias[W];
@@ -127,17 +130,18 @@ struct Finish {
         uint32_t at_r = n > 0 ? (uint32_t)((at_row * e.ld_res + col - col0) * SIZE) : kOutside;
         const uint32_t more_c = n > 0 ? (uint32_t)(ROWS * a.ldc * SIZE) : 0, more_z = n > 0 ? (uint32_t)(ROWS * e.ld_z * SIZE) : 0;
         const uint32_t more_r = n > 0 ? (uint32_t)(ROWS * e.ld_res * SIZE) : 0;
-        v4u res[AHEAD], next[AHEAD];
-        auto request = [&]() {
+        v4u res[AHEAD], next[GROUPS][AHEAD];                     // this group's residual, and the following groups'
+        auto request = [&](v4u(&to)[AHEAD]) {
             if constexpr (RES) {
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) {
-                    next[k] = __builtin_amdgcn_raw_buffer_load_b128(from_r, (int)at_r, 0, 0);
+                    to[k] = __builtin_amdgcn_raw_buffer_load_b128(from_r, (int)at_r, 0, 0);
                     at_r += more_r;
                 }
             }
         };
-        request();
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) request(next[g]);
         __syncthreads();                                         // every wavefront has read its last operands
 #pragma unroll 1
         for (int part = 0; part < PARTS; ++part) {
@@ -166,8 +170,12 @@ struct Finish {
 #pragma unroll 1
             for (int step = 0; step < STEPS; step += AHEAD) {
 #pragma unroll
-                for (int k = 0; k < AHEAD; ++k) res[k] = next[k];
-                request();                                       // behind the last rows: outside the buffer, or rows that nobody uses
+                for (int k = 0; k < AHEAD; ++k) {
+                    res[k] = next[0][k];
+#pragma unroll
+                    for (int g = 1; g < GROUPS; ++g) next[g - 1][k] = next[g][k];
+                }
+                request(next[GROUPS - 1]);                       // behind the last rows: outside the buffer, or rows that nobody uses
                 // a group of steps without a branch, so that they cover one another's latencies, and then its stores
                 v4f x[AHEAD][W / 4];
                 v4u zs[AHEAD], ys[AHEAD];
@@ -406,6 +414,7 @@ hipError_t launch_split_by_columns(const GemmArgs& a, const EpilogueArgs& e, hip
 }
 template <bool F32>
 hipError_t launch_by_shape(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
+    if (a.config < 0 && small_tiles_twice(a)) return launch_split<4, 4, F32>(a, e, s);
     const int64_t wide = two_widths(a);      // -1 where N is no multiple of 16 or one width is faster
     if (wide >= 0) return launch_two_widths<F32>(a, e, wide, s);
     switch (a.config < 0 ? choose_config(a, nullptr) : a.config) {

@@ -190,6 +190,18 @@ inline int small_tile_columns(const GemmArgs& a) {
     return tiles_of(a, rows, 16) <= kComputeUnits ? 16 : tiles_of(a, rows, 32) <= kComputeUnits ? 32 : 64;
 }
 
+// 64 x 64 tiles in the small kernel where they are up to half as many again as compute units, for the product with an epilogue and a long K:
+// tiles of 128 x 128 leave two thirds of the chip idle there, and a compute unit that has two small tiles at once hides their start.  That is
+// faster only where all tiles of a column panel are on one XCD, which takes every eighth workgroup, so that B comes to one L2, and
+// where rows and columns are both cut often enough.  bf16 out with gelu and Z, 128 x 128 tiles / 64 x 64: 266 x 4096 x 12288 48.8 us / 39.0,
+// 291 x 4096 x 8192 34.7 / 29.4, 1075 x 1024 x 14336 57.0 / 44.1, 376 x 4096 x 10240 42.7 / 39.2; not taken: 242 x 4512 x 12288 (71 column
+// tiles) 50.1 / 52.3, 2163 x 512 x 12288 50.5 / 53.6, 125 x 8592 x 12288 51.4 / 53.0, 350 x 4096 x 5120 25.0 / 23.4, 327 x 4096 x 4096 20.0 / 20.2,
+// 106 x 14336 x 14336 (448 tiles) 59.6 / 62.0.
+inline bool small_tiles_twice(const GemmArgs& a) {
+    const int64_t rows = (a.M + 63) / 64, columns = (a.N + 63) / 64, tiles = rows * columns;
+    return a.K >= 8192 && tiles > kComputeUnits && 2 * tiles <= 3 * kComputeUnits && rows >= 3 && columns >= 16 && columns % 8 == 0;
+}
+
 // Estimated microseconds of launch_gemm_i8(a) / launch_gemm_i8_pair(a, *a2), for choices between ways to split the work.
 inline double gemm_i8_cost(const GemmArgs& a, const GemmArgs* a2) {
     const int c = a.config < 0 ? choose_config(a, a2) : a.config;
