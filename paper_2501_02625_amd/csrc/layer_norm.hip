@@ -537,18 +537,18 @@ hipError_t fwd_by_shape(const NormFwd& a, hipStream_t s) {
     return fwd<E, W32, 512, 8, 1>(a, s);
 }
 
-// Few rows, eight for each thread of the sums at most: E_X and the sums of the columns in one launch, by workgroups of their own, which read E
+// Few rows, 256 up to 512 columns and 512 beyond: E_X and the sums of the columns in one launch, by workgroups of their own, which read E
 // and X once more.  Layer norm with a base in a graph, one launch / parts and their sum: bf16, 64 x 512 4.1 us / 5.6, 128 x 14336 7.6 / 19.8,
-// 256 x 512 4.9 / 6.1, 512 x 512 6.3 / 5.9 (not taken), 512 x 4096 7.0 / 15.9, 512 x 14336 21.1 / 29.1, 1024 x 4096 12.0 / 16.1 (not
+// 256 x 512 4.9 / 6.1, 512 x 512 6.3 / 5.9 (not taken), 512 x 2048 6.9 / 10.9, 512 x 4096 7.0 / 15.9, 512 x 14336 21.1 / 29.1, 1024 x 4096 12.0 / 16.1 (not
 // taken), 1024 x 8192 the same; fp32, 256 x 4096 6.7 / 11.8, 512 x 8192 22.0 / 20.4, 1024 x 8192 36.5 / 29.1 (not taken).
-inline bool few_rows(const NormBwd& a, int threads) { return (a.GW || a.GB) && a.rows > 0 && a.rows <= (threads < 512 ? threads : 512); }
+inline bool few_rows(const NormBwd& a) { return (a.GW || a.GB) && a.rows > 0 && a.rows <= (a.cols <= 512 ? 256 : 512); }
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
 hipError_t bwd_few_rows(const NormBwd& a, hipStream_t s) {
     const unsigned groups = a.EX ? groups_of(a.rows, TEAMS, kMostBwd) : 0, columns = (unsigned)(a.cols + 63) / 64;
     auto launch = [&](unsigned rows, unsigned behind) {
         hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, false>), dim3(rows + behind), dim3(LANES * TEAMS), 0, s, a, rows);
     };
-    if (a.EX == a.E || a.EX == a.X) {        // it would be overwritten while columns are read
+    if (a.EX && (a.EX == a.E || a.EX == a.X)) {       // it would be overwritten while columns are read
         launch(0, columns);
         launch(groups, 0);
     } else {
@@ -559,7 +559,7 @@ hipError_t bwd_few_rows(const NormBwd& a, hipStream_t s) {
 
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
 hipError_t bwd(const NormBwd& a, hipStream_t s) {
-    if (few_rows(a, LANES * TEAMS)) return bwd_few_rows<E, W32, LANES, GROUPS, TEAMS>(a, s);
+    if (few_rows(a)) return bwd_few_rows<E, W32, LANES, GROUPS, TEAMS>(a, s);
     const bool sums = a.GW || a.GB;
     const unsigned groups = groups_of(a.rows, TEAMS, most_bwd<LANES, GROUPS>());
     if (groups && sums) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, true>), dim3(groups), dim3(LANES * TEAMS), 0, s, a, groups);
@@ -575,7 +575,7 @@ inline int64_t apart_parts(int64_t rows, int64_t cols) {
 }
 template <typename E, bool W32, int GROUPS>
 hipError_t bwd_apart(const NormBwd& a, hipStream_t s) {
-    if (few_rows(a, 512)) return bwd_few_rows<E, W32, 512, GROUPS, 1>(a, s);
+    if (few_rows(a)) return bwd_few_rows<E, W32, 512, GROUPS, 1>(a, s);
     if (a.GW || a.GB) {
         const int64_t tiles = (a.cols + 511) / 512, most = apart_parts(a.rows, a.cols);
         const int64_t per = most ? (a.rows + most - 1) / most : 1, parts = (a.rows + per - 1) / per;
