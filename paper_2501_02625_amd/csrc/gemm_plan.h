@@ -202,8 +202,9 @@ inline bool small_tiles_twice(const GemmArgs& a) {
     return a.K >= 8192 && tiles > kComputeUnits && 2 * tiles <= 3 * kComputeUnits && rows >= 3 && columns >= 16 && columns % 8 == 0;
 }
 
-// 128 x 128 tiles instead of 256 x 128 (or of the two widths) for the product with an epilogue and a short K, where the larger ones take more than
-// one round: the epilogue is then a good part of a tile's time, and of two workgroups on a compute unit one can be in its main loop meanwhile.
+// 128 x 128 tiles instead of 256 x 128 (or of the two widths) for the product with an epilogue and a short K, where the larger ones
+// take more than one round: the epilogue is then a good part of a tile's time, and of two workgroups on a compute unit one can be in its main loop
+// meanwhile.
 // bf16 out with gelu and Z, chosen by product_cost / 128 x 128: 7435 x 2624 x 256 34.2 us / 27.7, 2524 x 14336 x 400 65.3 / 55.4, 6109 x
 // 8800 x 512 88.7 / 82.3, 3596 x 14336 x 640 92.5 / 80.2, 6038 x 4096 x 768 43.7 / 41.7, 4096 x 14336 x 512 the worst of 13 such at 2 % more;
 // in one round 2048 x 4096 x 512 14.5 / 15.9.  With 256 x 256 by cost (8192 x 14336 x 512) 128 x 128 are level or up to 10 % slower.

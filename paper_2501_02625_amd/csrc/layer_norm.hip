@@ -539,8 +539,9 @@ hipError_t fwd_by_shape(const NormFwd& a, hipStream_t s) {
 
 // Few rows, 256 up to 512 columns and 512 beyond: E_X and the sums of the columns in one launch, by workgroups of their own, which read E
 // and X once more.  Layer norm with a base in a graph, one launch / parts and their sum: bf16, 64 x 512 4.1 us / 5.6, 128 x 14336 7.6 / 19.8,
-// 256 x 512 4.9 / 6.1, 512 x 512 6.3 / 5.9 (not taken), 512 x 2048 6.9 / 10.9, 512 x 4096 7.0 / 15.9, 512 x 14336 21.1 / 29.1, 1024 x 4096 12.0 / 16.1 (not
-// taken), 1024 x 8192 the same; fp32, 256 x 4096 6.7 / 11.8, 512 x 8192 22.0 / 20.4, 1024 x 8192 36.5 / 29.1 (not taken).
+// 256 x 512 4.9 / 6.1, 512 x 512 6.3 / 5.9 (not taken), 512 x 2048 6.9 / 10.9, 512 x 4096 7.0 / 15.9, 512 x 14336 21.1 / 29.1,
+// 1024 x 4096 12.0 / 16.1 (not taken), 1024 x 8192 the same; fp32, 256 x 4096 6.7 / 11.8, 512 x 8192 22.0 / 20.4, 1024 x 8192
+// 36.5 / 29.1 (not taken).
 inline bool few_rows(const NormBwd& a) { return (a.GW || a.GB) && a.rows > 0 && a.rows <= (a.cols <= 512 ? 256 : 512); }
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
 hipError_t bwd_few_rows(const NormBwd& a, hipStream_t s) {
