@@ -191,7 +191,7 @@ struct Finish {
 #pragma unroll
                     for (int j = 0; j < W; ++j) {
                         z[j] = __builtin_fmaf(x[k][j / 4][j % 4], cs[j], bias[j]);
-                        y[j] = activation<ACT, !F32>(z[j]);
+                        y[j] = activation<ACT, !F32 && !RES>(z[j]);
                         if constexpr (RES) y[j] += P::get(res[k], j);
                     }
                     zs[k] = P::put(z);
@@ -269,8 +269,10 @@ __device__ __forceinline__ void store_one(char* p, float x) {
 template <bool F32>
 __device__ __forceinline__ void finish_one(const GemmArgs& a, const EpilogueArgs& e, int64_t row, int64_t col, float z) {
     float y = 0.0f;
-    with_activation(e.act, [&](auto act) { y = activation<decltype(act)::value, !F32>(z); });
-    if (e.residual) y += load_one<F32>(address<F32>(e.residual, e.ld_res, row, col));
+    with_activation(e.act, [&](auto act) {
+        if (e.residual) y = activation<decltype(act)::value, false>(z) + load_one<F32>(address<F32>(e.residual, e.ld_res, row, col));
+        else y = activation<decltype(act)::value, !F32>(z);
+    });
     if (e.Z) store_one<F32>(address<F32>(e.Z, e.ld_z, row, col), z);
     store_one<F32>(address<F32>(a.C, a.ldc, row, col), y);
 }
@@ -322,8 +324,13 @@ __global__ void __launch_bounds__(256) gemm_i8_epilogue_small_kernel(GemmArgs a,
 #pragma unroll
     for (int j = 0; j < EPT; ++j) z[j] = __builtin_fmaf((float)s.v[j / Sums::VW][j % Sums::VW] * rs, cs[j], bias[j]);
     with_activation(e.act, [&](auto act) {
+        if (e.residual) {
 #pragma unroll
-        for (int j = 0; j < EPT; ++j) y[j] = activation<decltype(act)::value, !F32>(z[j]) + res[j];
+            for (int j = 0; j < EPT; ++j) y[j] = activation<decltype(act)::value, false>(z[j]) + res[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < EPT; ++j) y[j] = activation<decltype(act)::value, !F32>(z[j]);
+        }
     });
     auto store = [&](const void* base, int64_t ld, const float* v) {
         if constexpr (PIECES > 0) {
