@@ -540,7 +540,8 @@ halo_status halo_layer_norm_bwd(const halo_norm_desc* desc, const void* E, int64
  *   step, lr, grad_scale   step counts from 1.  step_ptr, lr_ptr, grad_scale_ptr, where not NULL, are device memory that holds the
  *                          value (step below 1: 1) for this call: a captured graph then takes new ones at every replay.
  *   beta1, beta2           in [0, 1);  lr, eps, weight_decay: finite, not negative;  grad_scale: finite.
- *   count                  at most 1024 tensors, each of at most 2^34 elements.
+ *   count                  at most 1024 tensors, each of at most 2^34 elements.  The call takes up to 246 KB of host memory for their checks, not
+ *                          from the thread's stack (HALO_EHIP if there is none).
  * Pointers are 16-byte aligned, but for the scales, step_ptr (8), lr_ptr and grad_scale_ptr (4 bytes).  What the call writes overlaps
  * nothing else that it reads or writes, or it is refused (HALO_EINVAL; a gradient may belong to several tensors).  The array `tensors`
  * is host memory and is not used after the call returns; addresses are copied into a captured graph.  Infinities and NaN: 32 bits, their

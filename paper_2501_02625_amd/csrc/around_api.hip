@@ -3,6 +3,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <memory>
+#include <new>
 
 #include "around.h"
 #include "halo_internal.h"
@@ -143,8 +145,10 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
     if (count > kMost) return HALO_EUNSUPPORTED;
     const bool eight = d.state_bits == 8;
     const size_t pe = d.param_dt == HALO_BF16 ? 2 : 4, se = eight ? 1 : 4;
-    AdamwTensor list[kMost];
-    Range used[kMost * 7];
+    // on the heap: with 1024 tensors they are 246 KB, more than the whole stack of some threads
+    const std::unique_ptr<AdamwTensor[]> list(new (std::nothrow) AdamwTensor[count]);
+    const std::unique_ptr<Range[]> used(new (std::nothrow) Range[(size_t)count * 7]);
+    if (!list || !used) return from_hip(hipErrorOutOfMemory);
     int n = 0, ranges = 0;
     bool masters = false, plain = false;
     for (int32_t t = 0; t < count; ++t) {
@@ -174,7 +178,7 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
     }
     if (masters && plain) return HALO_EINVAL;
     // A tensor given twice would be updated by two workgroups at once.  Gradients may be shared.
-    std::sort(used, used + ranges, [](const Range& a, const Range& b) { return a.from < b.from; });
+    std::sort(used.get(), used.get() + ranges, [](const Range& a, const Range& b) { return a.from < b.from; });
     uintptr_t end = 0, written_end = 0;      // of what lies in front
     for (int i = 0; i < ranges; ++i) {
         if (used[i].from < (used[i].written ? end : written_end)) return HALO_EINVAL;
@@ -192,7 +196,7 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
     s.step_ptr = d.step_ptr; s.lr_ptr = d.lr_ptr; s.grad_scale_ptr = d.grad_scale_ptr;
     adamw_numbers((double)s.step, s.lr, d.beta1, d.beta2, d.weight_decay, &s.decay, &s.rate, &s.root);
     const int param = d.param_dt == HALO_F32 ? 0 : masters ? 2 : 1;
-    return from_hip(launch_adamw(s, list, n, param, d.grad_dt == HALO_F32 ? 1 : 0, eight ? 1 : 0, reinterpret_cast<hipStream_t>(stream)));
+    return from_hip(launch_adamw(s, list.get(), n, param, d.grad_dt == HALO_F32 ? 1 : 0, eight ? 1 : 0, reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"
