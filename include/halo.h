@@ -543,9 +543,9 @@ halo_status halo_layer_norm_bwd(const halo_norm_desc* desc, const void* E, int64
  *   count                  at most 1024 tensors, each of at most 2^34 elements.  The call takes up to 246 KB of host memory for their checks, not
  *                          from the thread's stack (HALO_EHIP if there is none).
  * Pointers are 16-byte aligned, but for the scales, step_ptr (8), lr_ptr and grad_scale_ptr (4 bytes).  What the call writes overlaps
- * nothing else that it reads or writes, or it is refused (HALO_EINVAL; a gradient may belong to several tensors).  The array `tensors`
- * is host memory and is not used after the call returns; addresses are copied into a captured graph.  Infinities and NaN: 32 bits, their
- * own elements; 8 bits, their 256 elements' states and own parameters.
+ * nothing else that it reads or writes, what step_ptr, lr_ptr and grad_scale_ptr point to among it, or it is refused (HALO_EINVAL; a
+ * gradient may belong to several tensors).  The array `tensors` is host memory and is not used after the call returns; addresses are copied
+ * into a captured graph.  Infinities and NaN: 32 bits, their own elements; 8 bits, their 256 elements' states and own parameters.
  */
 #define HALO_ADAMW_BLOCK 256
 typedef struct halo_adamw_tensor {

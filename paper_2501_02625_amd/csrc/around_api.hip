@@ -147,10 +147,13 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
     const size_t pe = d.param_dt == HALO_BF16 ? 2 : 4, se = eight ? 1 : 4;
     // on the heap: with 1024 tensors they are 246 KB, more than the whole stack of some threads
     const std::unique_ptr<AdamwTensor[]> list(new (std::nothrow) AdamwTensor[count]);
-    const std::unique_ptr<Range[]> used(new (std::nothrow) Range[(size_t)count * 7]);
+    const std::unique_ptr<Range[]> used(new (std::nothrow) Range[(size_t)count * 7 + 3]);
     if (!list || !used) return from_hip(hipErrorOutOfMemory);
     int n = 0, ranges = 0;
     bool masters = false, plain = false;
+    auto add = [&](const void* p, size_t bytes, bool written = true) {
+        if (p) used[ranges++] = Range{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written};
+    };
     for (int32_t t = 0; t < count; ++t) {
         const halo_adamw_tensor& x = tensors[t];
         if (x.size < 0) return HALO_EINVAL;
@@ -161,9 +164,6 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
         if (x.size > (int64_t(1) << 34)) return HALO_EUNSUPPORTED;
         if (!aligned(x.param, 16) || !aligned(x.grad, 16) || !aligned(x.m, 16) || !aligned(x.v, 16) || !aligned(x.master, 16)) return HALO_EALIGN;
         if (eight && (!aligned(x.m_scale, 4) || !aligned(x.v_scale, 4))) return HALO_EALIGN;
-        auto add = [&](const void* p, size_t bytes, bool written = true) {
-            if (p) used[ranges++] = Range{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written};
-        };
         const size_t size = (size_t)x.size, blocks = (size + HALO_ADAMW_BLOCK - 1) / HALO_ADAMW_BLOCK;
         add(x.param, size * pe);
         add(x.grad, size * (d.grad_dt == HALO_BF16 ? 2 : 4), false);
@@ -177,7 +177,11 @@ halo_status halo_adamw(const halo_adamw_desc* desc, const halo_adamw_tensor* ten
         list[n++] = AdamwTensor{x.param, x.grad, x.m, x.v, x.master, x.m_scale, x.v_scale, x.size, t};
     }
     if (masters && plain) return HALO_EINVAL;
-    // A tensor given twice would be updated by two workgroups at once.  Gradients may be shared.
+    // A tensor given twice would be updated by two workgroups at once, and every workgroup reads the step's numbers.  What is only read may be
+    // shared.
+    add(d.step_ptr, 8, false);
+    add(d.lr_ptr, 4, false);
+    add(d.grad_scale_ptr, 4, false);
     std::sort(used.get(), used.get() + ranges, [](const Range& a, const Range& b) { return a.from < b.from; });
     uintptr_t end = 0, written_end = 0;      // of what lies in front
     for (int i = 0; i < ranges; ++i) {
