@@ -422,11 +422,9 @@ hipError_t launch_split_by_columns(const GemmArgs& a, const EpilogueArgs& e, hip
 }
 template <bool F32>
 hipError_t launch_by_shape(const GemmArgs& a, const EpilogueArgs& e, hipStream_t s) {
-    if (a.config < 0 && small_tiles_twice(a)) return launch_split<4, 4, F32>(a, e, s);
-    if (a.config < 0 && short_k_tiles128(a)) return launch_tiled<4, 4, F32>(a, e, s);
-    const int64_t wide = two_widths(a);      // -1 where N is no multiple of 16 or one width is faster
-    if (wide >= 0) return launch_two_widths<F32>(a, e, wide, s);
-    switch (a.config < 0 ? choose_config(a, nullptr) : a.config) {
+    const EpilogueWay way = epilogue_way(a);
+    if (way.wide >= 0) return launch_two_widths<F32>(a, e, way.wide, s);
+    switch (way.config) {
         case 0:
         case 1: return launch_tiled<8, 8, F32>(a, e, s);
         case 2: return launch_tiled<8, 4, F32>(a, e, s);

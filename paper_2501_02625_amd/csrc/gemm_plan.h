@@ -212,6 +212,19 @@ inline bool short_k_tiles128(const GemmArgs& a) {
     return a.K <= 768 && tiles_of(a, 256, 128) > kComputeUnits && choose_config(a, nullptr) == kTiles256x128;
 }
 
+// How the product with an epilogue is run: config, or, where wide is not -1, the first `wide` columns in tiles of 256 x 256 and the others in
+// 256 x 192.
+struct EpilogueWay {
+    int config;
+    int64_t wide;
+};
+inline EpilogueWay epilogue_way(const GemmArgs& a) {
+    if (a.config < 0 && small_tiles_twice(a)) return {kSmall64, -1};
+    if (a.config < 0 && short_k_tiles128(a)) return {kTiles128, -1};
+    const int64_t wide = two_widths(a);      // -1 where N is no multiple of 16 or one width is faster
+    return {wide >= 0 ? kTiles256 : a.config < 0 ? choose_config(a, nullptr) : a.config, wide};
+}
+
 // Estimated microseconds of launch_gemm_i8(a) / launch_gemm_i8_pair(a, *a2), for choices between ways to split the work.
 inline double gemm_i8_cost(const GemmArgs& a, const GemmArgs* a2) {
     const int c = a.config < 0 ? choose_config(a, a2) : a.config;

@@ -12,6 +12,8 @@ from tests.around_util import DTYPES, HALF, U, act_bound, host, matrix, target, 
 from tests.gpu_util import DEV
 
 pytestmark = pytest.mark.gpu
+# tiles of 256 x 192, and behind tiles of 256 x 256
+WIDE = [(2199, 5312, 1024, torch.bfloat16), (4531, 5520, 1024, torch.bfloat16), (4231, 6688, 1024, torch.float32)]
 ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
 
 
@@ -50,6 +52,6 @@ def test_every_tile(dtype, config):
     call(515, 700, 256, "gelu", dtype, config)
 
 
-@pytest.mark.parametrize("M,N,K,dtype", [(2199, 5312, 1024, torch.bfloat16), (4531, 5520, 1024, torch.bfloat16), (4231, 6688, 1024, torch.float32)])
+@pytest.mark.parametrize("M,N,K,dtype", WIDE)
 def test_two_widths(M, N, K, dtype):
     call(M, N, K, "gelu", dtype)
