@@ -11,6 +11,7 @@
 
 #include "around.h"
 #include "eight.h"
+#include "norm_plan.h"
 #include "wave_ops.h"
 
 namespace halo {
@@ -503,14 +504,10 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBwd a, int64_t ro
 // group of 256 / four of 64, 2048 x 4096 9.7 / 12.5; one of 512 / two of 256, 4096 x 8192 25.0 / 24.1, 4096 x 64 3.4 / 3.9; one of 1024 / two of
 // 512, 8192 x 2048 15.5 / 18.4; backward one of 512 / two of 256, 4096 x 2048 14.5 / 15.4.
 //
-// Workgroups of a launch: enough for every compute unit to hold several at once; each goes through its rows.  Forward 2^19 threads: 2^18 /
-// 2^19 / 2^20, 4096 x 8192 28.4 us / 25.0 / 24.4, 14336 x 1024 14.8 / 16.2 / 19.4, 1000 x 16384 14.5 / 14.9 / 16.3.  The gradient's hold 1024
-// threads of a compute unit's, or 512 where a thread has four groups: every one more writes a part of the sums and has fewer rows to
-// have on their way.  EX, G_W and G_B in bf16, 256 / 512 / 768 workgroups: 8192 x 4096 (512 lanes) 53.8 us / 47.4 / 53.6, 2048 x 8192 with
-// 1024 lanes 27.1 / 36 / 42, 1024 x 14336 (512 lanes, four groups) 38.4 / 46.4 / 53.6, 8192 x 512 12.1 / 10.4 / 9.8.
-constexpr int64_t kThreadsFwd = 1 << 19, kMostBwd = 512;
-template <int LANES, int GROUPS>
-constexpr int64_t most_bwd() { return LANES >= 1024 || GROUPS >= 4 ? kMostBwd / 2 : kMostBwd; }
+// Workgroups of a launch: enough for every compute unit to hold several at once; each goes through its rows.  Forward 2^19 threads, rows x
+// columns: 2^18 / 2^19 / 2^20, 8192 x 4096 28.4 us / 25.0 / 24.4, 1024 x 14336 14.8 / 16.2 / 19.4, 16384 x 1000 14.5 / 14.9 / 16.3.  The gradient's:
+// norm_plan.h.
+constexpr int64_t kThreadsFwd = 1 << 19;
 inline unsigned groups_of(int64_t rows, int teams, int64_t most) {
     const int64_t n = (rows + teams - 1) / teams;
     return (unsigned)(n < most ? n : most);
@@ -537,15 +534,9 @@ hipError_t fwd_by_shape(const NormFwd& a, hipStream_t s) {
     return fwd<E, W32, 512, 8, 1>(a, s);
 }
 
-// Few rows, 256 up to 512 columns and 512 beyond: E_X and the sums of the columns in one launch, by workgroups of their own, which read E
-// and X once more.  Layer norm with a base in a graph, one launch / parts and their sum: bf16, 64 x 512 4.1 us / 5.6, 128 x 14336 7.6 / 19.8,
-// 256 x 512 4.9 / 6.1, 512 x 512 6.3 / 5.9 (not taken), 512 x 2048 6.9 / 10.9, 512 x 4096 7.0 / 15.9, 512 x 14336 21.1 / 29.1,
-// 1024 x 4096 12.0 / 16.1 (not taken), 1024 x 8192 the same; fp32, 256 x 4096 6.7 / 11.8, 512 x 8192 22.0 / 20.4, 1024 x 8192
-// 36.5 / 29.1 (not taken).
-inline bool few_rows(const NormBwd& a) { return (a.GW || a.GB) && a.rows > 0 && a.rows <= (a.cols <= 512 ? 256 : 512); }
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
 hipError_t bwd_few_rows(const NormBwd& a, hipStream_t s) {
-    const unsigned groups = a.EX ? groups_of(a.rows, TEAMS, kMostBwd) : 0, columns = (unsigned)(a.cols + 63) / 64;
+    const unsigned groups = a.EX ? groups_of(a.rows, TEAMS, kMostNormBwd) : 0, columns = (unsigned)(a.cols + 63) / 64;
     auto launch = [&](unsigned rows, unsigned behind) {
         hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, false>), dim3(rows + behind), dim3(LANES * TEAMS), 0, s, a, rows);
     };
@@ -560,25 +551,21 @@ hipError_t bwd_few_rows(const NormBwd& a, hipStream_t s) {
 
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
 hipError_t bwd(const NormBwd& a, hipStream_t s) {
-    if (few_rows(a)) return bwd_few_rows<E, W32, LANES, GROUPS, TEAMS>(a, s);
     const bool sums = a.GW || a.GB;
-    const unsigned groups = groups_of(a.rows, TEAMS, most_bwd<LANES, GROUPS>());
+    if (sums && norm_bwd_one_launch(a.rows, a.cols)) return bwd_few_rows<E, W32, LANES, GROUPS, TEAMS>(a, s);
+    // as many parts as the workspace query counts
+    const unsigned groups = sums ? (unsigned)norm_bwd_parts(a.rows, a.cols, a.f32) : groups_of(a.rows, TEAMS, most_norm_bwd(a.cols));
     if (groups && sums) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, true>), dim3(groups), dim3(LANES * TEAMS), 0, s, a, groups);
     else if (groups) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, false>), dim3(groups), dim3(LANES * TEAMS), 0, s, a, groups);
     if (sums) return launch_sum_parts(a.part, a.GW, a.part + groups * ((a.cols + 3) / 4 * 4), a.GB, groups, a.cols, (a.cols + 3) / 4 * 4, s);
     return hipGetLastError();
 }
-// Rows without room for the sums: these in a launch of their own, in `parts` parts of the rows.  They go first: EX may be E itself.
-constexpr bool apart(int64_t cols, bool f32) { return cols > (f32 ? 8192 : 16384); }
-inline int64_t apart_parts(int64_t rows, int64_t cols) {
-    const int64_t tiles = (cols + 511) / 512, most = 2048 / tiles, parts = (rows + 15) / 16;
-    return parts < most ? parts : most;
-}
+// Rows without room for the sums: these in a launch of their own, in parts of the rows.  They go first: EX may be E itself.
 template <typename E, bool W32, int GROUPS>
 hipError_t bwd_apart(const NormBwd& a, hipStream_t s) {
-    if (few_rows(a)) return bwd_few_rows<E, W32, 512, GROUPS, 1>(a, s);
+    if ((a.GW || a.GB) && norm_bwd_one_launch(a.rows, a.cols)) return bwd_few_rows<E, W32, 512, GROUPS, 1>(a, s);
     if (a.GW || a.GB) {
-        const int64_t tiles = (a.cols + 511) / 512, most = apart_parts(a.rows, a.cols);
+        const int64_t tiles = (a.cols + 511) / 512, most = norm_bwd_parts(a.rows, a.cols, a.f32);
         const int64_t per = most ? (a.rows + most - 1) / most : 1, parts = (a.rows + per - 1) / per;
         if (parts) hipLaunchKernelGGL((norm_columns_kernel<E>), dim3((unsigned)tiles, (unsigned)parts), dim3(256), 0, s, a, per);
         const hipError_t e = launch_sum_parts(a.part, a.GW, a.part + parts * ((a.cols + 3) / 4 * 4), a.GB, parts, a.cols,
@@ -586,7 +573,7 @@ hipError_t bwd_apart(const NormBwd& a, hipStream_t s) {
         if (e != hipSuccess) return e;
     }
     if (a.EX && a.rows) {
-        const unsigned groups = groups_of(a.rows, 1, kMostBwd);
+        const unsigned groups = groups_of(a.rows, 1, kMostNormBwd);
         hipLaunchKernelGGL((norm_bwd_kernel<E, W32, 512, GROUPS, 1, false>), dim3(groups), dim3(512), 0, s, a, groups);
     }
     return hipGetLastError();
@@ -602,7 +589,7 @@ hipError_t bwd_by_shape(const NormBwd& a, hipStream_t s) {
     if (c <= 2048) return bwd<E, W32, 256, 1, 1>(a, s);
     if (c <= 4096) return bwd<E, W32, 512, 1, 1>(a, s);
     if (c <= 8192) return bwd<E, W32, 1024, 1, 1>(a, s);
-    if constexpr (!apart(16384, sizeof(E) == 4)) {
+    if constexpr (!norm_bwd_apart(16384, sizeof(E) == 4)) {
         if (c <= 16384) return bwd<E, W32, 512, 4, 1>(a, s);
     }
     return c <= 16384 ? bwd_apart<E, W32, 4>(a, s) : bwd_apart<E, W32, 8>(a, s);
@@ -611,7 +598,8 @@ hipError_t bwd_by_shape(const NormBwd& a, hipStream_t s) {
 }  // namespace
 
 size_t norm_bwd_workspace_floats(int64_t rows, int64_t cols, int f32) {
-    const int64_t parts = apart(cols, f32 != 0) ? apart_parts(rows, cols) : rows < kMostBwd ? rows : kMostBwd;
+    // one part where none is written: a call that wants sums brings a workspace, whatever its rows
+    const int64_t parts = norm_bwd_one_launch(rows, cols) ? 1 : norm_bwd_parts(rows, cols, f32 != 0);
     return 2 * (size_t)parts * (size_t)((cols + 3) / 4 * 4);
 }
 
