@@ -552,7 +552,7 @@ hipError_t bwd_few_rows(const NormBwd& a, hipStream_t s) {
 template <typename E, bool W32, int LANES, int GROUPS, int TEAMS>
 hipError_t bwd(const NormBwd& a, hipStream_t s) {
     const bool sums = a.GW || a.GB;
-    if (sums && norm_bwd_one_launch(a.rows, a.cols)) return bwd_few_rows<E, W32, LANES, GROUPS, TEAMS>(a, s);
+    if (sums && norm_bwd_one_launch(a.rows, a.cols, a.f32)) return bwd_few_rows<E, W32, LANES, GROUPS, TEAMS>(a, s);
     // as many parts as the workspace query counts
     const unsigned groups = sums ? (unsigned)norm_bwd_parts(a.rows, a.cols, a.f32) : groups_of(a.rows, TEAMS, most_norm_bwd(a.cols));
     if (groups && sums) hipLaunchKernelGGL((norm_bwd_kernel<E, W32, LANES, GROUPS, TEAMS, true>), dim3(groups), dim3(LANES * TEAMS), 0, s, a, groups);
@@ -563,7 +563,7 @@ hipError_t bwd(const NormBwd& a, hipStream_t s) {
 // Rows without room for the sums: these in a launch of their own, in parts of the rows.  They go first: EX may be E itself.
 template <typename E, bool W32, int GROUPS>
 hipError_t bwd_apart(const NormBwd& a, hipStream_t s) {
-    if ((a.GW || a.GB) && norm_bwd_one_launch(a.rows, a.cols)) return bwd_few_rows<E, W32, 512, GROUPS, 1>(a, s);
+    if ((a.GW || a.GB) && norm_bwd_one_launch(a.rows, a.cols, a.f32)) return bwd_few_rows<E, W32, 512, GROUPS, 1>(a, s);
     if (a.GW || a.GB) {
         const int64_t tiles = (a.cols + 511) / 512, most = norm_bwd_parts(a.rows, a.cols, a.f32);
         const int64_t per = most ? (a.rows + most - 1) / most : 1, parts = (a.rows + per - 1) / per;
@@ -599,7 +599,7 @@ hipError_t bwd_by_shape(const NormBwd& a, hipStream_t s) {
 
 size_t norm_bwd_workspace_floats(int64_t rows, int64_t cols, int f32) {
     // one part where none is written: a call that wants sums brings a workspace, whatever its rows
-    const int64_t parts = norm_bwd_one_launch(rows, cols) ? 1 : norm_bwd_parts(rows, cols, f32 != 0);
+    const int64_t parts = norm_bwd_one_launch(rows, cols, f32 != 0) ? 1 : norm_bwd_parts(rows, cols, f32 != 0);
     return 2 * (size_t)parts * (size_t)((cols + 3) / 4 * 4);
 }
 

@@ -102,3 +102,12 @@ def test_few_rows_in_the_place_of_x():
         whole = binding.halo_layer_norm_bwd(e, x, mean, rstd, w, base=base)
         got = binding.halo_layer_norm_bwd(e, x, mean, rstd, w, base=base, EX=x)
         assert got[0].data_ptr() == x.data_ptr() and all(torch.equal(a, b) for a, b in zip(got, whole))
+
+
+@pytest.mark.parametrize("rows", [432, 433])
+@pytest.mark.parametrize("cols", [4097, 8192])
+def test_fp32_rows_of_16_to_32_kb(cols, rows):
+    """Both sides of the number of rows from which on they take two launches."""
+    e, x, mean, rstd, w, base = case(rows, cols, torch.float32, torch.float32, "layer", 11)
+    ex, gw, gb = binding.halo_layer_norm_bwd(e, x, mean, rstd, w, base=base)
+    check_bwd(e, x, mean, rstd, w, base, "layer", ex, gw, gb, "%d x %d" % (rows, cols))
