@@ -428,8 +428,9 @@ halo_status halo_adapters_bwd(const halo_adapters_desc* desc, const void* E, int
  *   Z[i,j] = z[i,j] rounded to c_dt;        C[i,j] = act(z[i,j]) + residual[i,j] rounded to c_dt
  *
  *   act       none: x; relu: max(x, 0); gelu: x Phi(x), Phi the normal distribution function; gelu_tanh: x / (1 + exp(-2 u)) with
- *             u = sqrt(2 / pi) (x + 0.044715 x^3); silu: x / (1 + exp(-x)).  Where c_dt is bf16 and there is no residual, gelu is up to 2^-14.9 of itself
- *             off before it is rounded (half a step of bf16 is 2^-9 to 2^-8), otherwise, as all others, some roundings of fp32.
+ *             u = sqrt(2 / pi) (x + 0.044715 x^3); silu: x / (1 + exp(-x)).  Where c_dt is bf16 and there is no residual, gelu is up to
+ *             2^-14.9 of itself off before it is rounded (half a step of bf16 is 2^-9 to 2^-8), otherwise, as all others, some roundings of
+ *             fp32 (below 1e-30 it may be 0).
  *   bias      [N], bf16 or fp32 (bias_dt), 16-byte aligned; NULL = 0.
  *   residual  [M x N] of type c_dt; NULL = 0.  May be C itself, with the same leading dimension.
  *   Z         [M x N] of type c_dt, for halo_activation_bwd; NULL: not kept.

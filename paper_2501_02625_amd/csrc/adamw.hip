@@ -6,7 +6,7 @@
 // above v by the variance of the rounding, every step again), they follow.
 //
 // What bounds it: memory with states in 32 bits (12.6M elements in fp32 71 us, 5.0 TB/s; a large copy reaches 5.1), with 8 bits
-// instructions as much, some hundred an element: 219M elements in bf16 500 to 530 us on different cards, 4.1 to 4.4 TB/s; 467 without the
+// instructions as much, some hundred an element: 219M elements in bf16 492 to 530 us on different cards, 4.1 to 4.5 TB/s; 467 without the
 // random numbers where it takes 530.  There one round instead of two 545, and loads that stay in the caches 537; before the roots were what
 // they are, four rounds as two.
 #pragma clang fp contract(off)
@@ -188,7 +188,8 @@ __device__ __forceinline__ uint32_t most_of_32(uint32_t x) { return more_of<4>(m
 // root = sqrt(v) and quotient = m / (root * by + eps), each rounded to nearest as the language's root and division are, of which this
 // is the inner part: what they spend on arguments near the ends of the range is left out where a wavefront has none of those.  Then the
 // remainders v - s s and m - d q are exact, and one Newton step from the hardware's reciprocal root (two from its reciprocal) rounds
-// correctly: of the root that was tried for every significand, with even and odd exponents; the quotient's steps are those of the division.
+// correctly: of the root a test tries every significand, with even and odd exponents; the quotient's steps are those of the division, and the same
+// test takes quotients next to the middle between two numbers.
 // (The language's own for all: 566 us for 219M elements in bf16 with states in 8 bits instead of 523.)
 __device__ __forceinline__ void roots_and_quotients(const float (&v)[8], const float (&m)[8], float by, float eps,
                                                     float (&root)[8], float (&quotient)[8], uint32_t& most_m) {

@@ -499,10 +499,10 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormBwd a, int64_t ro
 }
 
 // Lanes and groups of a row.  As many lanes as the row has pieces of eight, up to 64, so that no wavefront meets another; beyond 512
-// columns two groups or more lanes, whichever was faster.  Forward, bf16, columns and rows: two groups of 64 lanes / one of 128, 1000 x
-// 16384 15.0 us / 16.0, but backward, where sums take registers, four teams of 128 lanes, 1003 x 1031 in fp32 6.3 us, and of 64 7.6; one
-// group of 256 / four of 64, 2048 x 4096 9.7 / 12.5; one of 512 / two of 256, 4096 x 8192 25.0 / 24.1, 4096 x 64 3.4 / 3.9; one of 1024 / two of
-// 512, 8192 x 2048 15.5 / 18.4; backward one of 512 / two of 256, 4096 x 2048 14.5 / 15.4.
+// columns two groups or more lanes, whichever was faster.  Rows x columns, forward, bf16: two groups of 64 lanes / one of 128, 16384 x 1000
+// 15.0 us / 16.0, but backward, where sums take registers, four teams of 128 lanes, 1031 x 1003 in fp32 6.3 us, and of 64 7.6; one
+// group of 256 / four of 64, 4096 x 2048 9.7 / 12.5; one of 512 / two of 256, 8192 x 4096 25.0 / 24.1, 64 x 4096 3.4 / 3.9; one of 1024 / two of
+// 512, 2048 x 8192 15.5 / 18.4; backward one of 512 / two of 256, 2048 x 4096 14.5 / 15.4.
 //
 // Workgroups of a launch: enough for every compute unit to hold several at once; each goes through its rows.  Forward 2^19 threads, rows x
 // columns: 2^18 / 2^19 / 2^20, 8192 x 4096 28.4 us / 25.0 / 24.4, 1024 x 14336 14.8 / 16.2 / 19.4, 16384 x 1000 14.5 / 14.9 / 16.3.  The gradient's:

@@ -17,9 +17,9 @@ inline int norm_bwd_teams(int64_t cols) { return cols <= 64 ? 32 : cols <= 128 ?
 // Few rows: E_X and the sums of the columns in one launch, by workgroups of their own, which read E and X once more.  512 rows at most, 256 up
 // to 512 columns, and in fp32 432 from 4097 to 8192, from where on the second reading costs more than the second launch.
 // Layer norm with a base in a graph, rows x columns, one launch / parts and their sum:
-//   bf16  64 x 512 4.5 us / 6.0, 256 x 512 5.3 / 6.5, 512 x 256 6.6 / 6.2 and 512 x 64 6.4 / 5.6 (not taken), 512 x 2048 7.3 / 11.2, 512 x 4096 7.4 / 16.2,
-//         512 x 8192 13.1 / 16.8, 512 x 14336 21.6 / 29.1, 512 x 32768 42 / 49; not taken 768 x 4096 9.6 / 16.3, 1024 x 4096 12.6 / 16.4, 1024 x 8192
-//         21.4 / 20.6
+//   bf16  64 x 512 4.5 us / 6.0, 256 x 512 5.3 / 6.5, 512 x 256 6.6 / 6.2 and 512 x 64 6.4 / 5.6 (not taken), 512 x 2048 7.3 / 11.2, 512 x 4096
+//         7.4 / 16.2, 512 x 8192 13.1 / 16.8, 512 x 14336 21.6 / 29.1, 512 x 32768 42 / 49; not taken 768 x 4096 9.6 / 16.3, 1024 x 4096 12.6 /
+//         16.4, 1024 x 8192 21.4 / 20.6
 //   fp32  256 x 512 6.6 / 6.6, 256 x 64 6.5 / 5.6 (taken: the host's part of a second launch, 3 us, is not in these), 512 x 512 9.4 / 6.6 (not
 //         taken), 512 x 4096 13.1 / 16.5; 5000 columns, 416 rows 14.2 / 15.6, 448 16.7 / 15.8, 512 17.8 / 16.6; 8192, 384 17.0 / 18.1, 416 19.4 /
 //         18.7, 512 22.3 / 20.6; 512 x 14336 37 / 42, 512 x 32768 114 / 128; 1024 x 8192 36.9 / 29.4 (not taken)

@@ -31,8 +31,8 @@ def test_workspace(lib, rows, cols, dt, parts):
 
 
 @pytest.mark.parametrize("rows,cols,dt,parts", [
-    (432, 8192, F32, 1), (433, 8192, F32, 256), (512, 8192, F32, 256), (432, 4097, F32, 1), (512, 4097, F32, 256), (512, 4096, F32, 1), (512, 8193, F32, 1),
-    (512, 4097, BF16, 1), (512, 8192, BF16, 1),
+    (432, 8192, F32, 1), (433, 8192, F32, 256), (512, 8192, F32, 256), (432, 4097, F32, 1), (512, 4097, F32, 256), (512, 4096, F32, 1),
+    (512, 8193, F32, 1), (512, 4097, BF16, 1), (512, 8192, BF16, 1),
 ])
 def test_one_launch_where_it_is_the_faster_way(lib, rows, cols, dt, parts):
     """fp32 rows of 16 to 32 KB: two launches from some 430 rows on (512 x 8192 20.6 us, one launch 22.3)."""
