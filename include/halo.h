@@ -489,7 +489,7 @@ halo_status halo_activation_bwd(const void* E, int64_t ld_e, const void* Z, int6
  *   EX, GW, GB          any may be NULL to skip it (not all three).  GW, GB fp32 [cols], 16-byte aligned; 0 where rows == 0.
  *   workspace           halo_layer_norm_bwd_workspace_bytes(desc) bytes, 16-byte aligned, for GW and GB only.
  * All in fp32, each result rounded once.  The squares are summed about the mean, in a second pass over the row in registers.  cols == 0
- * is a no-op, and so is rows == 0 but for GW and GB.
+ * is a no-op, which writes no statistics either, and so is rows == 0 but for GW and GB.
  */
 typedef enum { HALO_NORM_LAYER = 0, HALO_NORM_RMS = 1 } halo_norm_kind;
 

@@ -5,8 +5,8 @@
 // What bounds it is the product (the chip's power) and then the arithmetic behind it, of which a compute unit does nothing else meanwhile.
 // bf16 out, 8192 x 14336 x 4096: without any part of the epilogue 365 us, as the plain product; with silu and Z 386, with gelu and Z 425, on
 // other cards 404 to 436 (2.26 POP/s; 8192^3 without an epilogue 2.44); a pass of its own from Z to C would be 92 us at a large copy's
-// rate.  2048 x 4096 x 14336 with bias and residual 107 to 110, one row of 4096 x 4096 with them 4.5 (weights in the caches), 777 x 1003 x 1008 in fp32 with everything
-// 9.6, without any part 7.8 (the plain product 7.1); there in tiles of 32 x 64 10.9, of 128 x 128 12.0.
+// rate.  2048 x 4096 x 14336 with bias and residual 107 to 110, one row of 4096 x 4096 with them 4.5 (weights in the caches), 777 x 1003 x
+// 1008 in fp32 with everything 9.6, without any part 7.8 (the plain product 7.1); there in tiles of 32 x 64 10.9, of 128 x 128 12.0.
 #pragma clang fp contract(off)
 
 #include "activation.h"

@@ -585,6 +585,7 @@ PyObject* layer_norm_fwd(PyObject* const* a) {
     require(matrix(X, d.rows, d.cols, X->scalar_type()) && matrix(y, d.rows, d.cols, X->scalar_type()), "X and Y are matrices of one shape and type, with contiguous rows");
     require(floats(m, d.rows) && floats(r, d.rows), "mean and rstd are fp32, one element for each row");
     const bool stats = a[5] == Py_True, want_mean = (stats || m) && kind == HALO_NORM_LAYER, want_rstd = stats || r;
+    require(d.cols > 0 || d.rows == 0 || !(want_mean || want_rstd), "rows without columns have no statistics");
     const Context c;
     on_current_device(c, {X, w, b, y, m, r});
     const at::Tensor Y = y ? *y : new_padded(d.rows, d.cols, X->scalar_type(), *X, c.device),

@@ -111,3 +111,13 @@ def test_fp32_rows_of_16_to_32_kb(cols, rows):
     e, x, mean, rstd, w, base = case(rows, cols, torch.float32, torch.float32, "layer", 11)
     ex, gw, gb = binding.halo_layer_norm_bwd(e, x, mean, rstd, w, base=base)
     check_bwd(e, x, mean, rstd, w, base, "layer", ex, gw, gb, "%d x %d" % (rows, cols))
+
+
+def test_no_columns():
+    """Results as empty as the matrix; statistics are refused (tests/test_norm_without_columns.py)."""
+    x, v, w = torch.empty(5, 0, device=DEV), torch.ones(5, device=DEV), torch.empty(0, device=DEV)
+    y, mean, rstd = binding.halo_layer_norm_fwd(x, w, w, want_stats=False)
+    assert y.shape == (5, 0) and mean is None and rstd is None
+    assert [t.shape for t in binding.halo_layer_norm_bwd(x, x, v, v, w)] == [(5, 0), (0,), (0,)]
+    with pytest.raises(AssertionError):
+        binding.halo_layer_norm_fwd(x)
